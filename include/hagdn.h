@@ -201,6 +201,117 @@ int kda_decode(const void *q, const void *k, const void *v, const float *g,
                int num_slots, int N, int Hqk, int Hv, int Dk, int Dv,
                float scale, int dtype, int pre, void *o, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Gated linear recurrence (GLR): the channelwise relative of the delta rule,
+ * for layers whose mixer carries D independent scalars per sequence,
+ *   h_t = a_t h_{t-1} + w_t x_t,    a_t = e^(g_t),    w_t = 1 or 1 - a_t,
+ * over packed sequences, with its backward pass and a step for single tokens.
+ * The conventions above hold, except:
+ *   Token tensors are matrices of T rows (N for glr_decode) and D channels.
+ *   Inputs (x, g, dh) may be column slices of a wider matrix: each has a row
+ *   stride in ELEMENTS (>= 0; 0 repeats one row), channels being contiguous.
+ *   Outputs are contiguous.  Pointers need only their element's alignment
+ *   (workspace: 16 bytes).  D >= 1, any.
+ *   dtype is the type of x, h, dh and dx; gate_dtype that of g and dg:
+ *   HAGDN_F32, or (with dtype bf16 only) HAGDN_BF16.  States, sums and gate
+ *   arithmetic are fp32.
+ *   cu_seqlens may be NULL for N = 1: one sequence of T tokens.
+ *   convex: 0: w_t = 1;  1: w_t = 1 - a_t (h is a running weighted mean of x).
+ *   pre: 0, or HAGDN_PRE_GATE_SOFTPLUS: g holds raw values r and the log-gate is
+ *   -softplus(r), that is a_t = 1 / (1 + e^r); dg is then the gradient of r.
+ *   A finite g > 0 grows the state.  g = -inf (a = 0) forgets it, unless it is
+ *   not finite.  No value of one sequence reaches another.
+ * Malformed cu_seqlens: no token is processed (h, dx, dg, checkpoints untouched;
+ *   s_final receives s0 or zeros, ds0 dfinal or zeros) and hagdn_device_status()
+ *   reports HAGDN_DEV_BAD_SEQLENS. */
+
+/* Bytes of workspace glr_prefill and glr_backward need (0 on invalid sizes). */
+size_t glr_workspace_size(int T_total, int D);
+
+/* Forward.  s0, s_final: [N, D] fp32 or NULL, s_final may be s0 itself (exactly).
+ * checkpoints: NULL, or [ceil(T / 64), D] fp32, what glr_backward needs of the
+ * forward pass: entry i receives the state before packed token 64 i (unspecified
+ * where that token starts a sequence). */
+int glr_prefill(const void *x, int64_t x_stride, const void *g, int64_t g_stride,
+                const float *s0, const int32_t *cu_seqlens, int N, int T_total, int D,
+                int dtype, int gate_dtype, int convex, int pre, void *h, float *s_final,
+                float *checkpoints, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Backward: from dh, the gradient of h, and dfinal [N, D] fp32 (NULL: zero), that of
+ * s_final, the gradients of x, of g (as given: raw values under
+ * HAGDN_PRE_GATE_SOFTPLUS) and, if ds0 != NULL, of s0.  With d_t the whole gradient
+ * of h_t and e_t = a_t d_t,
+ *   d_t = dh_t + e_{t+1},  dx_t = w_t d_t,  d(log a_t) = e_t (h_{t-1} - [convex] x_t),
+ *   ds0 = e at the sequence's first token (e past the last: dfinal).
+ * x, g, s0, cu_seqlens, convex, pre: as in the forward call; checkpoints: what it
+ * wrote.  h itself is not read: its states are formed again from the checkpoints in
+ * fp32.  ds0 may be dfinal itself. */
+int glr_backward(const void *dh, int64_t dh_stride, const void *x, int64_t x_stride,
+                 const void *g, int64_t g_stride, const float *checkpoints, const float *s0,
+                 const float *dfinal, const int32_t *cu_seqlens, int N, int T_total, int D,
+                 int dtype, int gate_dtype, int convex, int pre, void *dx, void *dg,
+                 float *ds0, void *workspace, size_t workspace_bytes, void *stream);
+
+/* One token for each of N sequences: state [num_slots, D] fp32 is updated in place,
+ * h [N, D] receives the new states.  slots as in gdn_decode (NULL: sequence n in slot
+ * n; a slot outside [0, num_slots) is padding: its row of h is zero). */
+int glr_decode(const void *x, int64_t x_stride, const void *g, int64_t g_stride,
+               float *state, const int32_t *slots, int num_slots, int N, int D,
+               int dtype, int gate_dtype, int convex, int pre, void *h, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Norms before and after a block.  RMS norms: norm(v) = v / sqrt(mean(v^2) + eps).
+ * Rows of D >= 1 elements (at most 16384); inputs may be column slices (row strides in
+ * elements, >= 0), outputs are contiguous, pointers need their element's alignment.
+ * dtype: the block's operands; res_dtype: the residual stream, HAGDN_F32 or (with
+ * dtype bf16 only) HAGDN_BF16.  Weights and their gradients are fp32, all sums too.
+ * T = 0 is a no-op for the rows (weight gradients are zero).
+ *
+ * add_norm: a block's output x joins the residual stream and the next block's input
+ * is formed,
+ *   u = x, or norm(x) post_weight;   r' = res + scale u;   y = norm(r') weight.
+ * res NULL: zero.  scale_vec [D] replaces the number scale unless NULL; post_weight
+ * [D] or NULL.  y [T, D] dtype; res_out [T, D] res_dtype (r' rounded; y is formed from
+ * r' before rounding), or NULL, and it may be res itself if res is contiguous. */
+int hagdn_add_norm(const void *x, int64_t x_stride, const void *res, int64_t res_stride,
+                   const float *weight, const float *post_weight, const float *scale_vec,
+                   float scale, float eps, int T, int D, int dtype, int res_dtype, void *y,
+                   void *res_out, void *stream);
+
+/* Backward, from dy and dres (the gradient that reaches r' besides y; NULL: zero):
+ *   dres_out = dres + the gradient through y (the gradient of r', and of res);
+ *   dx; dweight [D]; dscale [D] (if scale_vec); dpost [D] (if post_weight).
+ * res here is r', as add_norm stored it; x is read only with scale_vec or
+ * post_weight (NULL otherwise).  dres_out may be NULL, or dres itself if that is
+ * contiguous.  Weight gradients are summed in an order that depends only on T, D
+ * and the device. */
+size_t hagdn_add_norm_workspace_size(int T, int D, int has_scale_vec, int has_post);
+int hagdn_add_norm_backward(const void *dy, int64_t dy_stride, const void *dres,
+                            int64_t dres_stride, const void *res, int64_t res_stride,
+                            const void *x, int64_t x_stride, const float *weight,
+                            const float *post_weight, const float *scale_vec, float scale,
+                            float eps, int T, int D, int dtype, int res_dtype, void *dx,
+                            void *dres_out, float *dweight, float *dscale, float *dpost,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/* gate_norm: the norm and gate between a mixer and its output projection, per token
+ * and head, y = norm(o) weight act(z): o, z, y [T, H, d] dtype, weight [d].  o and z
+ * (and dy) have a token stride in elements, a token's H x d elements being
+ * contiguous.  activation: */
+typedef enum { HAGDN_ACT_SILU = 0, HAGDN_ACT_SIGMOID = 1 } hagdn_activation;
+int hagdn_gate_norm(const void *o, int64_t o_stride, const void *z, int64_t z_stride,
+                    const float *weight, float eps, int T, int H, int d, int dtype,
+                    int activation, void *y, void *stream);
+
+/* Backward: the gradients do, dz [T, H, d] (contiguous) and dweight [d], which sums
+ * over tokens and heads. */
+size_t hagdn_gate_norm_workspace_size(int T, int H, int d);
+int hagdn_gate_norm_backward(const void *dy, int64_t dy_stride, const void *o,
+                             int64_t o_stride, const void *z, int64_t z_stride,
+                             const float *weight, float eps, int T, int H, int d, int dtype,
+                             int activation, void *d_o, void *d_z, float *dweight,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
 /* Message for the last non-OK return on this host thread ("" if none). */
 const char *hagdn_last_error(void);
 

@@ -19,6 +19,11 @@ state [N, Hv, Dk, Dv] fp32.  ``preprocess`` (PRE_* flags) makes the kernels
 normalise raw q/k and map raw gate / beta projections as they load them.
 The decode entry points advance one token per sequence and update a state
 pool in place.
+
+The operators around these layers are bound in ``layer.py``: a channelwise gated
+linear recurrence (``glr_prefill``, ``glr_backward``, ``glr_decode``) and the norms
+before and after a block (``add_norm``, ``gate_norm`` and their backward
+passes); ``autograd.py`` has differentiable forms of them.
 """
 
 from __future__ import annotations
@@ -30,7 +35,9 @@ __all__ = ["gdn_prefill", "kda_prefill", "gdn_decode", "kda_decode", "workspace_
            "device_status", "library_path", "load_library", "profile_begin", "profile_end", "kernel_names", "set_segment_chunks",
            "set_overlap", "overlap_for",
            "segment_chunks", "segment_chunks_for", "workspace_region", "measure_copy", "measure_mfma",
-           "HagdnError"]
+           "HagdnError",
+           "glr_prefill", "glr_backward", "glr_decode", "glr_workspace_size", "add_norm", "add_norm_backward",
+           "gate_norm", "gate_norm_backward"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libhagdn.so")
@@ -46,6 +53,8 @@ _PREFILL_ARGS = ([ctypes.c_void_p] * 7 + [ctypes.c_int] * 6 + [ctypes.c_float, c
 _PREFILL_TAIL = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
 _DECODE_ARGS = ([ctypes.c_void_p] * 7 + [ctypes.c_int] * 6 +
                 [ctypes.c_float, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p])
+_P = [ctypes.c_void_p]
+_ROWS = [ctypes.c_void_p, ctypes.c_int64]  # a matrix of rows: its pointer and row stride
 
 _SYMBOLS = {
     # name: (restype, argtypes)
@@ -79,6 +88,18 @@ _SYMBOLS = {
     "hagdn_measure_copy": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "hagdn_measure_mfma": (ctypes.c_int, [ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t,
                                           ctypes.POINTER(ctypes.c_double), ctypes.c_void_p]),
+    "glr_workspace_size": (ctypes.c_size_t, [ctypes.c_int] * 2),
+    "glr_prefill": (ctypes.c_int, _ROWS * 2 + _P * 2 + [ctypes.c_int] * 7 + _P * 4 + [ctypes.c_size_t] + _P),
+    "glr_backward": (ctypes.c_int, _ROWS * 3 + _P * 4 + [ctypes.c_int] * 7 + _P * 4 + [ctypes.c_size_t] + _P),
+    "glr_decode": (ctypes.c_int, _ROWS * 2 + _P * 2 + [ctypes.c_int] * 7 + _P * 2),
+    "hagdn_add_norm": (ctypes.c_int, _ROWS * 2 + _P * 3 + [ctypes.c_float] * 2 + [ctypes.c_int] * 4 + _P * 3),
+    "hagdn_add_norm_workspace_size": (ctypes.c_size_t, [ctypes.c_int] * 4),
+    "hagdn_add_norm_backward": (ctypes.c_int, _ROWS * 4 + _P * 3 + [ctypes.c_float] * 2 + [ctypes.c_int] * 4 +
+                                _P * 6 + [ctypes.c_size_t] + _P),
+    "hagdn_gate_norm": (ctypes.c_int, _ROWS * 2 + _P + [ctypes.c_float] + [ctypes.c_int] * 5 + _P * 2),
+    "hagdn_gate_norm_workspace_size": (ctypes.c_size_t, [ctypes.c_int] * 3),
+    "hagdn_gate_norm_backward": (ctypes.c_int, _ROWS * 3 + _P + [ctypes.c_float] + [ctypes.c_int] * 5 + _P * 4 +
+                                 [ctypes.c_size_t] + _P),
 }
 
 # workspace regions (hagdn_ws_region)
@@ -466,3 +487,17 @@ def profile_end():
     if rc != 0:
         raise HagdnError(rc, _err(lib))
     return dict(zip(kernel_names(), list(arr))), calls.value
+
+
+_LAYER = {"glr_prefill", "glr_backward", "glr_decode", "glr_workspace_size", "add_norm", "add_norm_backward",
+          "gate_norm", "gate_norm_backward"}
+
+
+def __getattr__(name):
+    """The operators of layer.py, bound on first use (that module imports torch)."""
+    if name not in _LAYER:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import layer
+    for n in _LAYER:
+        globals()[n] = getattr(layer, n)
+    return globals()[name]

@@ -25,23 +25,21 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
-#include <string>
 #include <vector>
 
 #include "../../include/hagdn.h"
+#include "layer.h"
 #include "prefill.h"
 
 namespace {
 
-thread_local std::string g_err;
+thread_local char g_err[512];
 
 int fail(int code, const char *fmt, ...) {
-  char buf[512];
   va_list ap;
   va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
+  vsnprintf(g_err, sizeof g_err, fmt, ap);
   va_end(ap);
-  g_err = buf;
   return code;
 }
 
@@ -501,6 +499,12 @@ hipError_t scratch_address(void **out) {
 
 }  // namespace
 
+// For the entry points of api_layer.cpp.
+namespace hagdn {
+int set_error(int code, const char *msg) { return fail(code, "%s", msg); }
+int device_cus() { return current_device_cus(); }
+}  // namespace hagdn
+
 extern "C" {
 
 int hagdn_prefill_noalloc(int kda, const void *q, const void *k, const void *v, const float *g,
@@ -578,7 +582,7 @@ int kda_prefill(const void *q, const void *k, const void *v, const float *g, con
                  dtype, 0, o, s_final, workspace, workspace_bytes, stream);
 }
 
-const char *hagdn_last_error(void) { return g_err.c_str(); }
+const char *hagdn_last_error(void) { return g_err; }
 
 int hagdn_device_status(const void *workspace, size_t workspace_bytes, void *stream, int *code) {
   if (!workspace || !code) return fail(HAGDN_EINVAL, "NULL workspace or code");

@@ -1,0 +1,86 @@
+// layer.h -- arguments and launchers of the operators around the delta-rule
+// layers: the gated linear recurrence (k6_glr.hip, k7_glr_backward.hip) and the
+// norms before and after a block (k8_norms.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace hagdn {
+
+// Records the message of a failed call for hagdn_last_error; returns code (api.cpp).
+int set_error(int code, const char *msg);
+// Compute units of the current device (0 if it cannot be queried) (api.cpp).
+int device_cus();
+
+// Tokens between two saved states of the recurrence (hagdn.h, glr_prefill).
+constexpr int kGlrGroup = 64;
+
+// One sequence's token range is [cu[n], cu[n+1]); cu == nullptr: N = 1, [0, T).
+struct GlrArgs {
+  const void *x, *g, *dh;  // rows of D channels, strides below (in elements)
+  long xs, gs, dhs;
+  const float *s0, *dfinal;  // [N, D] or null
+  const int32_t *cu;
+  int N, T, D;
+  void *h, *dx, *dg;       // [T, D], contiguous
+  float *s_final, *ds0;    // [N, D] or null
+  float *ckpt;             // [ceil(T / kGlrGroup), D] states before each group's first token, or null
+  int *status;             // workspace: device status word
+};
+
+struct GlrStepArgs {
+  const void *x, *g;
+  long xs, gs;
+  float *state;
+  const int32_t *slots;
+  int num_slots, N, D;
+  void *h;
+};
+
+// How the gate and the input weight are formed (hagdn.h, glr_prefill).
+struct GlrForm {
+  bool bf16, gate_bf16, raw, convex;
+};
+
+hipError_t launch_glr_forward(const GlrArgs &, const GlrForm &, hipStream_t);
+hipError_t launch_glr_backward(const GlrArgs &, const GlrForm &, hipStream_t);
+hipError_t launch_glr_step(const GlrStepArgs &, const GlrForm &, hipStream_t);
+
+struct AddNormArgs {
+  const void *x, *res, *dy, *dres;  // rows of D, strides below (in elements); res, dres may be null
+  long xs, rs, dys, drs;
+  const float *w, *post, *scale_vec;
+  float scale, eps;
+  int T, D;
+  void *y, *res_out;         // forward, contiguous
+  void *dx, *dres_out;       // backward, contiguous
+  float *dw, *dscale, *dpost;  // [D]; the last two or null
+  float *partial;            // workspace: [parts][1 + vector + post][D]
+  int parts;
+};
+
+struct GateNormArgs {
+  const void *o, *z, *dy;  // [T, H, d], token strides below (in elements)
+  long os, zs, dys;
+  const float *w;
+  float eps;
+  int T, H, d;
+  bool silu;               // else sigmoid
+  void *y, *dout, *dz;     // contiguous
+  float *dw;
+  float *partial;          // workspace: [parts][d]
+  int parts;
+};
+
+hipError_t launch_add_norm(const AddNormArgs &, bool bf16, bool res_bf16, hipStream_t);
+hipError_t launch_add_norm_backward(const AddNormArgs &, bool bf16, bool res_bf16, hipStream_t);
+hipError_t launch_gate_norm(const GateNormArgs &, bool bf16, hipStream_t);
+hipError_t launch_gate_norm_backward(const GateNormArgs &, bool bf16, hipStream_t);
+
+// Workgroups that share the rows of a backward norm, each with its own partial
+// sums of the weights' gradients: one to four a CU, never more than rows.
+int norm_parts(long rows, int cus);
+
+}  // namespace hagdn
