@@ -80,9 +80,10 @@ int check_glr(int N, int T, int D, int dtype, int gate_dtype, int convex, int pr
   return check_dtypes(dtype, gate_dtype, "gate");
 }
 
+// Workspace of a call: the header, and the words of the smaller (backward) tiles.
 size_t glr_bytes(int T, int D) {
-  (void)T, (void)D;
-  return 256;
+  const size_t tiles = ((size_t)T + hagdn::kGlrBackTile - 1) / hagdn::kGlrBackTile;
+  return hagdn::kGlrHeader + (tiles > 1 ? tiles * (size_t)D * 16 : 0);  // below 2^60
 }
 
 // Sizes, the sequences and the workspace, shared by the forward and backward calls.
@@ -96,6 +97,13 @@ int check_glr_call(const int32_t *cu, int N, int T, int D, int dtype, int gate_d
   const size_t need = glr_bytes(T, D);
   if (ws_bytes < need) return fail(HAGDN_EWORKSPACE, "workspace too small: %zu bytes, need %zu", ws_bytes, need);
   return HAGDN_OK;
+}
+
+void set_workspace(hagdn::GlrArgs *a, void *ws) {
+  char *p = static_cast<char *>(ws);
+  a->status = reinterpret_cast<int *>(p);
+  a->counter = reinterpret_cast<uint32_t *>(p + hagdn::kGlrCounter);
+  a->words = reinterpret_cast<uint64_t *>(p + hagdn::kGlrHeader);
 }
 
 hagdn::GlrForm form(int dtype, int gate_dtype, int convex, int pre) {
@@ -148,7 +156,7 @@ int glr_prefill(const void *x, int64_t x_stride, const void *g, int64_t g_stride
   hagdn::GlrArgs a = {};
   a.x = x; a.g = g; a.xs = x_stride; a.gs = g_stride; a.s0 = s0; a.cu = cu_seqlens;
   a.N = N; a.T = T_total; a.D = D; a.h = h; a.s_final = s_final; a.ckpt = checkpoints;
-  a.status = static_cast<int *>(workspace);
+  set_workspace(&a, workspace);
   return done(hagdn::launch_glr_forward(a, form(dtype, gate_dtype, convex, pre), static_cast<hipStream_t>(stream)));
 }
 
@@ -170,7 +178,7 @@ int glr_backward(const void *dh, int64_t dh_stride, const void *x, int64_t x_str
   a.x = x; a.g = g; a.dh = dh; a.xs = x_stride; a.gs = g_stride; a.dhs = dh_stride; a.s0 = s0; a.dfinal = dfinal;
   a.cu = cu_seqlens; a.N = N; a.T = T_total; a.D = D; a.dx = dx; a.dg = dg; a.ds0 = ds0;
   a.ckpt = const_cast<float *>(checkpoints);
-  a.status = static_cast<int *>(workspace);
+  set_workspace(&a, workspace);
   return done(hagdn::launch_glr_backward(a, form(dtype, gate_dtype, convex, pre), static_cast<hipStream_t>(stream)));
 }
 

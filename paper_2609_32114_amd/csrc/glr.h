@@ -1,11 +1,32 @@
-// glr.h -- the gate of the recurrence: the decay a and its complement 1 - a from a
-// log-gate or a raw projection.
+// glr.h -- shared parts of the gated linear recurrence's kernels: the gate, vector
+// access to rows of any alignment, the sequences that meet a run of tokens, and the
+// scan over tiles.
+//
+// The scan.  Over any run of tokens the state goes through an affine map, h_out =
+// A h_in + B per channel, and maps compose; a run with a sequence's first token in it
+// gives h_out = B whatever comes in (a reset).  The packed tokens are cut into tiles
+// whose elements stay in the registers of one workgroup from their only load to the
+// result's store, so that every input is read once:
+//   1. each wave forms the map of its few tokens, and the waves' maps meet in LDS;
+//   2. wave 0 composes them, publishes the tile's map, and follows the maps of the
+//      tiles before it back to the nearest state that is known whole, folds forward
+//      from there, and publishes the state its own tile leaves;
+//   3. each wave folds the maps of the waves before it onto that state and goes over
+//      its tokens again, from registers.
+// Workgroups take their tiles in order from a counter, so a tile's predecessors have
+// all been taken by workgroups that run or have ended, and every wait ends.  The state
+// is always folded forward from a whole one through the same products, so that its
+// bits do not depend on how far back that one was: results repeat exactly.
+// The backward pass runs the same scan from the last tile to the first.
 #pragma once
 
 #include "device.h"
+#include "layer.h"
+#include "prefill.h"
 
 namespace hagdn {
 
+// ---------------------------------------------------------------------- the gate
 struct Gate {
   float a, forget;  // decay e^g, and 1 - a
 };
@@ -37,5 +58,165 @@ template <bool RAW> __device__ __forceinline__ Gate glr_gate(float g) {
   }
   return k;
 }
+
+// ------------------------------------------------------------------- row access
+// V neighbouring elements as they lie in memory, at their element's alignment (a
+// column slice may start anywhere; the hardware takes dwords at any address).
+template <typename T, int V> struct __attribute__((packed, aligned(sizeof(T)))) Elems {
+  T v[V];
+};
+template <typename T, int V> __device__ __forceinline__ Elems<T, V> load_elems(const T *p) {
+  return *reinterpret_cast<const Elems<T, V> *>(p);
+}
+template <typename T, int V> __device__ __forceinline__ void store_elems(T *p, const float (&x)[V]) {
+  Elems<T, V> e;
+#pragma unroll
+  for (int i = 0; i < V; ++i) e.v[i] = Elt<T>::from_f32(x[i]);
+  *reinterpret_cast<Elems<T, V> *>(p) = e;
+}
+
+// --------------------------------------------------------------- sequences' ends
+// Whether cu[0 .. N] are the offsets of N sequences over T tokens; every thread of
+// the workgroup takes part and gets the answer.
+__device__ __forceinline__ bool glr_seqlens_ok(const int32_t *cu, int N, int T) {
+  if (!cu) return true;
+  int bad = 0;
+  for (int i = threadIdx.x; i < N; i += blockDim.x) bad |= cu[i] > cu[i + 1];
+  if (threadIdx.x == 0) bad |= cu[0] != 0 || cu[N] != T;
+  return !__syncthreads_or(bad);
+}
+
+// The first and last tokens of sequences among a wave's tokens [t0, t0 + L), as bit
+// masks, and the sequences' numbers in LDS.
+template <int L> struct Marks {
+  uint32_t first, last;  // uniform over the wave
+  const int32_t *cu;
+  const int *ids;        // [2 L]: of the sequence that starts, ends at token t0 + i
+  __device__ int starts(int i) const { return cu ? __builtin_amdgcn_readfirstlane(ids[i]) : 0; }
+  __device__ int ends(int i) const { return cu ? __builtin_amdgcn_readfirstlane(ids[L + i]) : 0; }
+};
+
+// Finds them.  The 64 lanes probe cu together: each round of the search divides the
+// range by 64, then one look at the offsets from there on (more if tens of empty
+// sequences lie there) marks every boundary.  No index or mark leaves its range
+// whatever cu holds.
+template <int L> __device__ __forceinline__ Marks<L> find_marks(const int32_t *cu, int N, int T, long t0, int (&ids)[2 * L]) {
+  const int lane = lane_id();
+  Marks<L> m{0, 0, cu, ids};
+  if (t0 >= T) return m;
+  if (!cu) {
+    m.first = t0 == 0;
+    m.last = t0 + L >= T ? 1u << (int)(T - 1 - t0) : 0;
+    return m;
+  }
+  int lo = 0, len = N;  // the last sequence that starts at or before t0 is in [lo, lo + len)
+  while (len > 1) {
+    const int step = (len + 63) / 64, at = lane * step;
+    const bool below = at < len && cu[lo + at] <= t0;
+    const int count = __popcll(__ballot(below));
+    const int skip = count > 1 ? (count - 1) * step : 0;
+    lo += skip;
+    len = min(step, len - skip);
+  }
+  if (lane < 2 * L) ids[lane] = -1;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  for (long base = lo; base <= N; base += 64) {
+    const long s = base + lane;
+    bool past = true;
+    if (s <= N) {
+      const long v = cu[s], i = v - t0;
+      if (s < N && cu[s + 1] > v && i >= 0 && i < L) ids[i] = (int)s;
+      if (s > 0 && cu[s - 1] < v && i >= 1 && i <= L) ids[L + i - 1] = (int)s - 1;
+      past = i > L;
+    }
+    if (__any(past)) break;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  const bool set = lane < 2 * L && ids[lane] >= 0;
+  const uint64_t bits = __ballot(set);
+  m.first = (uint32_t)(bits & ((1ull << L) - 1));
+  m.last = (uint32_t)(bits >> L) & (uint32_t)((1ull << L) - 1);
+  return m;
+}
+
+// ------------------------------------------------------------ states between tiles
+// Per tile and channel two 64-bit words, written and read whole (their halves cannot
+// part, so no fence orders them): a value and its tag.
+//   word 0: {A, kMap}
+//   word 1: {B, kMap}, then {the state the tile leaves, kState}
+// Untagged until then; glr_setup_kernel clears them.
+constexpr uint32_t kMap = 1, kState = 2;
+constexpr int kLookBack = 4;           // tiles seen in one look
+constexpr int kLookLimit = 1 << 20;    // looks before a wait is given up, about a second
+
+__device__ __forceinline__ void publish(uint64_t *w, float v, uint32_t tag) {
+  __hip_atomic_store(w, (uint64_t)tag << 32 | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t observe(const uint64_t *w) {
+  return __hip_atomic_load(const_cast<uint64_t *>(w), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint32_t tag_of(uint64_t w) { return (uint32_t)(w >> 32); }
+__device__ __forceinline__ float value_of(uint64_t w) { return __uint_as_float((uint32_t)w); }
+
+// The state that enters a tile, channels c .. c + V - 1 of one lane: near is the tile
+// beside it, dir the way to tiles further off, which there are `left` of, near
+// included.  The whole wave calls.
+template <int V>
+__device__ __forceinline__ void look_back(const uint64_t *words, int D, int c, long near, int dir, long left, int *status,
+                                          float (&s)[V]) {
+  for (int looks = 0; looks < kLookLimit; ++looks) {
+    uint64_t wa[kLookBack][V], wb[kLookBack][V];
+#pragma unroll
+    for (int k = 0; k < kLookBack; ++k) {
+      const long tile = near + dir * (k < left ? k : left - 1);
+      const uint64_t *w = words + (size_t)tile * 2 * D + c;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        wa[k][e] = observe(w + e);
+        wb[k][e] = observe(w + D + e);
+      }
+    }
+    int found = -1;
+    bool open = true;  // every tile so far has its map
+#pragma unroll
+    for (int k = 0; k < kLookBack; ++k) {
+      bool state = true, map = true;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const bool st = tag_of(wb[k][e]) == kState;
+        state &= st;
+        map &= st || (tag_of(wb[k][e]) == kMap && tag_of(wa[k][e]) == kMap);
+      }
+      if (open && found < 0 && __all(state)) found = k;
+      open &= (bool)__all(map);
+    }
+    if (found >= 0) {
+#pragma unroll
+      for (int k = kLookBack - 1; k >= 0; --k)
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (k <= found)
+            s[e] = tag_of(wb[k][e]) == kState ? value_of(wb[k][e]) : value_of(wa[k][e]) * s[e] + value_of(wb[k][e]);
+      return;
+    }
+    __builtin_amdgcn_s_sleep(1);
+  }
+  if (lane_id() == 0) atomicMax(status, kDevWaitTimeout);
+}
+
+// The instance of a launcher for a call's form: Launch<T, G>::go<RAW, CONVEX>(a, s).
+template <template <typename, typename> class Launch, typename A>
+hipError_t glr_dispatch(const A &a, const GlrForm &f, hipStream_t s) {
+  auto forms = [&](auto types) {
+    using K = decltype(types);
+    if (f.raw) return f.convex ? K::template go<true, true>(a, s) : K::template go<true, false>(a, s);
+    return f.convex ? K::template go<false, true>(a, s) : K::template go<false, false>(a, s);
+  };
+  if (!f.bf16) return forms(Launch<float, float>());
+  return f.gate_bf16 ? forms(Launch<bf16_t, bf16_t>()) : forms(Launch<bf16_t, float>());
+}
+
+// Clears the words and the counter, checks the offsets, writes the status.
+hipError_t launch_glr_setup(const GlrArgs &, size_t words, hipStream_t);
 
 }  // namespace hagdn

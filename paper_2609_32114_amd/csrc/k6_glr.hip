@@ -1,90 +1,203 @@
-// k6_glr.hip -- the gated linear recurrence: h_t = a_t h_{t-1} + w_t x_t per
-// channel, with a_t = e^g_t and w_t = 1 or 1 - a_t, over packed sequences; its
-// backward pass; and one step for single tokens.
+// k6_glr.hip -- the gated linear recurrence, forward: h_t = a_t h_{t-1} + w_t x_t per
+// channel over packed sequences (a_t = e^g_t, w_t = 1 or 1 - a_t), and its step for
+// single tokens.
 //
-// One thread walks one channel of one sequence.
-#include "device.h"
+// The forward pass is the scan of glr.h over tiles of 128 tokens x 64 V channels:
+// eight waves of 16 tokens, a lane holding V channels of each.  It is bound by HBM:
+// x and g are read once and h written once, for some 15 operations an element.
 #include "glr.h"
-#include "layer.h"
-#include "prefill.h"
 
 namespace hagdn {
 
-constexpr int kGlrThreads = 64;
+constexpr int kGlrWaves = 8;
+constexpr int kGlrRun = kGlrTile / kGlrWaves;  // tokens of a wave
+constexpr unsigned kGlrMaxGrid = 1 << 20;      // workgroups: a launch holds fewer than 2^32 threads
 
-// Whether cu[0 .. N] are the offsets of N sequences over T tokens; every thread of
-// the workgroup takes part and gets the answer.
-__device__ __forceinline__ bool glr_seqlens_ok(const int32_t *cu, int N, int T) {
-  if (!cu) return true;
-  int bad = 0;
-  for (int i = threadIdx.x; i < N; i += blockDim.x) bad |= cu[i] > cu[i + 1];
-  if (threadIdx.x == 0) bad |= cu[0] != 0 || cu[N] != T;
-  return !__syncthreads_or(bad);
-}
-
-template <typename T, typename G, bool RAW, bool CONVEX>
-__global__ __launch_bounds__(kGlrThreads) void glr_forward_kernel(GlrArgs a) {
-  const int cols = (a.D + kGlrThreads - 1) / kGlrThreads;
-  const int n = blockIdx.x / cols, c = blockIdx.x % cols * kGlrThreads + threadIdx.x;
+// Clears `words` words and the tile counter, checks the sequence offsets (workgroup 0)
+// and writes the status.
+__global__ __launch_bounds__(256) void glr_setup_kernel(GlrArgs a, size_t words) {
+  typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+  u64x2 *w = reinterpret_cast<u64x2 *>(a.words);
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words / 2; i += (size_t)gridDim.x * 256) w[i] = u64x2{0, 0};
+  if (blockIdx.x != 0) return;
   const bool ok = glr_seqlens_ok(a.cu, a.N, a.T);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
-  if (c >= a.D) return;
-  const int t0 = !ok ? 0 : a.cu ? a.cu[n] : 0, t1 = !ok ? 0 : a.cu ? a.cu[n + 1] : a.T;
-  const T *x = static_cast<const T *>(a.x) + c;
-  const G *g = static_cast<const G *>(a.g) + c;
-  T *h = static_cast<T *>(a.h) + c;
-  float s = a.s0 ? a.s0[(size_t)n * a.D + c] : 0.f;
-  for (int t = t0; t < t1; ++t) {
-    if (a.ckpt && t % kGlrGroup == 0) a.ckpt[(size_t)(t / kGlrGroup) * a.D + c] = s;
-    const Gate k = glr_gate<RAW>(Elt<G>::to_f32(g[(size_t)t * a.gs]));
-    const float u = Elt<T>::to_f32(x[(size_t)t * a.xs]);
-    s = k.a * s + (CONVEX ? k.forget * u : u);
-    h[(size_t)t * a.D] = Elt<T>::from_f32(s);
+  if (threadIdx.x == 0) {
+    *a.counter = 0;
+    *a.status = ok ? 0 : kDevBadSeqlens;
   }
-  if (a.s_final) a.s_final[(size_t)n * a.D + c] = s;
 }
 
-template <typename T, typename G, bool RAW, bool CONVEX>
-__global__ __launch_bounds__(kGlrThreads) void glr_backward_kernel(GlrArgs a) {
-  __shared__ float before[kGlrGroup][kGlrThreads];  // the states before a group's tokens
-  const int cols = (a.D + kGlrThreads - 1) / kGlrThreads;
-  const int n = blockIdx.x / cols, c = blockIdx.x % cols * kGlrThreads + threadIdx.x;
-  const bool ok = glr_seqlens_ok(a.cu, a.N, a.T);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
-  if (c >= a.D) return;
-  const int t0 = !ok ? 0 : a.cu ? a.cu[n] : 0, t1 = !ok ? 0 : a.cu ? a.cu[n + 1] : a.T;
-  const T *x = static_cast<const T *>(a.x) + c, *dh = static_cast<const T *>(a.dh) + c;
-  const G *g = static_cast<const G *>(a.g) + c;
-  T *dx = static_cast<T *>(a.dx) + c;
-  G *dg = static_cast<G *>(a.dg) + c;
-  float e = a.dfinal ? a.dfinal[(size_t)n * a.D + c] : 0.f;
-  for (int hi = t1; hi > t0;) {
-    const int grp = (hi - 1) / kGlrGroup, lo = max(t0, grp * kGlrGroup);
-    float s = lo > t0 ? a.ckpt[(size_t)grp * a.D + c] : a.s0 ? a.s0[(size_t)n * a.D + c] : 0.f;
-    for (int t = lo; t < hi; ++t) {
-      before[t - lo][threadIdx.x] = s;
-      const Gate k = glr_gate<RAW>(Elt<G>::to_f32(g[(size_t)t * a.gs]));
-      const float u = Elt<T>::to_f32(x[(size_t)t * a.xs]);
-      s = k.a * s + (CONVEX ? k.forget * u : u);
+// out[n] = in[n] (null: 0) for the sequences without tokens (all of them if !ok), for
+// one workgroup's channels.
+template <int V>
+__device__ __forceinline__ void pass_empty(const int32_t *cu, int N, int T, bool ok, const float *in, float *out, int D, int c) {
+  if (!out) return;
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = lane_id();
+  for (long base = (long)wave * 64; base < N; base += waves * 64) {
+    const long n = base + lane;
+    const bool empty = n < N && (!ok || (cu ? cu[n] == cu[n + 1] : T == 0));
+    for (uint64_t left = __ballot(empty); left; left &= left - 1) {
+      const size_t at = (size_t)(base + __builtin_ctzll(left)) * D + c;
+      if (c < D)
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[at + e] = in ? in[at + e] : 0.f;
     }
-    for (int t = hi - 1; t >= lo; --t) {
-      const Gate k = glr_gate<RAW>(Elt<G>::to_f32(g[(size_t)t * a.gs]));
-      const float d = Elt<T>::to_f32(dh[(size_t)t * a.dhs]) + e;
-      e = k.a * d;
-      float u = before[t - lo][threadIdx.x];
-      if (CONVEX) u -= Elt<T>::to_f32(x[(size_t)t * a.xs]);
-      dx[(size_t)t * a.D] = Elt<T>::from_f32(CONVEX ? k.forget * d : d);
-      dg[(size_t)t * a.D] = Elt<G>::from_f32(RAW ? -k.forget * (e * u) : e * u);
-    }
-    hi = lo;
   }
-  if (a.ds0) a.ds0[(size_t)n * a.D + c] = e;
 }
 
+template <typename T, typename G, int V, bool RAW, bool CONVEX>
+__global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs a, long tiles, long cols) {
+  constexpr int L = kGlrRun, W = kGlrWaves;
+  __shared__ float sA[W][V][64], sB[W][V][64], sIn[V][64];
+  __shared__ int sIds[W][2 * L], sReset[W];
+  __shared__ uint32_t sNext;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  bool ok = true;
+  if (tiles > 1) {
+    ok = *a.status == 0;
+  } else {  // no setup kernel ran
+    ok = glr_seqlens_ok(a.cu, a.N, a.T);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
+  }
+  for (long turn = blockIdx.x;; turn += gridDim.x) {
+    long item = turn;
+    if (tiles > 1) {
+      if (threadIdx.x == 0) sNext = atomicAdd(a.counter, 1u);
+      __syncthreads();
+      item = __builtin_amdgcn_readfirstlane(sNext);
+    }
+    if (item >= tiles * cols) return;
+    const long tile = item / cols;
+    const int c = (int)(item % cols) * 64 * V + lane * V, cl = c < a.D ? c : 0;
+    if (tile == 0) pass_empty<V>(a.cu, a.N, a.T, ok, a.s0, a.s_final, a.D, c);
+    if (!ok || a.T == 0) {
+      __syncthreads();  // sNext is written again in the next turn
+      continue;
+    }
+
+    // the wave's tokens; rows past the end are loaded from the last one
+    const long t0 = tile * kGlrTile + wave * L;
+    const int count = (int)min((long)L, max(0l, a.T - t0));
+    Elems<T, V> x[L];
+    Elems<G, V> g[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const long t = min(t0 + i, (long)a.T - 1);
+      x[i] = load_elems<T, V>(static_cast<const T *>(a.x) + t * a.xs + cl);
+      g[i] = load_elems<G, V>(static_cast<const G *>(a.g) + t * a.gs + cl);
+    }
+    const Marks<L> m = find_marks<L>(a.cu, a.N, a.T, t0, sIds[wave]);
+
+    float k[L][V], b[L][V];  // h_t = k h_{t-1} + b
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const Gate q = glr_gate<RAW>(Elt<G>::to_f32(g[i].v[e]));
+        const float u = Elt<T>::to_f32(x[i].v[e]);
+        k[i][e] = i < count ? q.a : 1.f;
+        b[i][e] = i < count ? CONVEX ? q.forget * u : u : 0.f;
+      }
+    float A[V], B[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) A[e] = 1.f, B[e] = 0.f;
+    if (m.first == 0) {
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          A[e] *= k[i][e];
+          B[e] = k[i][e] * B[e] + b[i][e];
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        const bool first = m.first >> i & 1;
+        if (first && a.s0) {
+          const float *s0 = a.s0 + (size_t)m.starts(i) * a.D + cl;
+#pragma unroll
+          for (int e = 0; e < V; ++e) b[i][e] = k[i][e] * s0[e] + b[i][e];
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) B[e] = first ? b[i][e] : k[i][e] * B[e] + b[i][e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) sA[wave][e][lane] = A[e], sB[wave][e][lane] = B[e];
+    if (lane == 0) sReset[wave] = m.first != 0;
+    __syncthreads();
+
+    if (wave == 0) {
+      bool reset = false;
+#pragma unroll
+      for (int e = 0; e < V; ++e) A[e] = 1.f, B[e] = 0.f;
+      for (int w = 0; w < W; ++w) {
+        const bool r = sReset[w];
+        reset |= r;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          B[e] = r ? sB[w][e][lane] : sA[w][e][lane] * B[e] + sB[w][e][lane];
+          A[e] *= sA[w][e][lane];
+        }
+      }
+      const bool pass_on = tile + 1 < tiles && c < a.D;
+      uint64_t *words = a.words + (size_t)tile * 2 * a.D + cl;
+      if (pass_on)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (!reset) publish(words + e, A[e], kMap);
+          publish(words + a.D + e, B[e], reset ? kState : kMap);
+        }
+      float s[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] = 0.f;
+      if (tile > 0 && !(m.first & 1)) look_back<V>(a.words, a.D, cl, tile - 1, -1, tile, a.status, s);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        if (pass_on && !reset) publish(words + a.D + e, A[e] * s[e] + B[e], kState);
+        sIn[e][lane] = s[e];
+      }
+    }
+    __syncthreads();
+
+    float s[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = sIn[e][lane];
+    for (int w = 0; w < wave; ++w) {
+      const bool r = sReset[w];
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] = r ? sB[w][e][lane] : sA[w][e][lane] * s[e] + sB[w][e][lane];
+    }
+    const bool mine = c < a.D;
+    if (a.ckpt && t0 % kGlrGroup == 0 && count > 0 && mine) store_elems<float, V>(a.ckpt + (size_t)(t0 / kGlrGroup) * a.D + c, s);
+    T *h = static_cast<T *>(a.h) + (size_t)t0 * a.D + cl;
+    if ((m.first | m.last) == 0 && count == L) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] = k[i][e] * s[e] + b[i][e];
+        if (mine) store_elems<T, V>(h + (size_t)i * a.D, s);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        const bool first = m.first >> i & 1;
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] = first ? b[i][e] : k[i][e] * s[e] + b[i][e];
+        if (mine && i < count) store_elems<T, V>(h + (size_t)i * a.D, s);
+        if ((m.last >> i & 1) && a.s_final && mine) store_elems<float, V>(a.s_final + (size_t)m.ends(i) * a.D + c, s);
+      }
+    }
+    __syncthreads();  // LDS is used again in the next turn
+  }
+}
+
+constexpr int kStepThreads = 64;
+
 template <typename T, typename G, bool RAW, bool CONVEX>
-__global__ __launch_bounds__(kGlrThreads) void glr_step_kernel(GlrStepArgs a) {
-  const int cols = (a.D + kGlrThreads - 1) / kGlrThreads;
-  const int n = blockIdx.x / cols, c = blockIdx.x % cols * kGlrThreads + threadIdx.x;
+__global__ __launch_bounds__(kStepThreads) void glr_step_kernel(GlrStepArgs a) {
+  const int cols = (a.D + kStepThreads - 1) / kStepThreads;
+  const int n = blockIdx.x / cols, c = blockIdx.x % cols * kStepThreads + threadIdx.x;
   if (c >= a.D) return;
   T *h = static_cast<T *>(a.h) + (size_t)n * a.D + c;
   const int slot = a.slots ? a.slots[n] : n;
@@ -100,37 +213,40 @@ __global__ __launch_bounds__(kGlrThreads) void glr_step_kernel(GlrStepArgs a) {
   *h = Elt<T>::from_f32(r);
 }
 
-// The kernel's instance for a form: K<T, G, RAW, CONVEX>.
-#define HAGDN_GLR_FORM(K, grid, block, stream, args)                                                            \
-  do {                                                                                                         \
-    if (!f.bf16) HAGDN_GLR_TYPES(K, float, float, grid, block, stream, args);                                   \
-    else if (f.gate_bf16) HAGDN_GLR_TYPES(K, bf16_t, bf16_t, grid, block, stream, args);                        \
-    else HAGDN_GLR_TYPES(K, bf16_t, float, grid, block, stream, args);                                          \
-  } while (0)
-#define HAGDN_GLR_TYPES(K, T, G, grid, block, stream, args)                                                     \
-  do {                                                                                                         \
-    if (f.raw && f.convex) hipLaunchKernelGGL((K<T, G, true, true>), grid, block, 0, stream, args);             \
-    else if (f.raw) hipLaunchKernelGGL((K<T, G, true, false>), grid, block, 0, stream, args);                   \
-    else if (f.convex) hipLaunchKernelGGL((K<T, G, false, true>), grid, block, 0, stream, args);                \
-    else hipLaunchKernelGGL((K<T, G, false, false>), grid, block, 0, stream, args);                             \
-  } while (0)
-
-hipError_t launch_glr_forward(const GlrArgs &a, const GlrForm &f, hipStream_t s) {
-  const dim3 grid((unsigned)((size_t)a.N * ((a.D + kGlrThreads - 1) / kGlrThreads)));
-  HAGDN_GLR_FORM(glr_forward_kernel, grid, dim3(kGlrThreads), s, a);
+hipError_t launch_glr_setup(const GlrArgs &a, size_t words, hipStream_t s) {
+  const size_t blocks = (words / 2 + 256 * 4 - 1) / (256 * 4);
+  hipLaunchKernelGGL(glr_setup_kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, a,
+                     words);
   return hipGetLastError();
 }
 
-hipError_t launch_glr_backward(const GlrArgs &a, const GlrForm &f, hipStream_t s) {
-  const dim3 grid((unsigned)((size_t)a.N * ((a.D + kGlrThreads - 1) / kGlrThreads)));
-  HAGDN_GLR_FORM(glr_backward_kernel, grid, dim3(kGlrThreads), s, a);
+template <typename T, typename G, int V, bool RAW, bool CONVEX>
+static hipError_t launch_forward(const GlrArgs &a, hipStream_t s) {
+  const long tiles = a.T > 0 ? ((long)a.T + kGlrTile - 1) / kGlrTile : 1, cols = ((long)a.D + 64 * V - 1) / (64 * V);
+  if (tiles * cols > 0xffff0000l) return hipErrorInvalidValue;  // the counter's range
+  if (tiles > 1) {
+    const hipError_t e = launch_glr_setup(a, (size_t)tiles * 2 * a.D, s);
+    if (e != hipSuccess) return e;
+  }
+  const unsigned grid = (unsigned)(tiles * cols < kGlrMaxGrid ? tiles * cols : kGlrMaxGrid);
+  hipLaunchKernelGGL((glr_forward_kernel<T, G, V, RAW, CONVEX>), dim3(grid), dim3(kGlrWaves * 64), 0, s, a, tiles, cols);
   return hipGetLastError();
 }
 
-hipError_t launch_glr_step(const GlrStepArgs &a, const GlrForm &f, hipStream_t s) {
-  const dim3 grid((unsigned)((size_t)a.N * ((a.D + kGlrThreads - 1) / kGlrThreads)));
-  HAGDN_GLR_FORM(glr_step_kernel, grid, dim3(kGlrThreads), s, a);
-  return hipGetLastError();
-}
+template <typename T, typename G> struct Forward {
+  template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
+    return a.D % 2 == 0 ? launch_forward<T, G, 2, RAW, CONVEX>(a, s) : launch_forward<T, G, 1, RAW, CONVEX>(a, s);
+  }
+};
+template <typename T, typename G> struct Step {
+  template <bool RAW, bool CONVEX> static hipError_t go(const GlrStepArgs &a, hipStream_t s) {
+    const dim3 grid((unsigned)((size_t)a.N * ((a.D + kStepThreads - 1) / kStepThreads)));
+    hipLaunchKernelGGL((glr_step_kernel<T, G, RAW, CONVEX>), grid, dim3(kStepThreads), 0, s, a);
+    return hipGetLastError();
+  }
+};
+
+hipError_t launch_glr_forward(const GlrArgs &a, const GlrForm &f, hipStream_t s) { return glr_dispatch<Forward>(a, f, s); }
+hipError_t launch_glr_step(const GlrStepArgs &a, const GlrForm &f, hipStream_t s) { return glr_dispatch<Step>(a, f, s); }
 
 }  // namespace hagdn

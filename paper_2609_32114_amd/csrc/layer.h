@@ -27,8 +27,16 @@ struct GlrArgs {
   void *h, *dx, *dg;       // [T, D], contiguous
   float *s_final, *ds0;    // [N, D] or null
   float *ckpt;             // [ceil(T / kGlrGroup), D] states before each group's first token, or null
-  int *status;             // workspace: device status word
+  // workspace (glr_workspace): the device status word, the tile counter, and two words
+  // per tile and channel (glr.h)
+  int *status;
+  uint32_t *counter;
+  uint64_t *words;
 };
+
+// Tokens of a forward and of a backward tile: a call of one tile needs no words.
+constexpr int kGlrTile = 128, kGlrBackTile = 64;
+constexpr size_t kGlrHeader = 256, kGlrCounter = 128;  // bytes before the words; where the counter is
 
 struct GlrStepArgs {
   const void *x, *g;
