@@ -65,14 +65,39 @@ template <bool RAW> __device__ __forceinline__ Gate glr_gate(float g) {
 template <typename T, int V> struct __attribute__((packed, aligned(sizeof(T)))) Elems {
   T v[V];
 };
-template <typename T, int V> __device__ __forceinline__ Elems<T, V> load_elems(const T *p) {
-  return *reinterpret_cast<const Elems<T, V> *>(p);
+// Where element c of a row lies, for accesses whose address is a uniform row (a pair of
+// scalar registers) plus a lane's 32-bit offset.  The empty statements keep the compiler
+// from adding the two first and holding every row's sum in a pair of vector registers.
+#ifdef __HIP_DEVICE_COMPILE__
+#define HAGDN_GLOBAL __attribute__((address_space(1)))
+#define HAGDN_SCALAR(p) asm("" : "+s"(p))
+#define HAGDN_VECTOR(v) asm("" : "+v"(v))
+#else  // the compiler's host pass only parses device code
+#define HAGDN_GLOBAL
+#define HAGDN_SCALAR(p)
+#define HAGDN_VECTOR(v)
+#endif
+template <typename T> __device__ __forceinline__ HAGDN_GLOBAL char *in_row(T *row, uint32_t c) {
+  HAGDN_GLOBAL char *p = (HAGDN_GLOBAL char *)row;
+  uint32_t offset = c * (uint32_t)sizeof(T);
+  HAGDN_SCALAR(p);
+  HAGDN_VECTOR(offset);
+  return p + offset;
 }
-template <typename T, int V> __device__ __forceinline__ void store_elems(T *p, const float (&x)[V]) {
+// Elements c .. c + V - 1 of a row.
+template <typename T, int V> __device__ __forceinline__ Elems<T, V> load_elems(const T *row, uint32_t c) {
+  return *(const HAGDN_GLOBAL Elems<T, V> *)in_row(row, c);
+}
+template <int V> __device__ __forceinline__ void load_state(const float *row, uint32_t c, float (&s)[V]) {
+  const Elems<float, V> e = load_elems<float, V>(row, c);
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[i] = e.v[i];
+}
+template <typename T, int V> __device__ __forceinline__ void store_elems(T *row, uint32_t c, const float (&x)[V]) {
   Elems<T, V> e;
 #pragma unroll
   for (int i = 0; i < V; ++i) e.v[i] = Elt<T>::from_f32(x[i]);
-  *reinterpret_cast<Elems<T, V> *>(p) = e;
+  *(HAGDN_GLOBAL Elems<T, V> *)in_row(row, c) = e;
 }
 
 // --------------------------------------------------------------- sequences' ends
@@ -149,11 +174,13 @@ constexpr uint32_t kMap = 1, kState = 2;
 constexpr int kLookBack = 4;           // tiles seen in one look
 constexpr int kLookLimit = 1 << 20;    // looks before a wait is given up, about a second
 
-__device__ __forceinline__ void publish(uint64_t *w, float v, uint32_t tag) {
+__device__ __forceinline__ void publish(uint64_t *row, uint32_t c, float v, uint32_t tag) {
+  HAGDN_GLOBAL uint64_t *w = (HAGDN_GLOBAL uint64_t *)in_row(row, c);
   __hip_atomic_store(w, (uint64_t)tag << 32 | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ uint64_t observe(const uint64_t *w) {
-  return __hip_atomic_load(const_cast<uint64_t *>(w), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ uint64_t observe(uint64_t *row, uint32_t c) {
+  HAGDN_GLOBAL uint64_t *w = (HAGDN_GLOBAL uint64_t *)in_row(row, c);
+  return __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ uint32_t tag_of(uint64_t w) { return (uint32_t)(w >> 32); }
 __device__ __forceinline__ float value_of(uint64_t w) { return __uint_as_float((uint32_t)w); }
@@ -162,18 +189,18 @@ __device__ __forceinline__ float value_of(uint64_t w) { return __uint_as_float((
 // beside it, dir the way to tiles further off, which there are `left` of, near
 // included.  The whole wave calls.
 template <int V>
-__device__ __forceinline__ void look_back(const uint64_t *words, int D, int c, long near, int dir, long left, int *status,
+__device__ __forceinline__ void look_back(uint64_t *words, int D, uint32_t c, long near, int dir, long left, int *status,
                                           float (&s)[V]) {
   for (int looks = 0; looks < kLookLimit; ++looks) {
     uint64_t wa[kLookBack][V], wb[kLookBack][V];
 #pragma unroll
     for (int k = 0; k < kLookBack; ++k) {
       const long tile = near + dir * (k < left ? k : left - 1);
-      const uint64_t *w = words + (size_t)tile * 2 * D + c;
+      uint64_t *w = words + (size_t)tile * 2 * D;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        wa[k][e] = observe(w + e);
-        wb[k][e] = observe(w + D + e);
+        wa[k][e] = observe(w, c + e);
+        wb[k][e] = observe(w + D, c + e);
       }
     }
     int found = -1;

@@ -46,7 +46,7 @@ __device__ __forceinline__ void pass_empty(const int32_t *cu, int N, int T, bool
 }
 
 template <typename T, typename G, int V, bool RAW, bool CONVEX>
-__global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs a, long tiles, long cols) {
+__global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs a, uint32_t tiles, uint32_t cols) {
   constexpr int L = kGlrRun, W = kGlrWaves;
   __shared__ float sA[W][V][64], sB[W][V][64], sIn[V][64];
   __shared__ int sIds[W][2 * L], sReset[W];
@@ -59,16 +59,17 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     ok = glr_seqlens_ok(a.cu, a.N, a.T);
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
   }
-  for (long turn = blockIdx.x;; turn += gridDim.x) {
-    long item = turn;
+  for (uint32_t turn = blockIdx.x;; turn += gridDim.x) {
+    uint32_t item = turn;
     if (tiles > 1) {
       if (threadIdx.x == 0) sNext = atomicAdd(a.counter, 1u);
       __syncthreads();
       item = __builtin_amdgcn_readfirstlane(sNext);
     }
     if (item >= tiles * cols) return;
-    const long tile = item / cols;
-    const int c = (int)(item % cols) * 64 * V + lane * V, cl = c < a.D ? c : 0;
+    const uint32_t tile = __builtin_amdgcn_readfirstlane(item / cols);
+    const int c = (int)(item - tile * cols) * 64 * V + lane * V;
+    const uint32_t cl = c < a.D ? c : 0;  // lanes past the last channel compute the first one's, and store nothing
     if (tile == 0) pass_empty<V>(a.cu, a.N, a.T, ok, a.s0, a.s_final, a.D, c);
     if (!ok || a.T == 0) {
       __syncthreads();  // sNext is written again in the next turn
@@ -76,17 +77,24 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     }
 
     // the wave's tokens; rows past the end are loaded from the last one
-    const long t0 = tile * kGlrTile + wave * L;
-    const int count = (int)min((long)L, max(0l, a.T - t0));
+    const long t0 = (long)tile * kGlrTile + wave * L;
+    const int count = (int)min((long)L, max(0l, (long)a.T - t0));
     Elems<T, V> x[L];
     Elems<G, V> g[L];
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const long t = min(t0 + i, (long)a.T - 1);
-      x[i] = load_elems<T, V>(static_cast<const T *>(a.x) + t * a.xs + cl);
-      g[i] = load_elems<G, V>(static_cast<const G *>(a.g) + t * a.gs + cl);
+      x[i] = load_elems<T, V>(static_cast<const T *>(a.x) + t * a.xs, cl);
+      g[i] = load_elems<G, V>(static_cast<const G *>(a.g) + t * a.gs, cl);
     }
     const Marks<L> m = find_marks<L>(a.cu, a.N, a.T, t0, sIds[wave]);
+    // The initial state of the last sequence that starts here, the only one that can
+    // reach past the wave's tokens.  It is read before the tile's map is published, the
+    // others' when their tokens' turn comes: where s_final is s0, a state is written by
+    // this wave after that, or by one that waits for the map.
+    const int start = m.first ? 31 - __builtin_clz(m.first) : -1;
+    float s0[V] = {};
+    if (m.first && a.s0) load_state<V>(a.s0 + (size_t)m.starts(start) * a.D, cl, s0);
 
     float k[L][V], b[L][V];  // h_t = k h_{t-1} + b
 #pragma unroll
@@ -101,27 +109,13 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     float A[V], B[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) A[e] = 1.f, B[e] = 0.f;
-    if (m.first == 0) {
 #pragma unroll
-      for (int i = 0; i < L; ++i)
+    for (int i = 0; i < L; ++i)
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          A[e] *= k[i][e];
-          B[e] = k[i][e] * B[e] + b[i][e];
-        }
-    } else {
-#pragma unroll
-      for (int i = 0; i < L; ++i) {
-        const bool first = m.first >> i & 1;
-        if (first && a.s0) {
-          const float *s0 = a.s0 + (size_t)m.starts(i) * a.D + cl;
-#pragma unroll
-          for (int e = 0; e < V; ++e) b[i][e] = k[i][e] * s0[e] + b[i][e];
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e) B[e] = first ? b[i][e] : k[i][e] * B[e] + b[i][e];
+      for (int e = 0; e < V; ++e) {
+        A[e] *= k[i][e];
+        B[e] = k[i][e] * (i == start ? s0[e] : B[e]) + b[i][e];
       }
-    }
 #pragma unroll
     for (int e = 0; e < V; ++e) sA[wave][e][lane] = A[e], sB[wave][e][lane] = B[e];
     if (lane == 0) sReset[wave] = m.first != 0;
@@ -131,6 +125,7 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
       bool reset = false;
 #pragma unroll
       for (int e = 0; e < V; ++e) A[e] = 1.f, B[e] = 0.f;
+#pragma unroll 1
       for (int w = 0; w < W; ++w) {
         const bool r = sReset[w];
         reset |= r;
@@ -141,20 +136,20 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
         }
       }
       const bool pass_on = tile + 1 < tiles && c < a.D;
-      uint64_t *words = a.words + (size_t)tile * 2 * a.D + cl;
+      uint64_t *words = a.words + (size_t)tile * 2 * a.D;
       if (pass_on)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          if (!reset) publish(words + e, A[e], kMap);
-          publish(words + a.D + e, B[e], reset ? kState : kMap);
+          if (!reset) publish(words, cl + e, A[e], kMap);
+          publish(words + a.D, cl + e, B[e], reset ? kState : kMap);
         }
       float s[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) s[e] = 0.f;
-      if (tile > 0 && !(m.first & 1)) look_back<V>(a.words, a.D, cl, tile - 1, -1, tile, a.status, s);
+      if (tile > 0 && !(m.first & 1)) look_back<V>(a.words, a.D, cl, (long)tile - 1, -1, tile, a.status, s);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        if (pass_on && !reset) publish(words + a.D + e, A[e] * s[e] + B[e], kState);
+        if (pass_on && !reset) publish(words + a.D, cl + e, A[e] * s[e] + B[e], kState);
         sIn[e][lane] = s[e];
       }
     }
@@ -163,30 +158,34 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     float s[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) s[e] = sIn[e][lane];
+#pragma unroll 1
     for (int w = 0; w < wave; ++w) {
       const bool r = sReset[w];
 #pragma unroll
       for (int e = 0; e < V; ++e) s[e] = r ? sB[w][e][lane] : sA[w][e][lane] * s[e] + sB[w][e][lane];
     }
     const bool mine = c < a.D;
-    if (a.ckpt && t0 % kGlrGroup == 0 && count > 0 && mine) store_elems<float, V>(a.ckpt + (size_t)(t0 / kGlrGroup) * a.D + c, s);
-    T *h = static_cast<T *>(a.h) + (size_t)t0 * a.D + cl;
-    if ((m.first | m.last) == 0 && count == L) {
+    if (a.ckpt && t0 % kGlrGroup == 0 && count > 0 && mine) store_elems<float, V>(a.ckpt + (size_t)(t0 / kGlrGroup) * a.D, cl, s);
+    T *h = static_cast<T *>(a.h) + (size_t)t0 * a.D;
+    // from one sequence's first token to the next one's; mostly a single turn
+    for (int lo = 0; lo < count;) {
+      if (m.first >> lo & 1) {
 #pragma unroll
-      for (int i = 0; i < L; ++i) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) s[e] = k[i][e] * s[e] + b[i][e];
-        if (mine) store_elems<T, V>(h + (size_t)i * a.D, s);
+        for (int e = 0; e < V; ++e) s[e] = lo == start ? s0[e] : 0.f;
+        if (lo != start && a.s0) load_state<V>(a.s0 + (size_t)m.starts(lo) * a.D, cl, s);
       }
-    } else {
+      const uint32_t later = m.first & ~((2u << lo) - 1);
+      const int hi = later ? __builtin_ctz(later) : count;
 #pragma unroll
-      for (int i = 0; i < L; ++i) {
-        const bool first = m.first >> i & 1;
+      for (int i = 0; i < L; ++i)
+        if (i >= lo && i < hi) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) s[e] = first ? b[i][e] : k[i][e] * s[e] + b[i][e];
-        if (mine && i < count) store_elems<T, V>(h + (size_t)i * a.D, s);
-        if ((m.last >> i & 1) && a.s_final && mine) store_elems<float, V>(a.s_final + (size_t)m.ends(i) * a.D + c, s);
-      }
+          for (int e = 0; e < V; ++e) s[e] = k[i][e] * s[e] + b[i][e];
+          if (mine) store_elems<T, V>(h + (size_t)i * a.D, cl, s);
+        }
+      if ((m.last >> (hi - 1) & 1) && a.s_final && mine)
+        store_elems<float, V>(a.s_final + (size_t)m.ends(hi - 1) * a.D, cl, s);
+      lo = hi;
     }
     __syncthreads();  // LDS is used again in the next turn
   }
@@ -229,7 +228,8 @@ static hipError_t launch_forward(const GlrArgs &a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   const unsigned grid = (unsigned)(tiles * cols < kGlrMaxGrid ? tiles * cols : kGlrMaxGrid);
-  hipLaunchKernelGGL((glr_forward_kernel<T, G, V, RAW, CONVEX>), dim3(grid), dim3(kGlrWaves * 64), 0, s, a, tiles, cols);
+  hipLaunchKernelGGL((glr_forward_kernel<T, G, V, RAW, CONVEX>), dim3(grid), dim3(kGlrWaves * 64), 0, s, a,
+                     (uint32_t)tiles, (uint32_t)cols);
   return hipGetLastError();
 }
 
