@@ -229,8 +229,8 @@ int kda_decode(const void *q, const void *k, const void *v, const float *g,
 size_t glr_workspace_size(int T_total, int D);
 
 /* Forward.  s0, s_final: [N, D] fp32 or NULL, s_final may be s0 itself (exactly).
- * checkpoints: NULL, or [ceil(T / 64), D] fp32, what glr_backward needs of the
- * forward pass: entry i receives the state before packed token 64 i (unspecified
+ * checkpoints: NULL, or [ceil(T / 128), D] fp32, what glr_backward needs of the
+ * forward pass: entry i receives the state before packed token 128 i (unspecified
  * where that token starts a sequence). */
 int glr_prefill(const void *x, int64_t x_stride, const void *g, int64_t g_stride,
                 const float *s0, const int32_t *cu_seqlens, int N, int T_total, int D,

@@ -7,7 +7,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 
-#include "../../include/hagdn.h"
+#include "hagdn.h"
 #include "layer.h"
 #include "prefill.h"
 
@@ -80,10 +80,10 @@ int check_glr(int N, int T, int D, int dtype, int gate_dtype, int convex, int pr
   return check_dtypes(dtype, gate_dtype, "gate");
 }
 
-// Workspace of a call: the header, and the words of the smaller (backward) tiles.
+// Workspace of a call: the header, the counters and the words of the smaller (backward) tiles.
 size_t glr_bytes(int T, int D) {
   const size_t tiles = ((size_t)T + hagdn::kGlrBackTile - 1) / hagdn::kGlrBackTile;
-  return hagdn::kGlrHeader + (tiles > 1 ? tiles * (size_t)D * 16 : 0);  // below 2^60
+  return hagdn::kGlrHeader + (tiles > 1 ? hagdn::glr_counter_bytes(D) + tiles * (size_t)D * 8 : 0);  // below 2^60
 }
 
 // Sizes, the sequences and the workspace, shared by the forward and backward calls.
@@ -102,8 +102,8 @@ int check_glr_call(const int32_t *cu, int N, int T, int D, int dtype, int gate_d
 void set_workspace(hagdn::GlrArgs *a, void *ws) {
   char *p = static_cast<char *>(ws);
   a->status = reinterpret_cast<int *>(p);
-  a->counter = reinterpret_cast<uint32_t *>(p + hagdn::kGlrCounter);
-  a->words = reinterpret_cast<uint64_t *>(p + hagdn::kGlrHeader);
+  a->counters = reinterpret_cast<uint32_t *>(p + hagdn::kGlrHeader);
+  a->words = reinterpret_cast<uint64_t *>(p + hagdn::kGlrHeader + hagdn::glr_counter_bytes(a->D));
 }
 
 hagdn::GlrForm form(int dtype, int gate_dtype, int convex, int pre) {

@@ -13,8 +13,9 @@
 //      from there, and publishes the state its own tile leaves;
 //   3. each wave folds the maps of the waves before it onto that state and goes over
 //      its tokens again, from registers.
-// Workgroups take their tiles in order from a counter, so a tile's predecessors have
-// all been taken by workgroups that run or have ended, and every wait ends.  The state
+// Workgroups take the tiles of their 64 channels in order from a counter, so a tile's
+// predecessors have all been taken by workgroups that run or have ended, and every wait
+// ends.  (One counter for the whole call costs some 33 ns a tile: 8192 tiles 272 us.)  The state
 // is always folded forward from a whole one through the same products, so that its
 // bits do not depend on how far back that one was: results repeat exactly.
 // The backward pass runs the same scan from the last tile to the first.
@@ -60,11 +61,6 @@ template <bool RAW> __device__ __forceinline__ Gate glr_gate(float g) {
 }
 
 // ------------------------------------------------------------------- row access
-// V neighbouring elements as they lie in memory, at their element's alignment (a
-// column slice may start anywhere; the hardware takes dwords at any address).
-template <typename T, int V> struct __attribute__((packed, aligned(sizeof(T)))) Elems {
-  T v[V];
-};
 // Where element c of a row lies, for accesses whose address is a uniform row (a pair of
 // scalar registers) plus a lane's 32-bit offset.  The empty statements keep the compiler
 // from adding the two first and holding every row's sum in a pair of vector registers.
@@ -77,27 +73,12 @@ template <typename T, int V> struct __attribute__((packed, aligned(sizeof(T)))) 
 #define HAGDN_SCALAR(p)
 #define HAGDN_VECTOR(v)
 #endif
-template <typename T> __device__ __forceinline__ HAGDN_GLOBAL char *in_row(T *row, uint32_t c) {
+template <typename T> __device__ __forceinline__ HAGDN_GLOBAL T *in_row(T *row, uint32_t c) {
   HAGDN_GLOBAL char *p = (HAGDN_GLOBAL char *)row;
   uint32_t offset = c * (uint32_t)sizeof(T);
   HAGDN_SCALAR(p);
   HAGDN_VECTOR(offset);
-  return p + offset;
-}
-// Elements c .. c + V - 1 of a row.
-template <typename T, int V> __device__ __forceinline__ Elems<T, V> load_elems(const T *row, uint32_t c) {
-  return *(const HAGDN_GLOBAL Elems<T, V> *)in_row(row, c);
-}
-template <int V> __device__ __forceinline__ void load_state(const float *row, uint32_t c, float (&s)[V]) {
-  const Elems<float, V> e = load_elems<float, V>(row, c);
-#pragma unroll
-  for (int i = 0; i < V; ++i) s[i] = e.v[i];
-}
-template <typename T, int V> __device__ __forceinline__ void store_elems(T *row, uint32_t c, const float (&x)[V]) {
-  Elems<T, V> e;
-#pragma unroll
-  for (int i = 0; i < V; ++i) e.v[i] = Elt<T>::from_f32(x[i]);
-  *(HAGDN_GLOBAL Elems<T, V> *)in_row(row, c) = e;
+  return (HAGDN_GLOBAL T *)(p + offset);
 }
 
 // --------------------------------------------------------------- sequences' ends
@@ -164,71 +145,75 @@ template <int L> __device__ __forceinline__ Marks<L> find_marks(const int32_t *c
   return m;
 }
 
+// out[n] = in[n] (null: 0) for the sequences without tokens (all of them if !ok), in
+// channel c.
+__device__ __forceinline__ void pass_empty(const int32_t *cu, int N, int T, bool ok, const float *in, float *out, int D,
+                                           uint32_t c, bool mine) {
+  if (!out) return;
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = lane_id();
+  for (long base = (long)wave * 64; base < N; base += waves * 64) {
+    const long n = base + lane;
+    const bool empty = n < N && (!ok || (cu ? cu[n] == cu[n + 1] : T == 0));
+    for (uint64_t left = __ballot(empty); left; left &= left - 1) {
+      const size_t at = (size_t)(base + __builtin_ctzll(left)) * D + c;
+      if (mine) out[at] = in ? in[at] : 0.f;
+    }
+  }
+}
+
 // ------------------------------------------------------------ states between tiles
-// Per tile and channel two 64-bit words, written and read whole (their halves cannot
-// part, so no fence orders them): a value and its tag.
-//   word 0: {A, kMap}
-//   word 1: {B, kMap}, then {the state the tile leaves, kState}
-// Untagged until then; glr_setup_kernel clears them.
-constexpr uint32_t kMap = 1, kState = 2;
-constexpr int kLookBack = 4;           // tiles seen in one look
+// One 64-bit word per tile and channel, written and read whole (its halves cannot
+// part, so no fence orders them).  Low half: B, or the state that the tile leaves.  High
+// half, A being a product of e^g and so never negative:
+//   kNoWord   nothing yet (the whole word has all bits set; glr_setup_kernel)
+//   kState    the low half is the state
+//   else      A, the tile's map
+constexpr uint32_t kNoWord = 0xffffffffu, kState = 0x80000000u;
+constexpr int kLookBack = 16;          // tiles seen in one look
 constexpr int kLookLimit = 1 << 20;    // looks before a wait is given up, about a second
 
-__device__ __forceinline__ void publish(uint64_t *row, uint32_t c, float v, uint32_t tag) {
-  HAGDN_GLOBAL uint64_t *w = (HAGDN_GLOBAL uint64_t *)in_row(row, c);
-  __hip_atomic_store(w, (uint64_t)tag << 32 | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ void publish(uint64_t *row, uint32_t c, uint32_t high, float low) {
+  __hip_atomic_store(in_row(row, c), (uint64_t)high << 32 | __float_as_uint(low), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ uint64_t observe(uint64_t *row, uint32_t c) {
-  HAGDN_GLOBAL uint64_t *w = (HAGDN_GLOBAL uint64_t *)in_row(row, c);
-  return __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__device__ __forceinline__ void publish_map(uint64_t *row, uint32_t c, float A, float B) {
+  publish(row, c, __float_as_uint(A) & 0x7fffffffu, B);  // a NaN keeps no sign
 }
-__device__ __forceinline__ uint32_t tag_of(uint64_t w) { return (uint32_t)(w >> 32); }
-__device__ __forceinline__ float value_of(uint64_t w) { return __uint_as_float((uint32_t)w); }
 
-// The state that enters a tile, channels c .. c + V - 1 of one lane: near is the tile
-// beside it, dir the way to tiles further off, which there are `left` of, near
-// included.  The whole wave calls.
-template <int V>
-__device__ __forceinline__ void look_back(uint64_t *words, int D, uint32_t c, long near, int dir, long left, int *status,
-                                          float (&s)[V]) {
+// The state that enters a tile, for one channel a lane: near is the tile beside it, dir
+// the way to tiles further off, which there are `left` of, near included.  The whole wave
+// calls.  One look loads the words of 16 tiles together, so that a state known whole 16
+// tiles off costs one latency.
+__device__ __forceinline__ float look_back(uint64_t *words, int D, uint32_t c, long near, int dir, long left, int *status) {
   for (int looks = 0; looks < kLookLimit; ++looks) {
-    uint64_t wa[kLookBack][V], wb[kLookBack][V];
+    uint64_t w[kLookBack];
 #pragma unroll
-    for (int k = 0; k < kLookBack; ++k) {
-      const long tile = near + dir * (k < left ? k : left - 1);
-      uint64_t *w = words + (size_t)tile * 2 * D;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        wa[k][e] = observe(w, c + e);
-        wb[k][e] = observe(w + D, c + e);
-      }
-    }
+    for (int k = 0; k < kLookBack; ++k)
+      w[k] = __hip_atomic_load(in_row(words + (size_t)(near + dir * (k < left ? k : left - 1)) * D, c), __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
     int found = -1;
-    bool open = true;  // every tile so far has its map
+    bool open = true;  // every tile so far has its word
 #pragma unroll
     for (int k = 0; k < kLookBack; ++k) {
-      bool state = true, map = true;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const bool st = tag_of(wb[k][e]) == kState;
-        state &= st;
-        map &= st || (tag_of(wb[k][e]) == kMap && tag_of(wa[k][e]) == kMap);
-      }
-      if (open && found < 0 && __all(state)) found = k;
-      open &= (bool)__all(map);
+      const uint32_t high = (uint32_t)(w[k] >> 32);
+      if (found < 0 && open && __all(high == kState)) found = k;
+      open &= (bool)__all(high != kNoWord);
     }
     if (found >= 0) {
+      float s = 0.f;
 #pragma unroll
       for (int k = kLookBack - 1; k >= 0; --k)
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-          if (k <= found)
-            s[e] = tag_of(wb[k][e]) == kState ? value_of(wb[k][e]) : value_of(wa[k][e]) * s[e] + value_of(wb[k][e]);
-      return;
+        if (k <= found) {
+          const uint32_t high = (uint32_t)(w[k] >> 32);
+          const float low = __uint_as_float((uint32_t)w[k]);
+          s = high == kState ? low : __uint_as_float(high) * s + low;
+        }
+      return s;
     }
     __builtin_amdgcn_s_sleep(1);
   }
   if (lane_id() == 0) atomicMax(status, kDevWaitTimeout);
+  return 0.f;
 }
 
 // The instance of a launcher for a call's form: Launch<T, G>::go<RAW, CONVEX>(a, s).
@@ -244,6 +229,6 @@ hipError_t glr_dispatch(const A &a, const GlrForm &f, hipStream_t s) {
 }
 
 // Clears the words and the counter, checks the offsets, writes the status.
-hipError_t launch_glr_setup(const GlrArgs &, size_t words, hipStream_t);
+hipError_t launch_glr_setup(const GlrArgs &, size_t words, uint32_t cols, hipStream_t);
 
 }  // namespace hagdn

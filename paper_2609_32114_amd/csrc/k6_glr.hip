@@ -2,8 +2,8 @@
 // channel over packed sequences (a_t = e^g_t, w_t = 1 or 1 - a_t), and its step for
 // single tokens.
 //
-// The forward pass is the scan of glr.h over tiles of 128 tokens x 64 V channels:
-// eight waves of 16 tokens, a lane holding V channels of each.  It is bound by HBM:
+// The forward pass is the scan of glr.h over tiles of 256 tokens x 64 channels:
+// eight waves of 32 tokens, a lane to a channel.  It is bound by HBM:
 // x and g are read once and h written once, for some 15 operations an element.
 #include "glr.h"
 
@@ -13,42 +13,22 @@ constexpr int kGlrWaves = 8;
 constexpr int kGlrRun = kGlrTile / kGlrWaves;  // tokens of a wave
 constexpr unsigned kGlrMaxGrid = 1 << 20;      // workgroups: a launch holds fewer than 2^32 threads
 
-// Clears `words` words and the tile counter, checks the sequence offsets (workgroup 0)
-// and writes the status.
-__global__ __launch_bounds__(256) void glr_setup_kernel(GlrArgs a, size_t words) {
-  typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
-  u64x2 *w = reinterpret_cast<u64x2 *>(a.words);
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words / 2; i += (size_t)gridDim.x * 256) w[i] = u64x2{0, 0};
+// Empties `words` words and clears the columns' counters, checks the sequence offsets
+// (workgroup 0) and writes the status.
+__global__ __launch_bounds__(256) void glr_setup_kernel(GlrArgs a, size_t words, uint32_t cols) {
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < cols; i += gridDim.x * 256) a.counters[(size_t)i * kGlrCounterStride] = 0;
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) a.words[i] = ~0ull;
   if (blockIdx.x != 0) return;
   const bool ok = glr_seqlens_ok(a.cu, a.N, a.T);
   if (threadIdx.x == 0) {
-    *a.counter = 0;
     *a.status = ok ? 0 : kDevBadSeqlens;
   }
 }
 
-// out[n] = in[n] (null: 0) for the sequences without tokens (all of them if !ok), for
-// one workgroup's channels.
-template <int V>
-__device__ __forceinline__ void pass_empty(const int32_t *cu, int N, int T, bool ok, const float *in, float *out, int D, int c) {
-  if (!out) return;
-  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = lane_id();
-  for (long base = (long)wave * 64; base < N; base += waves * 64) {
-    const long n = base + lane;
-    const bool empty = n < N && (!ok || (cu ? cu[n] == cu[n + 1] : T == 0));
-    for (uint64_t left = __ballot(empty); left; left &= left - 1) {
-      const size_t at = (size_t)(base + __builtin_ctzll(left)) * D + c;
-      if (c < D)
-#pragma unroll
-        for (int e = 0; e < V; ++e) out[at + e] = in ? in[at + e] : 0.f;
-    }
-  }
-}
-
-template <typename T, typename G, int V, bool RAW, bool CONVEX>
+template <typename T, typename G, bool RAW, bool CONVEX>
 __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs a, uint32_t tiles, uint32_t cols) {
   constexpr int L = kGlrRun, W = kGlrWaves;
-  __shared__ float sA[W][V][64], sB[W][V][64], sIn[V][64];
+  __shared__ float sA[W][64], sB[W][64], sIn[64];
   __shared__ int sIds[W][2 * L], sReset[W];
   __shared__ uint32_t sNext;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -60,17 +40,17 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
   }
   for (uint32_t turn = blockIdx.x;; turn += gridDim.x) {
-    uint32_t item = turn;
+    if (turn >= tiles * cols) return;
+    const uint32_t col = __builtin_amdgcn_readfirstlane(turn % cols), at = col * 64 + lane;
+    uint32_t tile = 0;
     if (tiles > 1) {
-      if (threadIdx.x == 0) sNext = atomicAdd(a.counter, 1u);
+      if (threadIdx.x == 0) sNext = atomicAdd(a.counters + (size_t)col * kGlrCounterStride, 1u);
       __syncthreads();
-      item = __builtin_amdgcn_readfirstlane(sNext);
+      tile = __builtin_amdgcn_readfirstlane(sNext);
     }
-    if (item >= tiles * cols) return;
-    const uint32_t tile = __builtin_amdgcn_readfirstlane(item / cols);
-    const int c = (int)(item - tile * cols) * 64 * V + lane * V;
-    const uint32_t cl = c < a.D ? c : 0;  // lanes past the last channel compute the first one's, and store nothing
-    if (tile == 0) pass_empty<V>(a.cu, a.N, a.T, ok, a.s0, a.s_final, a.D, c);
+    const bool mine = at < (uint32_t)a.D;
+    const uint32_t c = mine ? at : 0;  // lanes past the last channel compute the first one's, and store nothing
+    if (tile == 0) pass_empty(a.cu, a.N, a.T, ok, a.s0, a.s_final, a.D, c, mine);
     if (!ok || a.T == 0) {
       __syncthreads();  // sNext is written again in the next turn
       continue;
@@ -79,13 +59,13 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     // the wave's tokens; rows past the end are loaded from the last one
     const long t0 = (long)tile * kGlrTile + wave * L;
     const int count = (int)min((long)L, max(0l, (long)a.T - t0));
-    Elems<T, V> x[L];
-    Elems<G, V> g[L];
+    T x[L];
+    G g[L];
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const long t = min(t0 + i, (long)a.T - 1);
-      x[i] = load_elems<T, V>(static_cast<const T *>(a.x) + t * a.xs, cl);
-      g[i] = load_elems<G, V>(static_cast<const G *>(a.g) + t * a.gs, cl);
+      x[i] = *in_row(static_cast<const T *>(a.x) + t * a.xs, c);
+      g[i] = *in_row(static_cast<const G *>(a.g) + t * a.gs, c);
     }
     const Marks<L> m = find_marks<L>(a.cu, a.N, a.T, t0, sIds[wave]);
     // The initial state of the last sequence that starts here, the only one that can
@@ -93,98 +73,67 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     // others' when their tokens' turn comes: where s_final is s0, a state is written by
     // this wave after that, or by one that waits for the map.
     const int start = m.first ? 31 - __builtin_clz(m.first) : -1;
-    float s0[V] = {};
-    if (m.first && a.s0) load_state<V>(a.s0 + (size_t)m.starts(start) * a.D, cl, s0);
+    float s0 = 0.f;
+    if (m.first && a.s0) s0 = *in_row(a.s0 + (size_t)m.starts(start) * a.D, c);
 
-    float k[L][V], b[L][V];  // h_t = k h_{t-1} + b
+    float k[L], b[L], A = 1.f, B = 0.f;  // h_t = k h_{t-1} + b; over the wave's tokens A h + B
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const Gate q = glr_gate<RAW>(Elt<G>::to_f32(g[i].v[e]));
-        const float u = Elt<T>::to_f32(x[i].v[e]);
-        k[i][e] = i < count ? q.a : 1.f;
-        b[i][e] = i < count ? CONVEX ? q.forget * u : u : 0.f;
-      }
-    float A[V], B[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) A[e] = 1.f, B[e] = 0.f;
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        A[e] *= k[i][e];
-        B[e] = k[i][e] * (i == start ? s0[e] : B[e]) + b[i][e];
-      }
-#pragma unroll
-    for (int e = 0; e < V; ++e) sA[wave][e][lane] = A[e], sB[wave][e][lane] = B[e];
+    for (int i = 0; i < L; ++i) {
+      const Gate q = glr_gate<RAW>(Elt<G>::to_f32(g[i]));
+      const float u = Elt<T>::to_f32(x[i]);
+      k[i] = i < count ? q.a : 1.f;
+      b[i] = i < count ? CONVEX ? q.forget * u : u : 0.f;
+      A *= k[i];
+      B = k[i] * (i == start ? s0 : B) + b[i];
+    }
+    sA[wave][lane] = A;
+    sB[wave][lane] = B;
     if (lane == 0) sReset[wave] = m.first != 0;
     __syncthreads();
 
     if (wave == 0) {
       bool reset = false;
-#pragma unroll
-      for (int e = 0; e < V; ++e) A[e] = 1.f, B[e] = 0.f;
+      A = 1.f;
+      B = 0.f;
 #pragma unroll 1
       for (int w = 0; w < W; ++w) {
         const bool r = sReset[w];
         reset |= r;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          B[e] = r ? sB[w][e][lane] : sA[w][e][lane] * B[e] + sB[w][e][lane];
-          A[e] *= sA[w][e][lane];
-        }
+        B = r ? sB[w][lane] : sA[w][lane] * B + sB[w][lane];
+        A *= sA[w][lane];
       }
-      const bool pass_on = tile + 1 < tiles && c < a.D;
-      uint64_t *words = a.words + (size_t)tile * 2 * a.D;
-      if (pass_on)
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          if (!reset) publish(words, cl + e, A[e], kMap);
-          publish(words + a.D, cl + e, B[e], reset ? kState : kMap);
-        }
-      float s[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) s[e] = 0.f;
-      if (tile > 0 && !(m.first & 1)) look_back<V>(a.words, a.D, cl, (long)tile - 1, -1, tile, a.status, s);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        if (pass_on && !reset) publish(words + a.D, cl + e, A[e] * s[e] + B[e], kState);
-        sIn[e][lane] = s[e];
+      const bool pass_on = tile + 1 < tiles && mine;
+      uint64_t *row = a.words + (size_t)tile * a.D;
+      if (pass_on) {
+        if (reset) publish(row, c, kState, B);
+        else publish_map(row, c, A, B);
       }
+      float s = 0.f;
+      if (tile > 0 && !(m.first & 1)) s = look_back(a.words, a.D, c, (long)tile - 1, -1, tile, a.status);
+      if (pass_on && !reset) publish(row, c, kState, A * s + B);
+      sIn[lane] = s;
     }
     __syncthreads();
 
-    float s[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) s[e] = sIn[e][lane];
+    float s = sIn[lane];
 #pragma unroll 1
-    for (int w = 0; w < wave; ++w) {
-      const bool r = sReset[w];
-#pragma unroll
-      for (int e = 0; e < V; ++e) s[e] = r ? sB[w][e][lane] : sA[w][e][lane] * s[e] + sB[w][e][lane];
-    }
-    const bool mine = c < a.D;
-    if (a.ckpt && t0 % kGlrGroup == 0 && count > 0 && mine) store_elems<float, V>(a.ckpt + (size_t)(t0 / kGlrGroup) * a.D, cl, s);
-    T *h = static_cast<T *>(a.h) + (size_t)t0 * a.D;
+    for (int w = 0; w < wave; ++w) s = sReset[w] ? sB[w][lane] : sA[w][lane] * s + sB[w][lane];
+    if (a.ckpt && t0 % kGlrGroup == 0 && count > 0 && mine) *in_row(a.ckpt + (size_t)(t0 / kGlrGroup) * a.D, c) = s;
     // from one sequence's first token to the next one's; mostly a single turn
     for (int lo = 0; lo < count;) {
       if (m.first >> lo & 1) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) s[e] = lo == start ? s0[e] : 0.f;
-        if (lo != start && a.s0) load_state<V>(a.s0 + (size_t)m.starts(lo) * a.D, cl, s);
+        s = lo == start ? s0 : 0.f;
+        if (lo != start && a.s0) s = *in_row(a.s0 + (size_t)m.starts(lo) * a.D, c);
       }
       const uint32_t later = m.first & ~((2u << lo) - 1);
       const int hi = later ? __builtin_ctz(later) : count;
 #pragma unroll
       for (int i = 0; i < L; ++i)
         if (i >= lo && i < hi) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) s[e] = k[i][e] * s[e] + b[i][e];
-          if (mine) store_elems<T, V>(h + (size_t)i * a.D, cl, s);
+          s = k[i] * s + b[i];
+          if (mine) *in_row(static_cast<T *>(a.h) + (size_t)(t0 + i) * a.D, c) = Elt<T>::from_f32(s);
         }
-      if ((m.last >> (hi - 1) & 1) && a.s_final && mine)
-        store_elems<float, V>(a.s_final + (size_t)m.ends(hi - 1) * a.D, cl, s);
+      if ((m.last >> (hi - 1) & 1) && a.s_final && mine) *in_row(a.s_final + (size_t)m.ends(hi - 1) * a.D, c) = s;
       lo = hi;
     }
     __syncthreads();  // LDS is used again in the next turn
@@ -212,30 +161,25 @@ __global__ __launch_bounds__(kStepThreads) void glr_step_kernel(GlrStepArgs a) {
   *h = Elt<T>::from_f32(r);
 }
 
-hipError_t launch_glr_setup(const GlrArgs &a, size_t words, hipStream_t s) {
-  const size_t blocks = (words / 2 + 256 * 4 - 1) / (256 * 4);
+hipError_t launch_glr_setup(const GlrArgs &a, size_t words, uint32_t cols, hipStream_t s) {
+  const size_t blocks = (words + 256 * 8 - 1) / (256 * 8);
   hipLaunchKernelGGL(glr_setup_kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, a,
-                     words);
-  return hipGetLastError();
-}
-
-template <typename T, typename G, int V, bool RAW, bool CONVEX>
-static hipError_t launch_forward(const GlrArgs &a, hipStream_t s) {
-  const long tiles = a.T > 0 ? ((long)a.T + kGlrTile - 1) / kGlrTile : 1, cols = ((long)a.D + 64 * V - 1) / (64 * V);
-  if (tiles * cols > 0xffff0000l) return hipErrorInvalidValue;  // the counter's range
-  if (tiles > 1) {
-    const hipError_t e = launch_glr_setup(a, (size_t)tiles * 2 * a.D, s);
-    if (e != hipSuccess) return e;
-  }
-  const unsigned grid = (unsigned)(tiles * cols < kGlrMaxGrid ? tiles * cols : kGlrMaxGrid);
-  hipLaunchKernelGGL((glr_forward_kernel<T, G, V, RAW, CONVEX>), dim3(grid), dim3(kGlrWaves * 64), 0, s, a,
-                     (uint32_t)tiles, (uint32_t)cols);
+                     words, cols);
   return hipGetLastError();
 }
 
 template <typename T, typename G> struct Forward {
   template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
-    return a.D % 2 == 0 ? launch_forward<T, G, 2, RAW, CONVEX>(a, s) : launch_forward<T, G, 1, RAW, CONVEX>(a, s);
+    const long tiles = a.T > 0 ? ((long)a.T + kGlrTile - 1) / kGlrTile : 1, cols = ((long)a.D + 63) / 64;
+    if (tiles * cols > 0xffff0000l) return hipErrorInvalidValue;  // the counter's range
+    if (tiles > 1) {
+      const hipError_t e = launch_glr_setup(a, (size_t)tiles * a.D, (uint32_t)cols, s);
+      if (e != hipSuccess) return e;
+    }
+    const unsigned grid = (unsigned)(tiles * cols < kGlrMaxGrid ? tiles * cols : kGlrMaxGrid);
+    hipLaunchKernelGGL((glr_forward_kernel<T, G, RAW, CONVEX>), dim3(grid), dim3(kGlrWaves * 64), 0, s, a, (uint32_t)tiles,
+                       (uint32_t)cols);
+    return hipGetLastError();
   }
 };
 template <typename T, typename G> struct Step {

@@ -15,7 +15,7 @@ int set_error(int code, const char *msg);
 int device_cus();
 
 // Tokens between two saved states of the recurrence (hagdn.h, glr_prefill).
-constexpr int kGlrGroup = 64;
+constexpr int kGlrGroup = 128;
 
 // One sequence's token range is [cu[n], cu[n+1]); cu == nullptr: N = 1, [0, T).
 struct GlrArgs {
@@ -27,16 +27,18 @@ struct GlrArgs {
   void *h, *dx, *dg;       // [T, D], contiguous
   float *s_final, *ds0;    // [N, D] or null
   float *ckpt;             // [ceil(T / kGlrGroup), D] states before each group's first token, or null
-  // workspace (glr_workspace): the device status word, the tile counter, and two words
-  // per tile and channel (glr.h)
+  // workspace: the device status word, a tile counter per 64 channels, and a word per
+  // tile and channel (glr.h)
   int *status;
-  uint32_t *counter;
+  uint32_t *counters;
   uint64_t *words;
 };
 
 // Tokens of a forward and of a backward tile: a call of one tile needs no words.
-constexpr int kGlrTile = 128, kGlrBackTile = 64;
-constexpr size_t kGlrHeader = 256, kGlrCounter = 128;  // bytes before the words; where the counter is
+constexpr int kGlrTile = 256, kGlrBackTile = 128;
+constexpr size_t kGlrHeader = 256;          // bytes before the counters
+constexpr size_t kGlrCounterStride = 32;    // counters lie in memory lines of their own
+inline size_t glr_counter_bytes(int D) { return ((size_t)D + 63) / 64 * kGlrCounterStride * sizeof(uint32_t); }
 
 struct GlrStepArgs {
   const void *x, *g;

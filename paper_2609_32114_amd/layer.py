@@ -119,7 +119,7 @@ def glr_prefill(x, g, initial_state=None, cu_seqlens=None, convex=False, preproc
         _check_buffer("initial_state", initial_state, dev, torch.float32, (N, D))
     h = _output("out", out, shape, x.dtype, dev)
     final = _output("final_out", final_out, (N, D), torch.float32, dev) if output_final_state else None
-    saved = torch.empty(((T + 63) // 64, D), dtype=torch.float32, device=dev) if output_checkpoints else None
+    saved = torch.empty(((T + 127) // 128, D), dtype=torch.float32, device=dev) if output_checkpoints else None
     ws = _workspace(workspace, glr_workspace_size(T, D) if workspace is None else 0, dev)
     _call(lib.glr_prefill, x.data_ptr(), xs, g.data_ptr(), gs, _ptr(initial_state), cu, N, T, D, dt, gt, int(convex),
           int(preprocess), h.data_ptr(), _ptr(final), _ptr(saved), ws.data_ptr(), _bytes(ws), _raw_stream(di))
@@ -141,7 +141,7 @@ def glr_backward(dh, x, g, checkpoints, initial_state=None, dfinal=None, cu_seql
     if dh.dtype != x.dtype:
         raise TypeError(f"dh must be {x.dtype} (got {dh.dtype})")
     N, cu = _sequences(cu_seqlens, di)
-    _check_buffer("checkpoints", checkpoints, dev, torch.float32, ((T + 63) // 64, D))
+    _check_buffer("checkpoints", checkpoints, dev, torch.float32, ((T + 127) // 128, D))
     for name, t in (("initial_state", initial_state), ("dfinal", dfinal)):
         if t is not None:
             _check_buffer(name, t, dev, torch.float32, (N, D))

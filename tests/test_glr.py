@@ -280,7 +280,7 @@ def test_malformed_offsets(T):
         _, s = P.glr_prefill(x, g, initial_state=s0, cu_seqlens=cu, workspace=ws, out=h)
         assert P.device_status(ws) == P.DEV_BAD_SEQLENS
         assert torch.equal(s, s0) and bool((h == 7.0).all())
-        saved = torch.zeros((T + 63) // 64, D, device="cuda")
+        saved = torch.zeros((T + 127) // 128, D, device="cuda")
         _, _, ds0 = P.glr_backward(x, x, g, saved, initial_state=s0, dfinal=3 * s0, cu_seqlens=cu, workspace=ws)
         assert P.device_status(ws) == P.DEV_BAD_SEQLENS and torch.equal(ds0, 3 * s0)
     _, s = P.glr_prefill(x, g, initial_state=s0, cu_seqlens=torch.tensor([0, 10, 50, T], dtype=torch.int32, device="cuda"),
@@ -443,7 +443,7 @@ def test_writes_stay_inside():
 
         esz = {"bf16": 2, "f32": 4}
         h, s = guarded("h", T * D * esz[dtype]), guarded("s", N * D * 4)
-        ck = guarded("ck", (T + 63) // 64 * D * 4)
+        ck = guarded("ck", (T + 127) // 128 * D * 4)
         n = P.glr_workspace_size(T, D)
         ws = guarded("ws", n)
         dx, dg, ds0 = guarded("dx", T * D * esz[dtype]), guarded("dg", T * D * esz[gate]), guarded("ds0", N * D * 4)
