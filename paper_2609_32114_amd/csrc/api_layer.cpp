@@ -80,9 +80,9 @@ int check_glr(int N, int T, int D, int dtype, int gate_dtype, int convex, int pr
   return check_dtypes(dtype, gate_dtype, "gate");
 }
 
-// Workspace of a call: the header, the counters and the words of the smaller (backward) tiles.
+// Workspace of a call: the header, the counters and the words of the smallest tiles.
 size_t glr_bytes(int T, int D) {
-  const size_t tiles = ((size_t)T + hagdn::kGlrBackTile - 1) / hagdn::kGlrBackTile;
+  const size_t tiles = ((size_t)T + hagdn::kGlrLeastTile - 1) / hagdn::kGlrLeastTile;
   return hagdn::kGlrHeader + (tiles > 1 ? hagdn::glr_counter_bytes(D) + tiles * (size_t)D * 8 : 0);  // below 2^60
 }
 
@@ -101,6 +101,7 @@ int check_glr_call(const int32_t *cu, int N, int T, int D, int dtype, int gate_d
 
 void set_workspace(hagdn::GlrArgs *a, void *ws) {
   char *p = static_cast<char *>(ws);
+  a->cus = hagdn::device_cus();
   a->status = reinterpret_cast<int *>(p);
   a->counters = reinterpret_cast<uint32_t *>(p + hagdn::kGlrHeader);
   a->words = reinterpret_cast<uint64_t *>(p + hagdn::kGlrHeader + hagdn::glr_counter_bytes(a->D));

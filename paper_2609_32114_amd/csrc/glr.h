@@ -169,7 +169,6 @@ __device__ __forceinline__ void pass_empty(const int32_t *cu, int N, int T, bool
 //   kState    the low half is the state
 //   else      A, the tile's map
 constexpr uint32_t kNoWord = 0xffffffffu, kState = 0x80000000u;
-constexpr int kLookBack = 16;          // tiles seen in one look
 constexpr int kLookLimit = 1 << 20;    // looks before a wait is given up, about a second
 
 __device__ __forceinline__ void publish(uint64_t *row, uint32_t c, uint32_t high, float low) {
@@ -180,40 +179,53 @@ __device__ __forceinline__ void publish_map(uint64_t *row, uint32_t c, float A, 
   publish(row, c, __float_as_uint(A) & 0x7fffffffu, B);  // a NaN keeps no sign
 }
 
-// The state that enters a tile, for one channel a lane: near is the tile beside it, dir
-// the way to tiles further off, which there are `left` of, near included.  The whole wave
-// calls.  One look loads the words of 16 tiles together, so that a state known whole 16
-// tiles off costs one latency.
-__device__ __forceinline__ float look_back(uint64_t *words, int D, uint32_t c, long near, int dir, long left, int *status) {
-  for (int looks = 0; looks < kLookLimit; ++looks) {
-    uint64_t w[kLookBack];
+// One look at the K tiles nearest to one, for one channel a lane: near is the first, dir
+// the way to those further off, of which there are `left`, near included.  If some
+// tile's state is known whole and every map between is too, the state that enters.
+template <int K>
+__device__ __forceinline__ bool look(uint64_t *words, int D, uint32_t c, long near, int dir, long left, float &s) {
+  uint64_t w[K];
 #pragma unroll
-    for (int k = 0; k < kLookBack; ++k)
-      w[k] = __hip_atomic_load(in_row(words + (size_t)(near + dir * (k < left ? k : left - 1)) * D, c), __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_AGENT);
-    int found = -1;
-    bool open = true;  // every tile so far has its word
+  for (int k = 0; k < K; ++k)
+    w[k] = __hip_atomic_load(in_row(words + (size_t)(near + dir * (k < left ? k : left - 1)) * D, c), __ATOMIC_RELAXED,
+                             __HIP_MEMORY_SCOPE_AGENT);
+  int found = -1;
+  bool open = true;  // every tile so far has its word
 #pragma unroll
-    for (int k = 0; k < kLookBack; ++k) {
+  for (int k = 0; k < K; ++k) {
+    const uint32_t high = (uint32_t)(w[k] >> 32);
+    if (found < 0 && open && __all(high == kState)) found = k;
+    open &= (bool)__all(high != kNoWord);
+  }
+  if (found < 0) return false;
+#pragma unroll
+  for (int k = K - 1; k >= 0; --k)
+    if (k <= found) {
       const uint32_t high = (uint32_t)(w[k] >> 32);
-      if (found < 0 && open && __all(high == kState)) found = k;
-      open &= (bool)__all(high != kNoWord);
+      const float low = __uint_as_float((uint32_t)w[k]);
+      s = high == kState ? low : __uint_as_float(high) * s + low;
     }
-    if (found >= 0) {
-      float s = 0.f;
-#pragma unroll
-      for (int k = kLookBack - 1; k >= 0; --k)
-        if (k <= found) {
-          const uint32_t high = (uint32_t)(w[k] >> 32);
-          const float low = __uint_as_float((uint32_t)w[k]);
-          s = high == kState ? low : __uint_as_float(high) * s + low;
-        }
-      return s;
-    }
+  return true;
+}
+
+// The state that enters a tile.  The whole wave calls.  Mostly one of the nearest tiles'
+// states is there when its turn comes; where a call has few channels its tiles all wait
+// for each other, and a wider look, which costs no more time, moves the states on by
+// more tiles at once.
+__device__ __forceinline__ float look_back(uint64_t *words, int D, uint32_t c, long near, int dir, long left, int *status) {
+  float s = 0.f;
+  if (look<4>(words, D, c, near, dir, left, s)) return s;
+  for (int looks = 0; looks < kLookLimit; ++looks) {
+    if (look<8>(words, D, c, near, dir, left, s)) return s;
     __builtin_amdgcn_s_sleep(1);
   }
   if (lane_id() == 0) atomicMax(status, kDevWaitTimeout);
   return 0.f;
+}
+
+// The next tile of a column of 64 channels, in the order in which they are taken.
+__device__ __forceinline__ uint32_t take_tile(const GlrArgs &a, uint32_t col) {
+  return atomicAdd(a.counters + (size_t)col * kGlrCounterStride, 1u);
 }
 
 // The instance of a launcher for a call's form: Launch<T, G>::go<RAW, CONVEX>(a, s).

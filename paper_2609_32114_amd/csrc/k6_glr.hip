@@ -10,8 +10,6 @@
 namespace hagdn {
 
 constexpr int kGlrWaves = 8;
-constexpr int kGlrRun = kGlrTile / kGlrWaves;  // tokens of a wave
-constexpr unsigned kGlrMaxGrid = 1 << 20;      // workgroups: a launch holds fewer than 2^32 threads
 
 // Empties `words` words and clears the columns' counters, checks the sequence offsets
 // (workgroup 0) and writes the status.
@@ -25,9 +23,9 @@ __global__ __launch_bounds__(256) void glr_setup_kernel(GlrArgs a, size_t words,
   }
 }
 
-template <typename T, typename G, bool RAW, bool CONVEX>
+template <typename T, typename G, bool RAW, bool CONVEX, int L>
 __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs a, uint32_t tiles, uint32_t cols) {
-  constexpr int L = kGlrRun, W = kGlrWaves;
+  constexpr int W = kGlrWaves;
   __shared__ float sA[W][64], sB[W][64], sIn[64];
   __shared__ int sIds[W][2 * L], sReset[W];
   __shared__ uint32_t sNext;
@@ -39,33 +37,36 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     ok = glr_seqlens_ok(a.cu, a.N, a.T);
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
   }
-  for (uint32_t turn = blockIdx.x;; turn += gridDim.x) {
-    if (turn >= tiles * cols) return;
-    const uint32_t col = __builtin_amdgcn_readfirstlane(turn % cols), at = col * 64 + lane;
-    uint32_t tile = 0;
-    if (tiles > 1) {
-      if (threadIdx.x == 0) sNext = atomicAdd(a.counters + (size_t)col * kGlrCounterStride, 1u);
-      __syncthreads();
-      tile = __builtin_amdgcn_readfirstlane(sNext);
-    }
+  uint32_t next = 0;  // thread 0: the tile of the next turn
+  if (tiles > 1 && threadIdx.x == 0) next = take_tile(a, blockIdx.x % cols);
+  for (uint32_t turn = blockIdx.x; turn < tiles * cols; turn += gridDim.x) {
+    if (threadIdx.x == 0) sNext = next;
+    __syncthreads();
+    const uint32_t tile = __builtin_amdgcn_readfirstlane(sNext);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(turn % cols) * 64 + lane;
     const bool mine = at < (uint32_t)a.D;
     const uint32_t c = mine ? at : 0;  // lanes past the last channel compute the first one's, and store nothing
     if (tile == 0) pass_empty(a.cu, a.N, a.T, ok, a.s0, a.s_final, a.D, c, mine);
+    const uint32_t after = turn + gridDim.x;
+    if (tiles > 1 && threadIdx.x == 0 && after < tiles * cols) next = take_tile(a, after % cols);
     if (!ok || a.T == 0) {
       __syncthreads();  // sNext is written again in the next turn
       continue;
     }
 
     // the wave's tokens; rows past the end are loaded from the last one
-    const long t0 = (long)tile * kGlrTile + wave * L;
+    const long t0 = (long)tile * (W * L) + wave * L;
     const int count = (int)min((long)L, max(0l, (long)a.T - t0));
     T x[L];
     G g[L];
+    const T *px = static_cast<const T *>(a.x) + min(t0, (long)a.T - 1) * a.xs;
+    const G *pg = static_cast<const G *>(a.g) + min(t0, (long)a.T - 1) * a.gs;
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-      const long t = min(t0 + i, (long)a.T - 1);
-      x[i] = *in_row(static_cast<const T *>(a.x) + t * a.xs, c);
-      g[i] = *in_row(static_cast<const G *>(a.g) + t * a.gs, c);
+      x[i] = __builtin_nontemporal_load(in_row(px, c));
+      g[i] = __builtin_nontemporal_load(in_row(pg, c));
+      px += i + 1 < count ? a.xs : 0;
+      pg += i + 1 < count ? a.gs : 0;
     }
     const Marks<L> m = find_marks<L>(a.cu, a.N, a.T, t0, sIds[wave]);
     // The initial state of the last sequence that starts here, the only one that can
@@ -76,15 +77,31 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     float s0 = 0.f;
     if (m.first && a.s0) s0 = *in_row(a.s0 + (size_t)m.starts(start) * a.D, c);
 
+    if (count < L) {  // the last tile: tokens past the end pass the state on
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i >= count) {
+          x[i] = Elt<T>::from_f32(0.f);
+          g[i] = Elt<G>::from_f32(RAW ? -__builtin_inff() : 0.f);
+        }
+    }
     float k[L], b[L], A = 1.f, B = 0.f;  // h_t = k h_{t-1} + b; over the wave's tokens A h + B
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const Gate q = glr_gate<RAW>(Elt<G>::to_f32(g[i]));
       const float u = Elt<T>::to_f32(x[i]);
-      k[i] = i < count ? q.a : 1.f;
-      b[i] = i < count ? CONVEX ? q.forget * u : u : 0.f;
-      A *= k[i];
-      B = k[i] * (i == start ? s0 : B) + b[i];
+      k[i] = q.a;
+      b[i] = CONVEX ? q.forget * u : u;
+    }
+    if (m.first == 0) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        A *= k[i];
+        B = k[i] * B + b[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) B = k[i] * (i == start ? s0 : B) + b[i];
     }
     sA[wave][lane] = A;
     sB[wave][lane] = B;
@@ -119,7 +136,18 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
 #pragma unroll 1
     for (int w = 0; w < wave; ++w) s = sReset[w] ? sB[w][lane] : sA[w][lane] * s + sB[w][lane];
     if (a.ckpt && t0 % kGlrGroup == 0 && count > 0 && mine) *in_row(a.ckpt + (size_t)(t0 / kGlrGroup) * a.D, c) = s;
-    // from one sequence's first token to the next one's; mostly a single turn
+    if ((m.first | m.last) == 0 && count == L) {
+      T *ph = static_cast<T *>(a.h) + (size_t)t0 * a.D;
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        s = k[i] * s + b[i];
+        if (mine) __builtin_nontemporal_store(Elt<T>::from_f32(s), in_row(ph, c));
+        ph += a.D;
+      }
+      __syncthreads();  // LDS is used again in the next turn
+      continue;
+    }
+    // from one sequence's first token to the next one's
     for (int lo = 0; lo < count;) {
       if (m.first >> lo & 1) {
         s = lo == start ? s0 : 0.f;
@@ -169,17 +197,25 @@ hipError_t launch_glr_setup(const GlrArgs &a, size_t words, uint32_t cols, hipSt
 }
 
 template <typename T, typename G> struct Forward {
-  template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
-    const long tiles = a.T > 0 ? ((long)a.T + kGlrTile - 1) / kGlrTile : 1, cols = ((long)a.D + 63) / 64;
-    if (tiles * cols > 0xffff0000l) return hipErrorInvalidValue;  // the counter's range
+  template <bool RAW, bool CONVEX, int L> static hipError_t tiled(const GlrArgs &a, hipStream_t s) {
+    constexpr int kTile = kGlrWaves * L;
+    const long tiles = a.T > 0 ? ((long)a.T + kTile - 1) / kTile : 1, cols = ((long)a.D + 63) / 64;
+    if (tiles * cols > 0xffff0000l) return hipErrorInvalidValue;  // the turns' range
     if (tiles > 1) {
       const hipError_t e = launch_glr_setup(a, (size_t)tiles * a.D, (uint32_t)cols, s);
       if (e != hipSuccess) return e;
     }
-    const unsigned grid = (unsigned)(tiles * cols < kGlrMaxGrid ? tiles * cols : kGlrMaxGrid);
-    hipLaunchKernelGGL((glr_forward_kernel<T, G, RAW, CONVEX>), dim3(grid), dim3(kGlrWaves * 64), 0, s, a, (uint32_t)tiles,
-                       (uint32_t)cols);
+    const long resident = 2l * (a.cus > 0 ? a.cus : 256);
+    const unsigned grid = (unsigned)(tiles * cols < resident ? tiles * cols : resident);
+    hipLaunchKernelGGL((glr_forward_kernel<T, G, RAW, CONVEX, L>), dim3(grid), dim3(kGlrWaves * 64), 0, s, a,
+                       (uint32_t)tiles, (uint32_t)cols);
     return hipGetLastError();
+  }
+  template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
+    const long items = ((long)a.T + 255) / 256 * (((long)a.D + 63) / 64);
+    if (a.T <= 64) return tiled<RAW, CONVEX, 8>(a, s);
+    if (a.T <= 128 || (a.T > 256 && 2 * items <= a.cus)) return tiled<RAW, CONVEX, 16>(a, s);
+    return tiled<RAW, CONVEX, 32>(a, s);
   }
 };
 template <typename T, typename G> struct Step {

@@ -1,51 +1,214 @@
-// k7_glr_backward.hip -- the gated linear recurrence's backward pass.
+// k7_glr_backward.hip -- the gated linear recurrence's backward pass.  With d_t the
+// gradient of h_t and e_t = a_t d_t,
+//   d_t = dh_t + e_{t+1},  dx_t = w_t d_t,  d(log a_t) = e_t (h_{t-1} - [convex] x_t).
+//
+// The scan of glr.h runs over e from the last tile to the first, eight waves of 16
+// tokens to a tile.  The states h_{t-1} are not read: each tile forms them again in fp32
+// from the saved state before its first token, in the same registers and with one more
+// map a wave in LDS, which costs three operations an element and saves reading h (and
+// its rounding).  Bound by HBM: x, g and dh are read once, dx and dg written once.
 #include "glr.h"
 
 namespace hagdn {
 
-constexpr int kGlrThreads = 64;
+constexpr int kBackWaves = 8, kBackRun = 16;
+static_assert(kBackWaves * kBackRun == kGlrGroup, "a tile starts at a saved state");
 
 template <typename T, typename G, bool RAW, bool CONVEX>
-__global__ __launch_bounds__(kGlrThreads) void glr_backward_kernel(GlrArgs a) {
-  __shared__ float before[kGlrGroup][kGlrThreads];  // the states before a group's tokens
-  const int cols = (a.D + kGlrThreads - 1) / kGlrThreads;
-  const int n = blockIdx.x / cols, c = blockIdx.x % cols * kGlrThreads + threadIdx.x;
-  const bool ok = glr_seqlens_ok(a.cu, a.N, a.T);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
-  if (c >= a.D) return;
-  const int t0 = !ok ? 0 : a.cu ? a.cu[n] : 0, t1 = !ok ? 0 : a.cu ? a.cu[n + 1] : a.T;
-  const T *x = static_cast<const T *>(a.x) + c, *dh = static_cast<const T *>(a.dh) + c;
-  const G *g = static_cast<const G *>(a.g) + c;
-  T *dx = static_cast<T *>(a.dx) + c;
-  G *dg = static_cast<G *>(a.dg) + c;
-  float e = a.dfinal ? a.dfinal[(size_t)n * a.D + c] : 0.f;
-  for (int hi = t1; hi > t0;) {
-    const int grp = (hi - 1) / kGlrGroup, lo = max(t0, grp * kGlrGroup);
-    float s = lo > t0 ? a.ckpt[(size_t)grp * a.D + c] : a.s0 ? a.s0[(size_t)n * a.D + c] : 0.f;
-    for (int t = lo; t < hi; ++t) {
-      before[t - lo][threadIdx.x] = s;
-      const Gate k = glr_gate<RAW>(Elt<G>::to_f32(g[(size_t)t * a.gs]));
-      const float u = Elt<T>::to_f32(x[(size_t)t * a.xs]);
-      s = k.a * s + (CONVEX ? k.forget * u : u);
-    }
-    for (int t = hi - 1; t >= lo; --t) {
-      const Gate k = glr_gate<RAW>(Elt<G>::to_f32(g[(size_t)t * a.gs]));
-      const float d = Elt<T>::to_f32(dh[(size_t)t * a.dhs]) + e;
-      e = k.a * d;
-      float u = before[t - lo][threadIdx.x];
-      if (CONVEX) u -= Elt<T>::to_f32(x[(size_t)t * a.xs]);
-      dx[(size_t)t * a.D] = Elt<T>::from_f32(CONVEX ? k.forget * d : d);
-      dg[(size_t)t * a.D] = Elt<G>::from_f32(RAW ? -k.forget * (e * u) : e * u);
-    }
-    hi = lo;
+__global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArgs a, uint32_t tiles, uint32_t cols) {
+  constexpr int L = kBackRun, W = kBackWaves;
+  __shared__ float sA[W][64], sF[W][64], sR[W][64], sIn[64];
+  __shared__ int sIds[W][2 * L], sFirst[W], sLast[W], sEnded;
+  __shared__ uint32_t sNext;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  bool ok = true;
+  if (tiles > 1) {
+    ok = *a.status == 0;
+  } else {  // no setup kernel ran
+    ok = glr_seqlens_ok(a.cu, a.N, a.T);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
   }
-  if (a.ds0) a.ds0[(size_t)n * a.D + c] = e;
+  uint32_t next = 0;  // thread 0: the number of the next turn's tile, counted from the last
+  if (tiles > 1 && threadIdx.x == 0) next = take_tile(a, blockIdx.x % cols);
+  for (uint32_t turn = blockIdx.x; turn < tiles * cols; turn += gridDim.x) {
+    if (threadIdx.x == 0) sNext = next;
+    __syncthreads();
+    const uint32_t tile = tiles - 1 - __builtin_amdgcn_readfirstlane(sNext);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(turn % cols) * 64 + lane;
+    const bool mine = at < (uint32_t)a.D;
+    const uint32_t c = mine ? at : 0;  // lanes past the last channel compute the first one's, and store nothing
+    if (tile == 0) pass_empty(a.cu, a.N, a.T, ok, a.dfinal, a.ds0, a.D, c, mine);
+    const uint32_t after = turn + gridDim.x;
+    if (tiles > 1 && threadIdx.x == 0 && after < tiles * cols) next = take_tile(a, after % cols);
+    if (!ok || a.T == 0) {
+      __syncthreads();  // sNext is written again in the next turn
+      continue;
+    }
+
+    // the wave's tokens; rows past the end are loaded from the last one
+    const long t0 = (long)tile * kGlrGroup + wave * L;
+    const int count = (int)min((long)L, max(0l, (long)a.T - t0));
+    T x[L], y[L];  // y: dh
+    G g[L];
+    const long row = min(t0, (long)a.T - 1);
+    const T *px = static_cast<const T *>(a.x) + row * a.xs, *py = static_cast<const T *>(a.dh) + row * a.dhs;
+    const G *pg = static_cast<const G *>(a.g) + row * a.gs;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      x[i] = __builtin_nontemporal_load(in_row(px, c));
+      g[i] = __builtin_nontemporal_load(in_row(pg, c));
+      y[i] = __builtin_nontemporal_load(in_row(py, c));
+      px += i + 1 < count ? a.xs : 0;
+      pg += i + 1 < count ? a.gs : 0;
+      py += i + 1 < count ? a.dhs : 0;
+    }
+    float s = *in_row(a.ckpt + (size_t)tile * a.D, c);
+    const Marks<L> m = find_marks<L>(a.cu, a.N, a.T, t0, sIds[wave]);
+    // The last sequence that starts here is the only one to reach past the wave's tokens,
+    // the first that ends here the only one to come from before them; its dfinal is read
+    // before the tile's map is published, the others' when their tokens' turn comes:
+    // where ds0 is dfinal, a gradient is written by this wave after that, or by one that
+    // waits for the map.
+    const int start = m.first ? 31 - __builtin_clz(m.first) : -1, end = m.last ? __builtin_ctz(m.last) : -1;
+    float s0 = 0.f, df = 0.f;
+    if (m.first && a.s0) s0 = *in_row(a.s0 + (size_t)m.starts(start) * a.D, c);
+    if (m.last && a.dfinal) df = *in_row(a.dfinal + (size_t)m.ends(end) * a.D, c);
+
+    if (count < L) {  // the last tile: tokens past the end pass everything on
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (i >= count) {
+          x[i] = y[i] = Elt<T>::from_f32(0.f);
+          g[i] = Elt<G>::from_f32(RAW ? -__builtin_inff() : 0.f);
+        }
+    }
+    float k[L], f[L], u[L], d[L];  // decay, its complement, x, dh
+    float A = 1.f, F = 0.f, R = 0.f;  // the tokens' maps: of the state A h + F, of e going back A e + R
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const Gate q = glr_gate<RAW>(Elt<G>::to_f32(g[i]));
+      k[i] = q.a;
+      f[i] = q.forget;
+      u[i] = Elt<T>::to_f32(x[i]);
+      d[i] = Elt<T>::to_f32(y[i]);
+    }
+    auto step = [&](int i, float h) { return k[i] * h + (CONVEX ? f[i] * u[i] : u[i]); };
+    if (m.first == 0) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) A *= k[i], F = step(i, F);
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) A *= k[i], F = step(i, i == start ? s0 : F);
+    }
+    if (m.last == 0) {
+#pragma unroll
+      for (int i = L - 1; i >= 0; --i) R = k[i] * (d[i] + R);
+    } else {
+#pragma unroll
+      for (int i = L - 1; i >= 0; --i) R = k[i] * (d[i] + (i == end ? df : R));
+    }
+    sA[wave][lane] = A;
+    sF[wave][lane] = F;
+    sR[wave][lane] = R;
+    if (lane == 0) {
+      sFirst[wave] = m.first != 0;
+      sLast[wave] = m.last != 0;
+      if (wave == W - 1) sEnded = m.last >> (L - 1) & 1;
+    }
+    __syncthreads();
+
+    if (wave == 0) {
+      bool reset = false;
+      A = 1.f;
+      R = 0.f;
+#pragma unroll 1
+      for (int w = W - 1; w >= 0; --w) {
+        const bool r = sLast[w];
+        reset |= r;
+        R = r ? sR[w][lane] : sA[w][lane] * R + sR[w][lane];
+        A *= sA[w][lane];
+      }
+      const bool pass_on = tile > 0 && mine;
+      uint64_t *words = a.words + (size_t)tile * a.D;
+      if (pass_on) {
+        if (reset) publish(words, c, kState, R);
+        else publish_map(words, c, A, R);
+      }
+      float e = 0.f;
+      if (tile + 1 < tiles && !sEnded) e = look_back(a.words, a.D, c, (long)tile + 1, 1, (long)tiles - 1 - tile, a.status);
+      if (pass_on && !reset) publish(words, c, kState, A * e + R);
+      sIn[lane] = e;
+    }
+    __syncthreads();
+
+    float e = sIn[lane];
+#pragma unroll 1
+    for (int w = W - 1; w > wave; --w) e = sLast[w] ? sR[w][lane] : sA[w][lane] * e + sR[w][lane];
+#pragma unroll 1
+    for (int w = 0; w < wave; ++w) s = sFirst[w] ? sF[w][lane] : sA[w][lane] * s + sF[w][lane];
+
+    auto state = [&](int i) {  // u: the state before the token, less x where convex
+      const float h = step(i, s);
+      u[i] = CONVEX ? s - u[i] : s;
+      s = h;
+    };
+    auto grads = [&](int i) {
+      const float di = d[i] + e;
+      e = k[i] * di;
+      if (!mine) return;
+      T *dx = static_cast<T *>(a.dx) + (size_t)(t0 + i) * a.D;
+      G *dg = static_cast<G *>(a.dg) + (size_t)(t0 + i) * a.D;
+      __builtin_nontemporal_store(Elt<T>::from_f32(CONVEX ? f[i] * di : di), in_row(dx, c));
+      __builtin_nontemporal_store(Elt<G>::from_f32(RAW ? -f[i] * (e * u[i]) : e * u[i]), in_row(dg, c));
+    };
+    if ((m.first | m.last) == 0 && count == L) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) state(i);
+#pragma unroll
+      for (int i = L - 1; i >= 0; --i) grads(i);
+    } else {
+      for (int lo = 0; lo < count;) {  // from one sequence's first token to the next one's
+        if (m.first >> lo & 1) {
+          s = lo == start ? s0 : 0.f;
+          if (lo != start && a.s0) s = *in_row(a.s0 + (size_t)m.starts(lo) * a.D, c);
+        }
+        const uint32_t later = m.first & ~((2u << lo) - 1);
+        const int hi = later ? __builtin_ctz(later) : count;
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+          if (i >= lo && i < hi) state(i);
+        lo = hi;
+      }
+      for (int hi = count; hi > 0;) {  // from one sequence's last token back to the one before
+        if (m.last >> (hi - 1) & 1) {
+          e = hi - 1 == end ? df : 0.f;
+          if (hi - 1 != end && a.dfinal) e = *in_row(a.dfinal + (size_t)m.ends(hi - 1) * a.D, c);
+        }
+        const uint32_t sooner = m.last & ((1u << (hi - 1)) - 1);
+        const int lo = sooner ? 32 - __builtin_clz(sooner) : 0;
+#pragma unroll
+        for (int i = L - 1; i >= 0; --i)
+          if (i >= lo && i < hi) grads(i);
+        if ((m.first >> lo & 1) && a.ds0 && mine) *in_row(a.ds0 + (size_t)m.starts(lo) * a.D, c) = e;
+        hi = lo;
+      }
+    }
+    __syncthreads();  // LDS is used again in the next turn
+  }
 }
 
 template <typename T, typename G> struct Backward {
   template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)((size_t)a.N * ((a.D + kGlrThreads - 1) / kGlrThreads)));
-    hipLaunchKernelGGL((glr_backward_kernel<T, G, RAW, CONVEX>), grid, dim3(kGlrThreads), 0, s, a);
+    const long tiles = a.T > 0 ? ((long)a.T + kGlrGroup - 1) / kGlrGroup : 1, cols = ((long)a.D + 63) / 64;
+    if (tiles * cols > 0xffff0000l) return hipErrorInvalidValue;  // the turns' range
+    if (tiles > 1) {
+      const hipError_t e = launch_glr_setup(a, (size_t)tiles * a.D, (uint32_t)cols, s);
+      if (e != hipSuccess) return e;
+    }
+    const long resident = 2l * (a.cus > 0 ? a.cus : 256);
+    const unsigned grid = (unsigned)(tiles * cols < resident ? tiles * cols : resident);
+    hipLaunchKernelGGL((glr_backward_kernel<T, G, RAW, CONVEX>), dim3(grid), dim3(kBackWaves * 64), 0, s, a, (uint32_t)tiles,
+                       (uint32_t)cols);
     return hipGetLastError();
   }
 };

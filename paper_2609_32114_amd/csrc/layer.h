@@ -27,6 +27,7 @@ struct GlrArgs {
   void *h, *dx, *dg;       // [T, D], contiguous
   float *s_final, *ds0;    // [N, D] or null
   float *ckpt;             // [ceil(T / kGlrGroup), D] states before each group's first token, or null
+  int cus;                 // compute units of the device
   // workspace: the device status word, a tile counter per 64 channels, and a word per
   // tile and channel (glr.h)
   int *status;
@@ -34,8 +35,8 @@ struct GlrArgs {
   uint64_t *words;
 };
 
-// Tokens of a forward and of a backward tile: a call of one tile needs no words.
-constexpr int kGlrTile = 256, kGlrBackTile = 128;
+// The smallest tile of the kernels, in tokens; a call of one tile needs no words.
+constexpr int kGlrLeastTile = 64;
 constexpr size_t kGlrHeader = 256;          // bytes before the counters
 constexpr size_t kGlrCounterStride = 32;    // counters lie in memory lines of their own
 inline size_t glr_counter_bytes(int D) { return ((size_t)D + 63) / 64 * kGlrCounterStride * sizeof(uint32_t); }
