@@ -66,10 +66,12 @@ template <bool RAW> __device__ __forceinline__ Gate glr_gate(float g) {
 // from adding the two first and holding every row's sum in a pair of vector registers.
 #ifdef __HIP_DEVICE_COMPILE__
 #define HAGDN_GLOBAL __attribute__((address_space(1)))
+#define HAGDN_LDS __attribute__((address_space(3)))
 #define HAGDN_SCALAR(p) asm("" : "+s"(p))
 #define HAGDN_VECTOR(v) asm("" : "+v"(v))
 #else  // the compiler's host pass only parses device code
 #define HAGDN_GLOBAL
+#define HAGDN_LDS
 #define HAGDN_SCALAR(p)
 #define HAGDN_VECTOR(v)
 #endif
@@ -92,25 +94,49 @@ __device__ __forceinline__ bool glr_seqlens_ok(const int32_t *cu, int N, int T) 
   return !__syncthreads_or(bad);
 }
 
+// The sequence offsets, in LDS where they fit: a wave looks its tokens' sequences up while
+// its rows are on their way, and loads from memory would have to wait for those (loads
+// return in order): packed batches of eight 251 -> XXX us in the backward pass.
+// The copy stands one entry further on, below a sentinel, so that no address formed on
+// the way to the entry before a sequence's lies below the array.  The pointers keep their
+// address spaces: a generic one to both would be a flat access, whose base may not
+// leave LDS even where its offset leads back.
+constexpr int kLdsOffsets = 1024;
+struct Offsets {
+  const HAGDN_GLOBAL int32_t *cu;  // null: one sequence of all tokens
+  int N;
+  const HAGDN_LDS int32_t *lds;
+  __device__ int operator[](int i) const {
+    if (N < kLdsOffsets) return lds[i + 1];
+    return cu[i];
+  }
+};
+// Fills the LDS copy; the caller's next barrier makes it whole.
+__device__ __forceinline__ Offsets stage_offsets(const int32_t *cu, int N, int32_t (&lds)[kLdsOffsets + 1]) {
+  if (cu && N < kLdsOffsets)
+    for (int i = threadIdx.x; i <= N + 1; i += blockDim.x) lds[i] = i == 0 ? -1 : cu[i - 1];
+  return {(const HAGDN_GLOBAL int32_t *)cu, N, (const HAGDN_LDS int32_t *)lds};
+}
+
 // The first and last tokens of sequences among a wave's tokens [t0, t0 + L), as bit
 // masks, and the sequences' numbers in LDS.
 template <int L> struct Marks {
   uint32_t first, last;  // uniform over the wave
-  const int32_t *cu;
+  bool many;             // more than one sequence in the call
   const int *ids;        // [2 L]: of the sequence that starts, ends at token t0 + i
-  __device__ int starts(int i) const { return cu ? __builtin_amdgcn_readfirstlane(ids[i]) : 0; }
-  __device__ int ends(int i) const { return cu ? __builtin_amdgcn_readfirstlane(ids[L + i]) : 0; }
+  __device__ int starts(int i) const { return many ? __builtin_amdgcn_readfirstlane(ids[i]) : 0; }
+  __device__ int ends(int i) const { return many ? __builtin_amdgcn_readfirstlane(ids[L + i]) : 0; }
 };
 
-// Finds them.  The 64 lanes probe cu together: each round of the search divides the
-// range by 64, then one look at the offsets from there on (more if tens of empty
+// Finds them.  The 64 lanes probe the offsets together: each round of the search divides
+// the range by 64, then one look at the offsets from there on (more if tens of empty
 // sequences lie there) marks every boundary.  No index or mark leaves its range
-// whatever cu holds.
-template <int L> __device__ __forceinline__ Marks<L> find_marks(const int32_t *cu, int N, int T, long t0, int (&ids)[2 * L]) {
-  const int lane = lane_id();
-  Marks<L> m{0, 0, cu, ids};
+// whatever they hold.
+template <int L> __device__ __forceinline__ Marks<L> find_marks(const Offsets &cu, int T, long t0, int (&ids)[2 * L]) {
+  const int lane = lane_id(), N = cu.N;
+  Marks<L> m{0, 0, cu.cu != nullptr, ids};
   if (t0 >= T) return m;
-  if (!cu) {
+  if (!m.many) {
     m.first = t0 == 0;
     m.last = t0 + L >= T ? 1u << (int)(T - 1 - t0) : 0;
     return m;
@@ -127,12 +153,12 @@ template <int L> __device__ __forceinline__ Marks<L> find_marks(const int32_t *c
   if (lane < 2 * L) ids[lane] = -1;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   for (long base = lo; base <= N; base += 64) {
-    const long s = base + lane;
+    const int s = (int)min(base + lane, (long)N + 1);  // N < 2^31 - 1
     bool past = true;
     if (s <= N) {
       const long v = cu[s], i = v - t0;
-      if (s < N && cu[s + 1] > v && i >= 0 && i < L) ids[i] = (int)s;
-      if (s > 0 && cu[s - 1] < v && i >= 1 && i <= L) ids[L + i - 1] = (int)s - 1;
+      if (s < N && cu[s + 1] > v && i >= 0 && i < L) ids[i] = s;
+      if (s > 0 && cu[s - 1] < v && i >= 1 && i <= L) ids[L + i - 1] = s - 1;
       past = i > L;
     }
     if (__any(past)) break;

@@ -28,8 +28,10 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
   constexpr int W = kGlrWaves;
   __shared__ float sA[W][64], sB[W][64], sIn[64];
   __shared__ int sIds[W][2 * L], sReset[W];
+  __shared__ int32_t sCu[kLdsOffsets + 1];
   __shared__ uint32_t sNext;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Offsets cu = stage_offsets(a.cu, a.N, sCu);
   bool ok = true;
   if (tiles > 1) {
     ok = *a.status == 0;
@@ -68,7 +70,7 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
       px += i + 1 < count ? a.xs : 0;
       pg += i + 1 < count ? a.gs : 0;
     }
-    const Marks<L> m = find_marks<L>(a.cu, a.N, a.T, t0, sIds[wave]);
+    const Marks<L> m = find_marks<L>(cu, a.T, t0, sIds[wave]);
     // The initial state of the last sequence that starts here, the only one that can
     // reach past the wave's tokens.  It is read before the tile's map is published, the
     // others' when their tokens' turn comes: where s_final is s0, a state is written by

@@ -19,8 +19,10 @@ __global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArg
   constexpr int L = kBackRun, W = kBackWaves;
   __shared__ float sA[W][64], sF[W][64], sR[W][64], sIn[64];
   __shared__ int sIds[W][2 * L], sFirst[W], sLast[W], sEnded;
+  __shared__ int32_t sCu[kLdsOffsets + 1];
   __shared__ uint32_t sNext;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Offsets cu = stage_offsets(a.cu, a.N, sCu);
   bool ok = true;
   if (tiles > 1) {
     ok = *a.status == 0;
@@ -63,7 +65,7 @@ __global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArg
       py += i + 1 < count ? a.dhs : 0;
     }
     float s = *in_row(a.ckpt + (size_t)tile * a.D, c);
-    const Marks<L> m = find_marks<L>(a.cu, a.N, a.T, t0, sIds[wave]);
+    const Marks<L> m = find_marks<L>(cu, a.T, t0, sIds[wave]);
     // The last sequence that starts here is the only one to reach past the wave's tokens,
     // the first that ends here the only one to come from before them; its dfinal is read
     // before the tile's map is published, the others' when their tokens' turn comes:
