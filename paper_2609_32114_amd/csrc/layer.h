@@ -90,8 +90,12 @@ hipError_t launch_add_norm_backward(const AddNormArgs &, bool bf16, bool res_bf1
 hipError_t launch_gate_norm(const GateNormArgs &, bool bf16, hipStream_t);
 hipError_t launch_gate_norm_backward(const GateNormArgs &, bool bf16, hipStream_t);
 
-// Workgroups that share the rows of a backward norm, each with its own partial
-// sums of the weights' gradients: one to four a CU, never more than rows.
-int norm_parts(long rows, int cus);
+// Workgroups that share the rows of a backward norm, each with its own partial sums of
+// `cols` weight gradients: as many as keep the device busy while the partial sums stay
+// small beside the rows.  At most one a row.
+inline int norm_parts(long rows, int cols, int cus) {
+  const long most = (cols <= 1024 ? 8l : cols <= 4096 ? 4l : 2l) * (cus > 0 ? cus : 256);
+  return (int)(rows < 1 ? 1 : rows < most ? rows : most);
+}
 
 }  // namespace hagdn
