@@ -112,7 +112,7 @@ hagdn::GlrForm form(int dtype, int gate_dtype, int convex, int pre) {
 }
 
 // --------------------------------------------------------------------- norms
-constexpr int kMaxNormDim = 16384;
+using hagdn::kMaxNormDim;
 
 int check_rows(int T, long per_token, int d, float eps) {
   if (T < 0) return fail(HAGDN_EINVAL, "T must be >= 0 (got %d)", T);
@@ -125,7 +125,7 @@ int check_rows(int T, long per_token, int d, float eps) {
 }
 
 size_t partial_bytes(long rows, int cols, int cus) {
-  return (size_t)hagdn::norm_parts(rows, cols, cus) * (size_t)cols * sizeof(float);
+  return (size_t)hagdn::norm_parts(rows, cus) * (size_t)cols * sizeof(float);
 }
 
 int query_cus() {
@@ -254,7 +254,7 @@ int hagdn_add_norm_backward(const void *dy, int64_t dy_stride, const void *dres,
   a.x = vec || post ? x : nullptr; a.xs = x_stride;
   a.w = weight; a.post = post_weight; a.scale_vec = scale_vec; a.scale = scale; a.eps = eps; a.T = T; a.D = D;
   a.dx = dx; a.dres_out = dres_out; a.dw = dweight; a.dscale = vec ? dscale : nullptr; a.dpost = post ? dpost : nullptr;
-  a.partial = static_cast<float *>(workspace); a.parts = hagdn::norm_parts(T, D * (1 + vec + post), cus);
+  a.partial = static_cast<float *>(workspace); a.parts = hagdn::norm_parts(T, cus);
   return done(hagdn::launch_add_norm_backward(a, dtype == HAGDN_BF16, res_dtype == HAGDN_BF16,
                                               static_cast<hipStream_t>(stream)));
 }
@@ -305,7 +305,7 @@ int hagdn_gate_norm_backward(const void *dy, int64_t dy_stride, const void *o, i
   hagdn::GateNormArgs a = {};
   a.dy = dy; a.dys = dy_stride; a.o = o; a.os = o_stride; a.z = z; a.zs = z_stride; a.w = weight; a.eps = eps;
   a.T = T; a.H = H; a.d = d; a.silu = activation == HAGDN_ACT_SILU; a.dout = d_o; a.dz = d_z; a.dw = dweight;
-  a.partial = static_cast<float *>(workspace); a.parts = hagdn::norm_parts((long)T * H, d, cus);
+  a.partial = static_cast<float *>(workspace); a.parts = hagdn::norm_parts((long)T * H, cus);
   return done(hagdn::launch_gate_norm_backward(a, dtype == HAGDN_BF16, static_cast<hipStream_t>(stream)));
 }
 

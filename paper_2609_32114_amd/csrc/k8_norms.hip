@@ -5,9 +5,8 @@
 // All are bound by HBM: some 10 to 25 operations an element against 6 to 20 bytes.  So
 // every operand is loaded once, 16 bytes a lane, and a row stays in the registers of the
 // lanes that share it from its loads to its stores.  A row of n 16-byte chunks has
-// 16 to 1024 lanes (forward_rows): up to a wave each lane holds one chunk, then up to four
-// per lane, so that rows to 2048 bf16 elements need no barrier at all; longer ones one
-// barrier per sum.  The sums of the backward passes are taken together in one round: the
+// 8 to 1024 lanes (norm_rows); those of more than a wave meet in LDS, with one barrier a
+// round of sums.  The sums of the backward passes are taken together in one round: the
 // second norm's, which depends on the first's result, is linear in it.
 //
 // The weights' gradients sum over rows.  Each lane adds up its own elements of all the
@@ -31,16 +30,28 @@ template <typename T, int VE> struct Raw {  // VE elements as they lie in memory
     for (int i = 0; i < VE; ++i) v[i] = p[i];
   }
   __device__ float get(int i) const { return Elt<T>::to_f32(v[i]); }
+  __device__ void clear(int i) { v[i] = T(0); }
+  __device__ void keep_packed() {}
 };
 template <> struct Raw<bf16_t, 8> {
   u32x4 v;
   __device__ void load(const bf16_t *p) { v = *reinterpret_cast<const u32x4_any *>(p); }
   __device__ float get(int i) const { return __uint_as_float(i & 1 ? v[i >> 1] & 0xffff0000u : v[i >> 1] << 16); }
+  __device__ void clear(int i) { v[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u; }
+  // Makes the compiler unpack the elements anew from here on rather than hold them in
+  // fp32, in twice the registers, since their last use.
+  __device__ void keep_packed() {
+#ifdef __HIP_DEVICE_COMPILE__
+    asm("" : "+v"(v));
+#endif
+  }
 };
 template <> struct Raw<float, 4> {
   f32x4 v;
   __device__ void load(const float *p) { v = *reinterpret_cast<const f32x4_any *>(p); }
   __device__ float get(int i) const { return v[i]; }
+  __device__ void clear(int i) { v[i] = 0.f; }
+  __device__ void keep_packed() {}
 };
 template <> struct Raw<float, 8> {
   f32x4 v[2];
@@ -49,6 +60,8 @@ template <> struct Raw<float, 8> {
     v[1] = *reinterpret_cast<const f32x4_any *>(p + 4);
   }
   __device__ float get(int i) const { return v[i >> 2][i & 3]; }
+  __device__ void clear(int i) { v[i >> 2][i & 3] = 0.f; }
+  __device__ void keep_packed() {}
 };
 template <int VE> __device__ __forceinline__ void store_vec(bf16_t *p, const float (&v)[VE]) {
   if constexpr (VE == 8) {
@@ -84,21 +97,22 @@ template <int VE> struct Chunk {
     at = min(e0, d - VE);
     skip = min(e0 - at, VE);
   }
-  template <typename T> __device__ Raw<T, VE> fetch(const T *row) const {
-    Raw<T, VE> r;
-    r.load(row + at);
-    return r;
-  }
-  // In fp32; elements that are another lane's come as zeros.
-  template <typename T> __device__ void open(const Raw<T, VE> &r, float (&v)[VE]) const {
+  template <typename T> __device__ void fetch(const T *row, Raw<T, VE> &r) const { r.load(row + at); }
+  // Clears the elements that are another lane's (those before `skip`; n = VE: all).
+  template <typename T> __device__ static void clear(Raw<T, VE> &r, int n) {
+    if (n > 0) {
 #pragma unroll
-    for (int j = 0; j < VE; ++j) v[j] = r.get(j);
-    if (skip > 0) {
-#pragma unroll
-      for (int j = 0; j < VE; ++j) v[j] = j < skip ? 0.f : v[j];
+      for (int j = 0; j < VE; ++j)
+        if (j < n) r.clear(j);
     }
   }
-  template <typename T> __device__ void load(const T *row, float (&v)[VE]) const { open(fetch(row), v); }
+  template <typename T> __device__ void load(const T *row, float (&v)[VE]) const {
+    Raw<T, VE> r;
+    fetch(row, r);
+    clear(r, skip);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) v[j] = r.get(j);
+  }
   template <typename T> __device__ void store(T *row, const float (&v)[VE]) const {
     if (skip == 0) {
       store_vec<VE>(row + at, v);
@@ -118,18 +132,18 @@ template <int CTRL> __device__ __forceinline__ float dpp_add(float x) {
   return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
 }
 template <int LANES> __device__ __forceinline__ float lanes_sum(float x) {
-  x = dpp_add<0xb1>(x);   // lanes 1, 0, 3, 2
-  x = dpp_add<0x4e>(x);   // lanes 2, 3, 0, 1
-  x = dpp_add<0x141>(x);  // 8 lanes mirrored
-  x = dpp_add<0x140>(x);  // 16 lanes mirrored
+  x = dpp_add<0xb1>(x);                             // lanes 1, 0, 3, 2
+  if constexpr (LANES >= 4) x = dpp_add<0x4e>(x);   // lanes 2, 3, 0, 1
+  if constexpr (LANES >= 8) x = dpp_add<0x141>(x);  // 8 lanes mirrored
+  if constexpr (LANES >= 16) x = dpp_add<0x140>(x);  // 16 lanes mirrored
   if constexpr (LANES >= 32) x += __shfl_xor(x, 16);
   if constexpr (LANES >= 64) x += __shfl_xor(x, 32);
   return x;
 }
-template <int LANES> constexpr int row_threads() { return LANES > 256 ? LANES : 256; }  // of a workgroup
-template <int LANES, int K> struct RowSums {
+// THREADS: of the workgroup, whose rows all take their barriers together.
+template <int LANES, int THREADS, int K> struct RowSums {
   static constexpr int kWaves = LANES / 64;
-  float (*buf)[row_threads<LANES>() / 64][K];  // [2]
+  float (*buf)[THREADS / 64][K];  // [2]
   int turn = 0;
   __device__ void operator()(float (&v)[K]) {
 #pragma unroll
@@ -140,19 +154,16 @@ template <int LANES, int K> struct RowSums {
 #pragma unroll
         for (int k = 0; k < K; ++k) buf[turn][wave][k] = v[k];
       __syncthreads();
+      const int first = threadIdx.x / LANES * kWaves;
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        v[k] = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) v[k] += buf[turn][threadIdx.x / LANES * kWaves + w][k];
-      }
+      for (int k = 0; k < K; ++k) v[k] = lanes_sum<kWaves>(buf[turn][first + threadIdx.x % kWaves][k]);
       turn ^= 1;
     }
   }
 };
-#define HAGDN_ROW_SUMS(name, LANES, K)                              \
-  __shared__ float name##_buf[2][row_threads<LANES>() / 64][K];     \
-  RowSums<LANES, K> name{name##_buf}
+#define HAGDN_ROW_SUMS(name, LANES, THREADS, K)           \
+  __shared__ float name##_buf[2][(THREADS) / 64][K];      \
+  RowSums<LANES, THREADS, K> name{name##_buf}
 
 __device__ __forceinline__ float rstd(float sum, float inv, float eps) { return 1.f / sqrtf(sum * inv + eps); }
 
@@ -211,16 +222,24 @@ static hipError_t sum_parts(const float *partial, int parts, int D, float *o0, f
   return hipGetLastError();
 }
 
+// Threads of a workgroup: rows of up to a wave need no barrier, and short workgroups end
+// apart; in the backward passes more rows together mean fewer partial sums.
+template <int LANES> constexpr int forward_threads() { return LANES > 256 ? LANES : 256; }
+template <int LANES> constexpr int backward_threads() { return LANES > 512 ? LANES : 512; }
+
 // ---------------------------------------------------------------------- add_norm
 template <typename T, typename R, int VE, int LANES, int C>
-__global__ __launch_bounds__(row_threads<LANES>()) void add_norm_kernel(AddNormArgs a) {
-  constexpr int kRows = row_threads<LANES>() / LANES;
-  HAGDN_ROW_SUMS(sums, LANES, 1);
+__global__ __launch_bounds__(forward_threads<LANES>()) void add_norm_kernel(AddNormArgs a) {
+  constexpr int kThreads = forward_threads<LANES>(), kRows = kThreads / LANES;
+  HAGDN_ROW_SUMS(sums, LANES, kThreads, 1);
   const float inv = 1.f / (float)a.D;
   Chunk<VE> ch[C];
 #pragma unroll
   for (int j = 0; j < C; ++j) ch[j] = Chunk<VE>((j * LANES + threadIdx.x % LANES) * VE, a.D);
-  for (long row = (long)blockIdx.x * kRows + threadIdx.x / LANES; row < a.T; row += (long)gridDim.x * kRows) {
+  // the loop's bounds are those of the workgroup's first row: all lanes take every turn
+  for (long first = (long)blockIdx.x * kRows; first < a.T; first += (long)gridDim.x * kRows) {
+    const bool live = first + threadIdx.x / LANES < a.T;
+    const long row = live ? first + threadIdx.x / LANES : a.T - 1;
     const T *x = static_cast<const T *>(a.x) + row * a.xs;
     float u[C][VE], r[C][VE], w[VE], v[1];
 #pragma unroll
@@ -267,11 +286,11 @@ __global__ __launch_bounds__(row_threads<LANES>()) void add_norm_kernel(AddNormA
     const float rr = rstd(v[0], inv, a.eps);
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      if (a.res_out) ch[j].store(static_cast<R *>(a.res_out) + row * a.D, r[j]);
+      if (a.res_out && live) ch[j].store(static_cast<R *>(a.res_out) + row * a.D, r[j]);
       ch[j].load(a.w, w);
 #pragma unroll
       for (int e = 0; e < VE; ++e) r[j][e] *= rr * w[e];
-      ch[j].store(static_cast<T *>(a.y) + row * a.D, r[j]);
+      if (live) ch[j].store(static_cast<T *>(a.y) + row * a.D, r[j]);
     }
   }
 }
@@ -279,77 +298,80 @@ __global__ __launch_bounds__(row_threads<LANES>()) void add_norm_kernel(AddNormA
 // With D the gradient of r', m = mean(r' w dy) and q = mean(x post s D):
 //   D = dres + rr (w dy - r' rr^2 m),   dx = rx (post s D - x rx^2 q).
 // q is taken from D's three terms' own sums, so that one round of sums serves the row.
-// READS_X: a scale vector or post_weight is there.
+// The operands stay as they were loaded (bf16 ones two to a register), the weights in
+// registers for all of the workgroup's rows.  READS_X: a scale vector or post_weight is
+// there.
 template <typename T, typename R, int VE, int LANES, int C, bool READS_X>
-__global__ __launch_bounds__(row_threads<LANES>(), 4) void add_norm_backward_kernel(AddNormArgs a) {
-  constexpr int kRows = row_threads<LANES>() / LANES, kSums = READS_X ? 6 : 2;
-  HAGDN_ROW_SUMS(sums, LANES, kSums);
+__global__ __launch_bounds__(backward_threads<LANES>(), LANES > 512 || !READS_X ? 4 : 2) void add_norm_backward_kernel(
+    AddNormArgs a) {
+  constexpr int kThreads = backward_threads<LANES>(), kRows = kThreads / LANES, kSums = READS_X ? 6 : 2;
+  HAGDN_ROW_SUMS(sums, LANES, kThreads, kSums);
   __shared__ float lds[kRows > 1 ? kRows * LANES : 1];
   const float inv = 1.f / (float)a.D;
   Chunk<VE> ch[C];
-  float aw[C][VE], as[C][VE], ap[C][VE];
+  float aw[C][VE], as[C][VE], ap[C][VE];  // the weights' gradients
+  float w[C][VE], s[C][VE], p[C][VE];     // weight, scale, post_weight
 #pragma unroll
   for (int j = 0; j < C; ++j) {
     ch[j] = Chunk<VE>((j * LANES + threadIdx.x % LANES) * VE, a.D);
 #pragma unroll
     for (int e = 0; e < VE; ++e) aw[j][e] = as[j][e] = ap[j][e] = 0.f;
   }
+#pragma unroll
+  for (int j = 0; j < C; ++j) {
+    ch[j].load(a.w, w[j]);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) s[j][e] = a.scale, p[j][e] = 1.f;
+    if (READS_X && a.scale_vec) ch[j].load(a.scale_vec, s[j]);
+    if (READS_X && a.post) ch[j].load(a.post, p[j]);
+  }
   // the loop's bounds are those of the workgroup's first row: all lanes take every turn.
   // A row's operands are fetched while the one before is worked on.
   const long step = (long)gridDim.x * kRows, own = threadIdx.x / LANES;
-  Raw<R, VE> fr[C], fd[C];
-  Raw<T, VE> fg[C], fx[C];
+  Raw<R, VE> nr[C], nd[C];
+  Raw<T, VE> ng[C], nx[C];
   auto fetch = [&](long row) {
     row = min(row, (long)a.T - 1);
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      fr[j] = ch[j].fetch(static_cast<const R *>(a.res) + row * a.rs);
-      fg[j] = ch[j].fetch(static_cast<const T *>(a.dy) + row * a.dys);
-      if (a.dres) fd[j] = ch[j].fetch(static_cast<const R *>(a.dres) + row * a.drs);
-      if constexpr (READS_X) fx[j] = ch[j].fetch(static_cast<const T *>(a.x) + row * a.xs);
+      ch[j].fetch(static_cast<const R *>(a.res) + row * a.rs, nr[j]);
+      ch[j].fetch(static_cast<const T *>(a.dy) + row * a.dys, ng[j]);
+      if (a.dres) ch[j].fetch(static_cast<const R *>(a.dres) + row * a.drs, nd[j]);
+      if constexpr (READS_X) ch[j].fetch(static_cast<const T *>(a.x) + row * a.xs, nx[j]);
     }
   };
   if (a.T > 0) fetch((long)blockIdx.x * kRows + own);
   for (long first = (long)blockIdx.x * kRows; first < a.T; first += step) {
     const long row = first + own;
     const bool live = row < a.T;
-    float x[C][VE], r[C][VE], g[C][VE], d[C][VE];  // x, r', dy then w dy, dres then D
-    float v[kSums] = {};
+    Raw<R, VE> r[C], d[C];  // r', dres
+    Raw<T, VE> g[C], x[C];  // dy, x
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      ch[j].open(fr[j], r[j]);
-      ch[j].open(fg[j], g[j]);
-      if (a.dres) ch[j].open(fd[j], d[j]);
-      if constexpr (READS_X) ch[j].open(fx[j], x[j]);
-#pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        if (!a.dres) d[j][e] = 0.f;
-        if (!live) g[j][e] = d[j][e] = 0.f;
-      }
+      r[j] = nr[j], g[j] = ng[j], d[j] = nd[j];
+      if constexpr (READS_X) x[j] = nx[j];
+      Chunk<VE>::clear(r[j], ch[j].skip);
+      if constexpr (READS_X) Chunk<VE>::clear(x[j], ch[j].skip);
+      Chunk<VE>::clear(g[j], live ? ch[j].skip : VE);  // a row past the end adds nothing
+      Chunk<VE>::clear(d[j], live && a.dres ? ch[j].skip : VE);
     }
     if (first + step < a.T) fetch(row + step);
+    float v[kSums] = {};
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-      float w[VE], s[VE], p[VE];
-      ch[j].load(a.w, w);
-      if constexpr (READS_X) {
-        if (a.scale_vec) ch[j].load(a.scale_vec, s);
-        if (a.post) ch[j].load(a.post, p);
-      }
+    for (int j = 0; j < C; ++j)
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        const float wg = w[e] * g[j][e];
-        v[0] += r[j][e] * r[j][e];
-        v[1] += r[j][e] * wg;
+        const float re = r[j].get(e), wg = w[j][e] * g[j].get(e);
+        v[0] += re * re;
+        v[1] += re * wg;
         if constexpr (READS_X) {
-          const float ps = (a.post ? p[e] : 1.f) * (a.scale_vec ? s[e] : a.scale), xs = x[j][e] * ps;
-          v[2] += x[j][e] * x[j][e];
-          v[3] += xs * d[j][e];
+          const float xe = x[j].get(e), xs = xe * (p[j][e] * s[j][e]);
+          v[2] += xe * xe;
+          v[3] += xs * d[j].get(e);
           v[4] += xs * wg;
-          v[5] += xs * r[j][e];
+          v[5] += xs * re;
         }
       }
-    }
     sums(v);
     const float rr = rstd(v[0], inv, a.eps), m = rr * rr * rr * v[1] * inv;
     float rx = 1.f, q = 0.f;
@@ -361,31 +383,29 @@ __global__ __launch_bounds__(row_threads<LANES>(), 4) void add_norm_backward_ker
     }
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      float w[VE], s[VE], p[VE];
-      ch[j].load(a.w, w);
-      if constexpr (READS_X) {
-        if (a.scale_vec) ch[j].load(a.scale_vec, s);
-        if (a.post) ch[j].load(a.post, p);
-      }
+      float out[VE], dx[VE];
+      r[j].keep_packed();
+      g[j].keep_packed();
+      d[j].keep_packed();
+      if constexpr (READS_X) x[j].keep_packed();
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        aw[j][e] += g[j][e] * (r[j][e] * rr);
-        d[j][e] += rr * (w[e] * g[j][e]) - m * r[j][e];
+        const float re = r[j].get(e), ge = g[j].get(e);
+        aw[j][e] += ge * (re * rr);
+        out[e] = d[j].get(e) + (rr * (w[j][e] * ge) - m * re);
+        const float du = s[j][e] * out[e];
         if constexpr (READS_X) {
-          const float xn = x[j][e] * rx, se = a.scale_vec ? s[e] : a.scale;
-          const float du = se * d[j][e];
-          if (live) {
-            as[j][e] += d[j][e] * xn * (a.post ? p[e] : 1.f);
-            ap[j][e] += du * xn;
-          }
-          x[j][e] = a.post ? rx * (p[e] * du - x[j][e] * q) : du;
+          const float xe = x[j].get(e), xn = xe * rx;
+          as[j][e] += out[e] * xn * p[j][e];
+          ap[j][e] += du * xn;
+          dx[e] = rx * (p[j][e] * du - xe * q);
         } else {
-          g[j][e] = a.scale * d[j][e];
+          dx[e] = du;
         }
       }
       if (live) {
-        if (a.dres_out) ch[j].store(static_cast<R *>(a.dres_out) + row * a.D, d[j]);
-        ch[j].store(static_cast<T *>(a.dx) + row * a.D, READS_X ? x[j] : g[j]);
+        if (a.dres_out) ch[j].store(static_cast<R *>(a.dres_out) + row * a.D, out);
+        ch[j].store(static_cast<T *>(a.dx) + row * a.D, dx);
       }
     }
   }
@@ -414,15 +434,18 @@ __device__ __forceinline__ long head_row(uint32_t row, int H, int d, long stride
 }
 
 template <typename T, int VE, int LANES, int C>
-__global__ __launch_bounds__(row_threads<LANES>()) void gate_norm_kernel(GateNormArgs a) {
-  constexpr int kRows = row_threads<LANES>() / LANES;
-  HAGDN_ROW_SUMS(sums, LANES, 1);
+__global__ __launch_bounds__(forward_threads<LANES>()) void gate_norm_kernel(GateNormArgs a) {
+  constexpr int kThreads = forward_threads<LANES>(), kRows = kThreads / LANES;
+  HAGDN_ROW_SUMS(sums, LANES, kThreads, 1);
   const float inv = 1.f / (float)a.d;
   const long rows = (long)a.T * a.H;
   Chunk<VE> ch[C];
 #pragma unroll
   for (int j = 0; j < C; ++j) ch[j] = Chunk<VE>((j * LANES + threadIdx.x % LANES) * VE, a.d);
-  for (long row = (long)blockIdx.x * kRows + threadIdx.x / LANES; row < rows; row += (long)gridDim.x * kRows) {
+  // the loop's bounds are those of the workgroup's first row: all lanes take every turn
+  for (long first = (long)blockIdx.x * kRows; first < rows; first += (long)gridDim.x * kRows) {
+    const bool live = first + threadIdx.x / LANES < rows;
+    const long row = live ? first + threadIdx.x / LANES : rows - 1;
     const T *o = static_cast<const T *>(a.o) + head_row((uint32_t)row, a.H, a.d, a.os);
     const T *zr = static_cast<const T *>(a.z) + head_row((uint32_t)row, a.H, a.d, a.zs);
     float x[C][VE], z[C][VE], w[VE], v[1] = {0.f};
@@ -446,30 +469,32 @@ __global__ __launch_bounds__(row_threads<LANES>()) void gate_norm_kernel(GateNor
         activation(a.silu, z[j][e], f, df);
         x[j][e] *= r * w[e] * f;
       }
-      ch[j].store(static_cast<T *>(a.y) + row * a.d, x[j]);
+      if (live) ch[j].store(static_cast<T *>(a.y) + row * a.d, x[j]);
     }
   }
 }
 
 template <typename T, int VE, int LANES, int C>
-__global__ __launch_bounds__(row_threads<LANES>(), 4) void gate_norm_backward_kernel(GateNormArgs a) {
-  constexpr int kRows = row_threads<LANES>() / LANES;
-  HAGDN_ROW_SUMS(sums, LANES, 2);
+__global__ __launch_bounds__(backward_threads<LANES>(), LANES > 512 || sizeof(T) == 2 ? 4 : 3) void gate_norm_backward_kernel(
+    GateNormArgs a) {
+  constexpr int kThreads = backward_threads<LANES>(), kRows = kThreads / LANES;
+  HAGDN_ROW_SUMS(sums, LANES, kThreads, 2);
   __shared__ float lds[kRows > 1 ? kRows * LANES : 1];
   const float inv = 1.f / (float)a.d;
   const long rows = (long)a.T * a.H;
   Chunk<VE> ch[C];
-  float aw[C][VE];
+  float aw[C][VE], w[C][VE];
 #pragma unroll
   for (int j = 0; j < C; ++j) {
     ch[j] = Chunk<VE>((j * LANES + threadIdx.x % LANES) * VE, a.d);
+    ch[j].load(a.w, w[j]);
 #pragma unroll
     for (int e = 0; e < VE; ++e) aw[j][e] = 0.f;
   }
   // the loop's bounds are those of the workgroup's first row: all lanes take every turn.
   // A row's operands are fetched while the one before is worked on.
   const long step = (long)gridDim.x * kRows, own = threadIdx.x / LANES;
-  Raw<T, VE> fx[C], fz[C], fg[C];
+  Raw<T, VE> nx[C], nz[C], ng[C];
   auto fetch = [&](long row) {
     const uint32_t r = (uint32_t)min(row, rows - 1);
     const T *o = static_cast<const T *>(a.o) + head_row(r, a.H, a.d, a.os);
@@ -477,52 +502,55 @@ __global__ __launch_bounds__(row_threads<LANES>(), 4) void gate_norm_backward_ke
     const T *dy = static_cast<const T *>(a.dy) + head_row(r, a.H, a.d, a.dys);
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      fx[j] = ch[j].fetch(o);
-      fz[j] = ch[j].fetch(z);
-      fg[j] = ch[j].fetch(dy);
+      ch[j].fetch(o, nx[j]);
+      ch[j].fetch(z, nz[j]);
+      ch[j].fetch(dy, ng[j]);
     }
   };
   if (rows > 0) fetch((long)blockIdx.x * kRows + own);
   for (long first = (long)blockIdx.x * kRows; first < rows; first += step) {
     const long row = first + own;
     const bool live = row < rows;
-    float x[C][VE], z[C][VE], g[C][VE], v[2] = {0.f, 0.f};  // o, z then dz's factor, dy then dn
+    Raw<T, VE> x[C];
+    float z[C][VE], g[C][VE], v[2] = {0.f, 0.f};  // dy w act'(z), dn
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      ch[j].open(fx[j], x[j]);
-      ch[j].open(fz[j], z[j]);
-      ch[j].open(fg[j], g[j]);
-    }
-    if (first + step < rows) fetch(row + step);
-#pragma unroll
-    for (int j = 0; j < C; ++j) {
-      float w[VE];
-      ch[j].load(a.w, w);
+      x[j] = nx[j];
+      Raw<T, VE> dy = ng[j];
+      Chunk<VE>::clear(x[j], ch[j].skip);
+      Chunk<VE>::clear(dy, live ? ch[j].skip : VE);  // a row past the end adds nothing
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
         float f, df;
-        activation(a.silu, z[j][e], f, df);
-        z[j][e] = g[j][e] * w[e] * df;
-        g[j][e] = live ? g[j][e] * f : 0.f;
-        v[0] += x[j][e] * x[j][e];
-        v[1] += x[j][e] * w[e] * g[j][e];
+        activation(a.silu, nz[j].get(e), f, df);
+        z[j][e] = dy.get(e) * w[j][e] * df;
+        g[j][e] = dy.get(e) * f;
       }
     }
+    if (first + step < rows) fetch(row + step);
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const float xe = x[j].get(e);
+        v[0] += xe * xe;
+        v[1] += xe * (w[j][e] * g[j][e]);
+      }
     sums(v);
     const float r = rstd(v[0], inv, a.eps), m = r * r * r * v[1] * inv;
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      float w[VE], dn[VE];
-      ch[j].load(a.w, w);
+      float dx[VE];
+      x[j].keep_packed();
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        const float n = x[j][e] * r;
+        const float xe = x[j].get(e), n = xe * r;
         aw[j][e] += g[j][e] * n;
         z[j][e] *= n;
-        dn[e] = r * (w[e] * g[j][e]) - m * x[j][e];
+        dx[e] = r * (w[j][e] * g[j][e]) - m * xe;
       }
       if (live) {
-        ch[j].store(static_cast<T *>(a.dout) + row * a.d, dn);
+        ch[j].store(static_cast<T *>(a.dout) + row * a.d, dx);
         ch[j].store(static_cast<T *>(a.dz) + row * a.d, z[j]);
       }
     }
@@ -532,33 +560,23 @@ __global__ __launch_bounds__(row_threads<LANES>(), 4) void gate_norm_backward_ke
 
 // -------------------------------------------------------------------- launches
 // The lanes of a row of d elements and the chunks of each, K::go<VE, LANES, C>; V is the
-// vector's elements (16 bytes of the operands' type).
-template <int V, typename K> static hipError_t forward_rows(int d, const K &k) {
-  const int n = (d + V - 1) / V;
-  if (d < V) return k.template go<1, 16, 1>();
-  if (n <= 16) return k.template go<V, 16, 1>();
-  if (n <= 32) return k.template go<V, 32, 1>();
-  if (n <= 64) return k.template go<V, 64, 1>();
-  if (n <= 128) return k.template go<V, 64, 2>();
-  if (n <= 256) return k.template go<V, 64, 4>();
-  if (n <= 512) return k.template go<V, 256, 2>();
-  if (n <= 1024) return k.template go<V, 256, 4>();
-  if constexpr (V == 4)
-    if (n > 2048) return k.template go<V, 1024, 4>();
-  return k.template go<V, 1024, 2>();
-}
-// Backward passes keep sums of their own beside the row, so eight elements a lane (of the
-// widest rows 16) and a barrier a row beyond 512 elements.
-template <int V, typename K> static hipError_t backward_rows(int d, const K &k) {
-  constexpr int C = 8 / V;
-  if (d < V) return k.template go<1, 16, 1>();
-  if (d <= 128) return k.template go<V, 16, C>();
-  if (d <= 256) return k.template go<V, 32, C>();
-  if (d <= 512) return k.template go<V, 64, C>();
-  if (d <= 1024) return k.template go<V, 128, C>();
-  if (d <= 2048) return k.template go<V, 256, C>();
-  if (d <= 4096) return k.template go<V, 512, C>();
-  if (d <= 8192) return k.template go<V, 1024, C>();
+// vector's elements (16 bytes of the operands' type).  One chunk a lane, in the backward
+// passes eight elements, wherever 1024 lanes hold the row: rows of 2048 bf16 elements on
+// one wave with four chunks a lane, which need no barrier, took 115 us instead of 98
+// (32768 of them, add_norm).
+template <int V, int C, typename K> static hipError_t norm_rows(int d, const K &k) {
+  constexpr int E = V * C;
+  if (d < V) return k.template go<1, 8, 1>();
+  if (d <= 8 * E) return k.template go<V, 8, C>();
+  if (d <= 16 * E) return k.template go<V, 16, C>();
+  if (d <= 32 * E) return k.template go<V, 32, C>();
+  if (d <= 64 * E) return k.template go<V, 64, C>();
+  if (d <= 128 * E) return k.template go<V, 128, C>();
+  if (d <= 256 * E) return k.template go<V, 256, C>();
+  if (d <= 512 * E) return k.template go<V, 512, C>();
+  if (d <= 1024 * E) return k.template go<V, 1024, C>();
+  if constexpr (1024 * E * 2 < kMaxNormDim)
+    if (d > 1024 * E * 2) return k.template go<V, 1024, 4 * C>();
   return k.template go<V, 1024, 2 * C>();
 }
 
@@ -572,8 +590,8 @@ template <typename T, typename R> struct AddNorm {
   const AddNormArgs &a;
   hipStream_t s;
   template <int VE, int LANES, int C> hipError_t go() const {
-    hipLaunchKernelGGL((add_norm_kernel<T, R, VE, LANES, C>), dim3(norm_grid(a.T, row_threads<LANES>() / LANES)),
-                       dim3(row_threads<LANES>()), 0, s, a);
+    hipLaunchKernelGGL((add_norm_kernel<T, R, VE, LANES, C>), dim3(norm_grid(a.T, forward_threads<LANES>() / LANES)),
+                       dim3(forward_threads<LANES>()), 0, s, a);
     return hipGetLastError();
   }
 };
@@ -581,7 +599,7 @@ template <typename T, typename R> struct AddNormBackward {
   const AddNormArgs &a;
   hipStream_t s;
   template <int VE, int LANES, int C> hipError_t go() const {
-    const dim3 grid(a.parts), block(row_threads<LANES>());
+    const dim3 grid(a.parts), block(backward_threads<LANES>());
     if (a.post || a.scale_vec) hipLaunchKernelGGL((add_norm_backward_kernel<T, R, VE, LANES, C, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((add_norm_backward_kernel<T, R, VE, LANES, C, false>), grid, block, 0, s, a);
     const hipError_t e = hipGetLastError();
@@ -593,8 +611,8 @@ template <typename T> struct GateNorm {
   const GateNormArgs &a;
   hipStream_t s;
   template <int VE, int LANES, int C> hipError_t go() const {
-    hipLaunchKernelGGL((gate_norm_kernel<T, VE, LANES, C>), dim3(norm_grid((long)a.T * a.H, row_threads<LANES>() / LANES)),
-                       dim3(row_threads<LANES>()), 0, s, a);
+    hipLaunchKernelGGL((gate_norm_kernel<T, VE, LANES, C>), dim3(norm_grid((long)a.T * a.H, forward_threads<LANES>() / LANES)),
+                       dim3(forward_threads<LANES>()), 0, s, a);
     return hipGetLastError();
   }
 };
@@ -602,29 +620,29 @@ template <typename T> struct GateNormBackward {
   const GateNormArgs &a;
   hipStream_t s;
   template <int VE, int LANES, int C> hipError_t go() const {
-    hipLaunchKernelGGL((gate_norm_backward_kernel<T, VE, LANES, C>), dim3(a.parts), dim3(row_threads<LANES>()), 0, s, a);
+    hipLaunchKernelGGL((gate_norm_backward_kernel<T, VE, LANES, C>), dim3(a.parts), dim3(backward_threads<LANES>()), 0, s, a);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : sum_parts(a.partial, a.parts, a.d, a.dw, nullptr, nullptr, s);
   }
 };
 
 hipError_t launch_add_norm(const AddNormArgs &a, bool bf16, bool res_bf16, hipStream_t s) {
-  if (!bf16) return forward_rows<4>(a.D, AddNorm<float, float>{a, s});
-  return res_bf16 ? forward_rows<8>(a.D, AddNorm<bf16_t, bf16_t>{a, s}) : forward_rows<8>(a.D, AddNorm<bf16_t, float>{a, s});
+  if (!bf16) return norm_rows<4, 1>(a.D, AddNorm<float, float>{a, s});
+  return res_bf16 ? norm_rows<8, 1>(a.D, AddNorm<bf16_t, bf16_t>{a, s}) : norm_rows<8, 1>(a.D, AddNorm<bf16_t, float>{a, s});
 }
 
 hipError_t launch_add_norm_backward(const AddNormArgs &a, bool bf16, bool res_bf16, hipStream_t s) {
-  if (!bf16) return backward_rows<4>(a.D, AddNormBackward<float, float>{a, s});
-  return res_bf16 ? backward_rows<8>(a.D, AddNormBackward<bf16_t, bf16_t>{a, s})
-                  : backward_rows<8>(a.D, AddNormBackward<bf16_t, float>{a, s});
+  if (!bf16) return norm_rows<4, 2>(a.D, AddNormBackward<float, float>{a, s});
+  return res_bf16 ? norm_rows<8, 1>(a.D, AddNormBackward<bf16_t, bf16_t>{a, s})
+                  : norm_rows<8, 1>(a.D, AddNormBackward<bf16_t, float>{a, s});
 }
 
 hipError_t launch_gate_norm(const GateNormArgs &a, bool bf16, hipStream_t s) {
-  return bf16 ? forward_rows<8>(a.d, GateNorm<bf16_t>{a, s}) : forward_rows<4>(a.d, GateNorm<float>{a, s});
+  return bf16 ? norm_rows<8, 1>(a.d, GateNorm<bf16_t>{a, s}) : norm_rows<4, 1>(a.d, GateNorm<float>{a, s});
 }
 
 hipError_t launch_gate_norm_backward(const GateNormArgs &a, bool bf16, hipStream_t s) {
-  return bf16 ? backward_rows<8>(a.d, GateNormBackward<bf16_t>{a, s}) : backward_rows<4>(a.d, GateNormBackward<float>{a, s});
+  return bf16 ? norm_rows<8, 1>(a.d, GateNormBackward<bf16_t>{a, s}) : norm_rows<4, 2>(a.d, GateNormBackward<float>{a, s});
 }
 
 }  // namespace hagdn

@@ -90,11 +90,14 @@ hipError_t launch_add_norm_backward(const AddNormArgs &, bool bf16, bool res_bf1
 hipError_t launch_gate_norm(const GateNormArgs &, bool bf16, hipStream_t);
 hipError_t launch_gate_norm_backward(const GateNormArgs &, bool bf16, hipStream_t);
 
+// Elements of a norm's row at most.
+constexpr int kMaxNormDim = 16384;
 // Workgroups that share the rows of a backward norm, each with its own partial sums of
-// `cols` weight gradients: as many as keep the device busy while the partial sums stay
-// small beside the rows.  At most one a row.
-inline int norm_parts(long rows, int cols, int cus) {
-  const long most = (cols <= 1024 ? 8l : cols <= 4096 ? 4l : 2l) * (cus > 0 ? cus : 256);
+// the weights' gradients: one a CU.  With two the rows flow no faster and the sums are
+// twice as many (add_norm, 8192 rows of 2048 with both vectors 57 us instead of 50;
+// gate_norm, 8192 x 32 heads of 128 72 instead of 67).
+inline int norm_parts(long rows, int cus) {
+  const long most = cus > 0 ? cus : 256;
   return (int)(rows < 1 ? 1 : rows < most ? rows : most);
 }
 
