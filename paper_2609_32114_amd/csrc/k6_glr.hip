@@ -170,25 +170,42 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
   }
 }
 
-constexpr int kStepThreads = 64;
+// ------------------------------------------------------------- single tokens
+// A thread holds four channels of one sequence (one, where D is no multiple of four): bound by
+// the state's way there and back and, for few sequences, by the launch.
+constexpr int kStepThreads = 256;
 
-template <typename T, typename G, bool RAW, bool CONVEX>
-__global__ __launch_bounds__(kStepThreads) void glr_step_kernel(GlrStepArgs a) {
-  const int cols = (a.D + kStepThreads - 1) / kStepThreads;
-  const int n = blockIdx.x / cols, c = blockIdx.x % cols * kStepThreads + threadIdx.x;
-  if (c >= a.D) return;
-  T *h = static_cast<T *>(a.h) + (size_t)n * a.D + c;
-  const int slot = a.slots ? a.slots[n] : n;
-  if (slot < 0 || slot >= a.num_slots) {  // padding entry
-    *h = Elt<T>::from_f32(0.f);
-    return;
+template <typename T, int V> struct __attribute__((packed, aligned(sizeof(T)))) Elems {
+  T v[V];
+};
+
+template <typename T, typename G, bool RAW, bool CONVEX, int V>
+__global__ __launch_bounds__(kStepThreads) void glr_step_kernel(GlrStepArgs a, uint32_t cols, uint32_t items) {
+  for (uint32_t i = blockIdx.x * kStepThreads + threadIdx.x; i < items; i += gridDim.x * kStepThreads) {
+    const uint32_t n = i / cols, c = (i - n * cols) * V;
+    Elems<T, V> *h = reinterpret_cast<Elems<T, V> *>(static_cast<T *>(a.h) + (size_t)n * a.D + c);
+    const auto g = *reinterpret_cast<const Elems<G, V> *>(static_cast<const G *>(a.g) + (size_t)n * a.gs + c);
+    const auto x = *reinterpret_cast<const Elems<T, V> *>(static_cast<const T *>(a.x) + (size_t)n * a.xs + c);
+    const int slot = a.slots ? a.slots[n] : (int)n;
+    Elems<T, V> out;
+    if (slot < 0 || slot >= a.num_slots) {  // padding entry
+#pragma unroll
+      for (int e = 0; e < V; ++e) out.v[e] = Elt<T>::from_f32(0.f);
+      *h = out;
+      continue;
+    }
+    Elems<float, V> *row = reinterpret_cast<Elems<float, V> *>(a.state + (size_t)slot * a.D + c);
+    Elems<float, V> s = *row;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const Gate k = glr_gate<RAW>(Elt<G>::to_f32(g.v[e]));
+      const float u = Elt<T>::to_f32(x.v[e]);
+      s.v[e] = k.a * s.v[e] + (CONVEX ? k.forget * u : u);
+      out.v[e] = Elt<T>::from_f32(s.v[e]);
+    }
+    *row = s;
+    *h = out;
   }
-  float *s = a.state + (size_t)slot * a.D + c;
-  const Gate k = glr_gate<RAW>(Elt<G>::to_f32(static_cast<const G *>(a.g)[(size_t)n * a.gs + c]));
-  const float u = Elt<T>::to_f32(static_cast<const T *>(a.x)[(size_t)n * a.xs + c]);
-  const float r = k.a * *s + (CONVEX ? k.forget * u : u);
-  *s = r;
-  *h = Elt<T>::from_f32(r);
 }
 
 hipError_t launch_glr_setup(const GlrArgs &a, size_t words, uint32_t cols, hipStream_t s) {
@@ -221,10 +238,15 @@ template <typename T, typename G> struct Forward {
   }
 };
 template <typename T, typename G> struct Step {
-  template <bool RAW, bool CONVEX> static hipError_t go(const GlrStepArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)((size_t)a.N * ((a.D + kStepThreads - 1) / kStepThreads)));
-    hipLaunchKernelGGL((glr_step_kernel<T, G, RAW, CONVEX>), grid, dim3(kStepThreads), 0, s, a);
+  template <bool RAW, bool CONVEX, int V> static hipError_t wide(const GlrStepArgs &a, hipStream_t s) {
+    const uint32_t cols = (uint32_t)a.D / V, items = cols * (uint32_t)a.N;  // N x D < 2^31
+    const uint32_t blocks = (items + kStepThreads - 1) / kStepThreads;
+    hipLaunchKernelGGL((glr_step_kernel<T, G, RAW, CONVEX, V>), dim3(blocks < 1u << 20 ? blocks : 1u << 20),
+                       dim3(kStepThreads), 0, s, a, cols, items);
     return hipGetLastError();
+  }
+  template <bool RAW, bool CONVEX> static hipError_t go(const GlrStepArgs &a, hipStream_t s) {
+    return a.D % 4 == 0 ? wide<RAW, CONVEX, 4>(a, s) : wide<RAW, CONVEX, 1>(a, s);
   }
 };
 

@@ -20,14 +20,20 @@ import torch
 from . import (HAGDN_BF16, HAGDN_F32, HagdnError, _check_buffer, _err, _ptr, _raw_stream,
                load_library)
 
+_F32 = torch.float32
 _ACTIVATIONS = {"silu": 0, "sigmoid": 1}
 _CODES = {torch.bfloat16: HAGDN_BF16, torch.float32: HAGDN_F32}
 
 
-def _call(fn, *args):
-    rc = fn(*args)
+def _check(rc):
     if rc != 0:
         raise HagdnError(rc, _err(load_library()))
+
+
+def _alike(t, shape, di):
+    """Whether a tensor is contiguous, of this shape and on this GPU: the common case of
+    every check below, told without building its message."""
+    return t.get_device() == di and t.shape == shape and t.is_contiguous() and di >= 0
 
 
 def _code(name, t, like=None):
@@ -43,12 +49,12 @@ def _code(name, t, like=None):
 def _rows(name, t, shape, di):
     """Row stride in elements of a tensor whose rows (all but the first dimension)
     are contiguous; checks its device and shape."""
+    if _alike(t, shape, di):
+        return t.stride(0)
     if t.get_device() != di or di < 0:
         raise ValueError(f"{name} must be on the GPU of the call's first tensor")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
-    if t.is_contiguous():
-        return t.stride(0)
     inner = 1
     for size, stride in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
         if size != 1 and stride != inner:
@@ -58,7 +64,7 @@ def _rows(name, t, shape, di):
 
 
 def _vector(name, t, size, device):
-    if t is not None:
+    if t is not None and not (t.dtype is _F32 and _alike(t, (size,), device.index)):
         _check_buffer(name, t, device, torch.float32, (size,))
 
 
@@ -78,6 +84,14 @@ def _output(name, t, shape, dtype, device):
     if t is None:
         return torch.empty(shape, dtype=dtype, device=device)
     _check_buffer(name, t, device, dtype, shape)
+    return t
+
+
+def _like(name, t, x):
+    """A contiguous output of x's shape and type: t, or a new one."""
+    if t is None:
+        return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check_buffer(name, t, x.device, x.dtype, x.shape)
     return t
 
 
@@ -117,12 +131,13 @@ def glr_prefill(x, g, initial_state=None, cu_seqlens=None, convex=False, preproc
     N, cu = _sequences(cu_seqlens, di)
     if initial_state is not None:
         _check_buffer("initial_state", initial_state, dev, torch.float32, (N, D))
-    h = _output("out", out, shape, x.dtype, dev)
+    h = _like("out", out, x)
     final = _output("final_out", final_out, (N, D), torch.float32, dev) if output_final_state else None
     saved = torch.empty(((T + 127) // 128, D), dtype=torch.float32, device=dev) if output_checkpoints else None
     ws = _workspace(workspace, glr_workspace_size(T, D) if workspace is None else 0, dev)
-    _call(lib.glr_prefill, x.data_ptr(), xs, g.data_ptr(), gs, _ptr(initial_state), cu, N, T, D, dt, gt, int(convex),
-          int(preprocess), h.data_ptr(), _ptr(final), _ptr(saved), ws.data_ptr(), _bytes(ws), _raw_stream(di))
+    _check(lib.glr_prefill(
+        x.data_ptr(), xs, g.data_ptr(), gs, _ptr(initial_state), cu, N, T, D, dt, gt, int(convex), int(preprocess),
+        h.data_ptr(), _ptr(final), _ptr(saved), ws.data_ptr(), _bytes(ws), _raw_stream(di)))
     return (h, final, saved) if output_checkpoints else (h, final)
 
 
@@ -145,13 +160,13 @@ def glr_backward(dh, x, g, checkpoints, initial_state=None, dfinal=None, cu_seql
     for name, t in (("initial_state", initial_state), ("dfinal", dfinal)):
         if t is not None:
             _check_buffer(name, t, dev, torch.float32, (N, D))
-    dx = torch.empty(shape, dtype=x.dtype, device=dev)
-    dg = torch.empty(shape, dtype=g.dtype, device=dev)
+    dx, dg = _like("dx", None, x), _like("dg", None, g)
     ds0 = torch.empty((N, D), dtype=torch.float32, device=dev) if initial_state is not None else None
     ws = _workspace(workspace, glr_workspace_size(T, D) if workspace is None else 0, dev)
-    _call(lib.glr_backward, dh.data_ptr(), dhs, x.data_ptr(), xs, g.data_ptr(), gs, checkpoints.data_ptr(),
-          _ptr(initial_state), _ptr(dfinal), cu, N, T, D, dt, gt, int(convex), int(preprocess), dx.data_ptr(),
-          dg.data_ptr(), _ptr(ds0), ws.data_ptr(), _bytes(ws), _raw_stream(di))
+    _check(lib.glr_backward(
+        dh.data_ptr(), dhs, x.data_ptr(), xs, g.data_ptr(), gs, checkpoints.data_ptr(), _ptr(initial_state),
+        _ptr(dfinal), cu, N, T, D, dt, gt, int(convex), int(preprocess), dx.data_ptr(), dg.data_ptr(), _ptr(ds0),
+        ws.data_ptr(), _bytes(ws), _raw_stream(di)))
     return dx, dg, ds0
 
 
@@ -168,15 +183,17 @@ def glr_decode(x, g, state, slots=None, convex=False, preprocess=0, out=None):
     dt, gt = _code("x", x), _code("g", g, x)
     if state.dim() != 2:
         raise ValueError(f"state must be [slots, {D}]")
-    _check_buffer("state", state, dev, torch.float32, (state.shape[0], D))
+    if not (state.dtype is _F32 and _alike(state, (state.shape[0], D), di)):
+        _check_buffer("state", state, dev, _F32, (state.shape[0], D))
     if slots is None:
         if state.shape[0] < N:
             raise ValueError("without slots the state pool needs one state per sequence")
     else:
         _check_buffer("slots", slots, dev, torch.int32, (N,))
-    h = _output("out", out, shape, x.dtype, dev)
-    _call(lib.glr_decode, x.data_ptr(), xs, g.data_ptr(), gs, state.data_ptr(), _ptr(slots), state.shape[0], N, D, dt,
-          gt, int(convex), int(preprocess), h.data_ptr(), _raw_stream(di))
+    h = _like("out", out, x)
+    _check(lib.glr_decode(
+        x.data_ptr(), xs, g.data_ptr(), gs, state.data_ptr(), _ptr(slots), state.shape[0], N, D, dt, gt, int(convex),
+        int(preprocess), h.data_ptr(), _raw_stream(di)))
     return h
 
 
@@ -205,13 +222,17 @@ def add_norm(x, weight, residual=None, scale=1.0, post_weight=None, eps=1e-6, ou
         rs, rt, rdtype = _rows("residual", residual, shape, di), _code("residual", residual, x), residual.dtype
     elif residual_out is not None:
         rt, rdtype = _code("residual_out", residual_out, x), residual_out.dtype
-    _check_buffer("weight", weight, dev, torch.float32, (D,))
+    _vector("weight", weight, D, dev)
     _vector("post_weight", post_weight, D, dev)
     number, vector = _scale(scale, D, dev)
-    y = _output("out", out, shape, x.dtype, dev)
-    r = _output("residual_out", residual_out, shape, rdtype, dev)
-    _call(lib.hagdn_add_norm, x.data_ptr(), xs, _ptr(residual), rs, weight.data_ptr(), _ptr(post_weight), _ptr(vector),
-          number, eps, T, D, dt, rt, y.data_ptr(), r.data_ptr(), _raw_stream(di))
+    y = _like("out", out, x)
+    if residual_out is None and residual is not None:
+        r = _like("residual_out", None, residual)
+    else:
+        r = _output("residual_out", residual_out, shape, rdtype, dev)
+    _check(lib.hagdn_add_norm(
+        x.data_ptr(), xs, _ptr(residual), rs, weight.data_ptr(), _ptr(post_weight), _ptr(vector), number, eps, T, D,
+        dt, rt, y.data_ptr(), r.data_ptr(), _raw_stream(di)))
     return y, r
 
 
@@ -227,7 +248,7 @@ def add_norm_backward(dy, res, weight, dresidual=None, x=None, scale=1.0, post_w
     T, D = shape = dy.shape
     number, vector = _scale(scale, D, dev)
     _vector("post_weight", post_weight, D, dev)
-    _check_buffer("weight", weight, dev, torch.float32, (D,))
+    _vector("weight", weight, D, dev)
     dys, rs, dt, rt = _rows("dy", dy, shape, di), _rows("res", res, shape, di), _code("dy", dy), _code("res", res, dy)
     drs = xs = 0
     if dresidual is not None:
@@ -241,17 +262,16 @@ def add_norm_backward(dy, res, weight, dresidual=None, x=None, scale=1.0, post_w
         if x.dtype != dy.dtype:
             raise TypeError(f"x must be {dy.dtype} (got {x.dtype})")
         xs = _rows("x", x, shape, di)
-    dx = torch.empty(shape, dtype=dy.dtype, device=dev)
-    dres = torch.empty(shape, dtype=res.dtype, device=dev)
+    dx, dres = _like("dx", None, dy), _like("dres", None, res)
     grads = torch.empty((1 + (vector is not None) + (post_weight is not None), D), dtype=torch.float32, device=dev)
     dw, dscale = grads[0], grads[1] if vector is not None else None
     dpost = grads[-1] if post_weight is not None else None
     ws = _workspace(workspace, lib.hagdn_add_norm_workspace_size(T, D, vector is not None, post_weight is not None)
                     if workspace is None else 0, dev)
-    _call(lib.hagdn_add_norm_backward, dy.data_ptr(), dys, _ptr(dresidual), drs, res.data_ptr(), rs,
-          x.data_ptr() if reads_x else None, xs, weight.data_ptr(), _ptr(post_weight), _ptr(vector), number, eps, T, D,
-          dt, rt, dx.data_ptr(), dres.data_ptr(), dw.data_ptr(), _ptr(dscale), _ptr(dpost), ws.data_ptr(), _bytes(ws),
-          _raw_stream(di))
+    _check(lib.hagdn_add_norm_backward(
+        dy.data_ptr(), dys, _ptr(dresidual), drs, res.data_ptr(), rs, x.data_ptr() if reads_x else None, xs,
+        weight.data_ptr(), _ptr(post_weight), _ptr(vector), number, eps, T, D, dt, rt, dx.data_ptr(), dres.data_ptr(),
+        dw.data_ptr(), _ptr(dscale), _ptr(dpost), ws.data_ptr(), _bytes(ws), _raw_stream(di)))
     return dx, dres, dw, dscale, dpost
 
 
@@ -272,10 +292,11 @@ def gate_norm(o, z, weight, activation="silu", eps=1e-6, out=None):
     os_, zs, dt = _rows("o", o, shape, di), _rows("z", z, shape, di), _code("o", o)
     if z.dtype != o.dtype:
         raise TypeError(f"z must be {o.dtype} (got {z.dtype})")
-    _check_buffer("weight", weight, dev, torch.float32, (d,))
-    y = _output("out", out, shape, o.dtype, dev)
-    _call(lib.hagdn_gate_norm, o.data_ptr(), os_, z.data_ptr(), zs, weight.data_ptr(), eps, T, H, d, dt,
-          _activation(activation), y.data_ptr(), _raw_stream(di))
+    _vector("weight", weight, d, dev)
+    y = _like("out", out, o)
+    _check(lib.hagdn_gate_norm(
+        o.data_ptr(), os_, z.data_ptr(), zs, weight.data_ptr(), eps, T, H, d, dt, _activation(activation),
+        y.data_ptr(), _raw_stream(di)))
     return y
 
 
@@ -291,11 +312,12 @@ def gate_norm_backward(dy, o, z, weight, activation="silu", eps=1e-6, workspace=
     for name, t in (("z", z), ("dy", dy)):
         if t.dtype != o.dtype:
             raise TypeError(f"{name} must be {o.dtype} (got {t.dtype})")
-    _check_buffer("weight", weight, dev, torch.float32, (d,))
+    _vector("weight", weight, d, dev)
     act = _activation(activation)
-    do, dz = torch.empty(shape, dtype=o.dtype, device=dev), torch.empty(shape, dtype=o.dtype, device=dev)
+    do, dz = _like("do", None, o), _like("dz", None, z)
     dw = torch.empty(d, dtype=torch.float32, device=dev)
     ws = _workspace(workspace, lib.hagdn_gate_norm_workspace_size(T, H, d) if workspace is None else 0, dev)
-    _call(lib.hagdn_gate_norm_backward, dy.data_ptr(), dys, o.data_ptr(), os_, z.data_ptr(), zs, weight.data_ptr(), eps,
-          T, H, d, dt, act, do.data_ptr(), dz.data_ptr(), dw.data_ptr(), ws.data_ptr(), _bytes(ws), _raw_stream(di))
+    _check(lib.hagdn_gate_norm_backward(
+        dy.data_ptr(), dys, o.data_ptr(), os_, z.data_ptr(), zs, weight.data_ptr(), eps, T, H, d, dt, act,
+        do.data_ptr(), dz.data_ptr(), dw.data_ptr(), ws.data_ptr(), _bytes(ws), _raw_stream(di)))
     return do, dz, dw
