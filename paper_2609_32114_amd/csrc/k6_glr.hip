@@ -231,9 +231,14 @@ template <typename T, typename G> struct Forward {
     return hipGetLastError();
   }
   template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
+    // Tokens a wave: as few tiles as keep the chain of states short, but as many as there
+    // are CUs.  Tiles of 128 tokens instead of 256, us a call: 777 x 1280 11.2 and 14.6,
+    // 2048 x 2048 fp32 17.4 and 20.4, 8192 x 256 17.9 and 19.1; but 4096 x 2048 (512 tiles
+    // of 256) 25.9 and 23.2, 32768 x 2048 157 and 119, and 50000 x 64, whose 196 tiles of
+    // 256 all wait for each other, 54 and 34.
     const long items = ((long)a.T + 255) / 256 * (((long)a.D + 63) / 64);
     if (a.T <= 64) return tiled<RAW, CONVEX, 8>(a, s);
-    if (a.T <= 128 || (a.T > 256 && 2 * items <= a.cus)) return tiled<RAW, CONVEX, 16>(a, s);
+    if (a.T <= 128 || (a.T > 256 && a.T <= 8192 && items <= a.cus)) return tiled<RAW, CONVEX, 16>(a, s);
     return tiled<RAW, CONVEX, 32>(a, s);
   }
 };
