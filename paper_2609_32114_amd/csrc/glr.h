@@ -174,7 +174,7 @@ template <int L> __device__ __forceinline__ Marks<L> find_marks(const Offsets &c
 // out[n] = in[n] (null: 0) for the sequences without tokens (all of them if !ok), in
 // channel c.
 __device__ __forceinline__ void pass_empty(const int32_t *cu, int N, int T, bool ok, const float *in, float *out, int D,
-                                           uint32_t c, bool mine) {
+                                           uint32_t c) {
   if (!out) return;
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = lane_id();
   for (long base = (long)wave * 64; base < N; base += waves * 64) {
@@ -182,7 +182,7 @@ __device__ __forceinline__ void pass_empty(const int32_t *cu, int N, int T, bool
     const bool empty = n < N && (!ok || (cu ? cu[n] == cu[n + 1] : T == 0));
     for (uint64_t left = __ballot(empty); left; left &= left - 1) {
       const size_t at = (size_t)(base + __builtin_ctzll(left)) * D + c;
-      if (mine) out[at] = in ? in[at] : 0.f;
+      if (c < (uint32_t)D) out[at] = in ? in[at] : 0.f;
     }
   }
 }
@@ -249,7 +249,9 @@ __device__ __forceinline__ float look_back(uint64_t *words, int D, uint32_t c, l
   return 0.f;
 }
 
-// The next tile of a column of 64 channels, in the order in which they are taken.
+// The next tile of a column of 64 channels.  A tile is worked on as soon as it is taken:
+// workgroups that take one ahead, to hide the counter's latency, hold up those that took
+// later ones (packed batch of eight, 34800 x 2048 tokens, 147 us instead of 131).
 __device__ __forceinline__ uint32_t take_tile(const GlrArgs &a, uint32_t col) {
   return atomicAdd(a.counters + (size_t)col * kGlrCounterStride, 1u);
 }

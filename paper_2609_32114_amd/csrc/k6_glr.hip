@@ -39,22 +39,19 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     ok = glr_seqlens_ok(a.cu, a.N, a.T);
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
   }
-  uint32_t next = 0;  // thread 0: the tile of the next turn
-  if (tiles > 1 && threadIdx.x == 0) next = take_tile(a, blockIdx.x % cols);
+  if (!ok || a.T == 0) {  // no tokens: the states pass through
+    for (uint32_t col = blockIdx.x; col < cols; col += gridDim.x)
+      pass_empty(a.cu, a.N, a.T, ok, a.s0, a.s_final, a.D, col * 64 + lane);
+    return;
+  }
   for (uint32_t turn = blockIdx.x; turn < tiles * cols; turn += gridDim.x) {
-    if (threadIdx.x == 0) sNext = next;
+    const uint32_t col = __builtin_amdgcn_readfirstlane(turn % cols), at = col * 64 + lane;
+    if (threadIdx.x == 0) sNext = tiles > 1 ? take_tile(a, col) : 0;
     __syncthreads();
     const uint32_t tile = __builtin_amdgcn_readfirstlane(sNext);
-    const uint32_t at = __builtin_amdgcn_readfirstlane(turn % cols) * 64 + lane;
     const bool mine = at < (uint32_t)a.D;
     const uint32_t c = mine ? at : 0;  // lanes past the last channel compute the first one's, and store nothing
-    if (tile == 0) pass_empty(a.cu, a.N, a.T, ok, a.s0, a.s_final, a.D, c, mine);
-    const uint32_t after = turn + gridDim.x;
-    if (tiles > 1 && threadIdx.x == 0 && after < tiles * cols) next = take_tile(a, after % cols);
-    if (!ok || a.T == 0) {
-      __syncthreads();  // sNext is written again in the next turn
-      continue;
-    }
+    if (tile == 0) pass_empty(a.cu, a.N, a.T, ok, a.s0, a.s_final, a.D, at);
 
     // the wave's tokens; rows past the end are loaded from the last one
     const long t0 = (long)tile * (W * L) + wave * L;
