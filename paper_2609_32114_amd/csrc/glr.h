@@ -61,9 +61,9 @@ template <bool RAW> __device__ __forceinline__ Gate glr_gate(float g) {
 }
 
 // ------------------------------------------------------------------- row access
-// Where element c of a row lies, for accesses whose address is a uniform row (a pair of
-// scalar registers) plus a lane's 32-bit offset.  The empty statements keep the compiler
-// from adding the two first and holding every row's sum in a pair of vector registers.
+// Accesses have a uniform row (a pair of scalar registers) and a lane's 32-bit offset as
+// their address.  The empty statements keep the compiler from adding the two first and
+// holding every row's sum in a pair of vector registers.
 #ifdef __HIP_DEVICE_COMPILE__
 #define HAGDN_GLOBAL __attribute__((address_space(1)))
 #define HAGDN_LDS __attribute__((address_space(3)))
@@ -75,6 +75,7 @@ template <bool RAW> __device__ __forceinline__ Gate glr_gate(float g) {
 #define HAGDN_SCALAR(p)
 #define HAGDN_VECTOR(v)
 #endif
+// Where element c of a row lies.
 template <typename T> __device__ __forceinline__ HAGDN_GLOBAL T *in_row(T *row, uint32_t c) {
   HAGDN_GLOBAL char *p = (HAGDN_GLOBAL char *)row;
   uint32_t offset = c * (uint32_t)sizeof(T);
@@ -82,6 +83,24 @@ template <typename T> __device__ __forceinline__ HAGDN_GLOBAL T *in_row(T *row, 
   HAGDN_VECTOR(offset);
   return (HAGDN_GLOBAL T *)(p + offset);
 }
+// Element c of one row after another, `stride` elements apart (which may be negative).
+template <typename T> struct Rows {
+  HAGDN_GLOBAL char *p;
+  long step;
+  uint32_t offset;
+  __device__ Rows(T *row, long stride, uint32_t c)
+      : p((HAGDN_GLOBAL char *)row), step(stride * (long)sizeof(T)), offset(c * (uint32_t)sizeof(T)) {
+    HAGDN_SCALAR(p);
+  }
+  __device__ HAGDN_GLOBAL T *here() {
+    HAGDN_VECTOR(offset);
+    return (HAGDN_GLOBAL T *)(p + offset);
+  }
+  __device__ void advance() {
+    p += step;
+    HAGDN_SCALAR(p);
+  }
+};
 
 // --------------------------------------------------------------- sequences' ends
 // Whether cu[0 .. N] are the offsets of N sequences over T tokens; every thread of

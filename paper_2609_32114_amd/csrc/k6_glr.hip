@@ -136,12 +136,12 @@ __global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs 
     for (int w = 0; w < wave; ++w) s = sReset[w] ? sB[w][lane] : sA[w][lane] * s + sB[w][lane];
     if (a.ckpt && t0 % kGlrGroup == 0 && count > 0 && mine) *in_row(a.ckpt + (size_t)(t0 / kGlrGroup) * a.D, c) = s;
     if ((m.first | m.last) == 0 && count == L) {
-      T *ph = static_cast<T *>(a.h) + (size_t)t0 * a.D;
+      Rows<T> rh(static_cast<T *>(a.h) + (size_t)t0 * a.D, a.D, c);
 #pragma unroll
       for (int i = 0; i < L; ++i) {
         s = k[i] * s + b[i];
-        if (mine) __builtin_nontemporal_store(Elt<T>::from_f32(s), in_row(ph, c));
-        ph += a.D;
+        if (mine) __builtin_nontemporal_store(Elt<T>::from_f32(s), rh.here());
+        rh.advance();
       }
       __syncthreads();  // LDS is used again in the next turn
       continue;

@@ -50,16 +50,27 @@ __global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArg
     T x[L], y[L];  // y: dh
     G g[L];
     const long row = min(t0, (long)a.T - 1);
-    const T *px = static_cast<const T *>(a.x) + row * a.xs, *py = static_cast<const T *>(a.dh) + row * a.dhs;
-    const G *pg = static_cast<const G *>(a.g) + row * a.gs;
+    Rows<const T> rx(static_cast<const T *>(a.x) + row * a.xs, a.xs, c);
+    Rows<const G> rg(static_cast<const G *>(a.g) + row * a.gs, a.gs, c);
+    Rows<const T> ry(static_cast<const T *>(a.dh) + row * a.dhs, a.dhs, c);
+    if (count == L) {
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      x[i] = __builtin_nontemporal_load(in_row(px, c));
-      g[i] = __builtin_nontemporal_load(in_row(pg, c));
-      y[i] = __builtin_nontemporal_load(in_row(py, c));
-      px += i + 1 < count ? a.xs : 0;
-      pg += i + 1 < count ? a.gs : 0;
-      py += i + 1 < count ? a.dhs : 0;
+      for (int i = 0; i < L; ++i) {
+        x[i] = __builtin_nontemporal_load(rx.here());
+        g[i] = __builtin_nontemporal_load(rg.here());
+        y[i] = __builtin_nontemporal_load(ry.here());
+        rx.advance();
+        rg.advance();
+        ry.advance();
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+        x[i] = *rx.here();
+        g[i] = *rg.here();
+        y[i] = *ry.here();
+        if (i + 1 < count) rx.advance(), rg.advance(), ry.advance();
+      }
     }
     float s = *in_row(a.ckpt + (size_t)tile * a.D, c);
     const Marks<L> m = find_marks<L>(cu, a.T, t0, sIds[wave]);
@@ -151,20 +162,29 @@ __global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArg
       u[i] = CONVEX ? s - u[i] : s;
       s = h;
     };
-    auto grads = [&](int i) {
+    auto grads = [&](int i, T &dx, G &dg) {
       const float di = d[i] + e;
       e = k[i] * di;
-      if (!mine) return;
-      T *dx = static_cast<T *>(a.dx) + (size_t)(t0 + i) * a.D;
-      G *dg = static_cast<G *>(a.dg) + (size_t)(t0 + i) * a.D;
-      __builtin_nontemporal_store(Elt<T>::from_f32(CONVEX ? f[i] * di : di), in_row(dx, c));
-      __builtin_nontemporal_store(Elt<G>::from_f32(RAW ? -f[i] * (e * u[i]) : e * u[i]), in_row(dg, c));
+      dx = Elt<T>::from_f32(CONVEX ? f[i] * di : di);
+      dg = Elt<G>::from_f32(RAW ? -f[i] * (e * u[i]) : e * u[i]);
     };
     if ((m.first | m.last) == 0 && count == L) {
 #pragma unroll
       for (int i = 0; i < L; ++i) state(i);
+      Rows<T> rdx(static_cast<T *>(a.dx) + (size_t)(t0 + L - 1) * a.D, -(long)a.D, c);
+      Rows<G> rdg(static_cast<G *>(a.dg) + (size_t)(t0 + L - 1) * a.D, -(long)a.D, c);
 #pragma unroll
-      for (int i = L - 1; i >= 0; --i) grads(i);
+      for (int i = L - 1; i >= 0; --i) {
+        T dx;
+        G dg;
+        grads(i, dx, dg);
+        if (mine) {
+          __builtin_nontemporal_store(dx, rdx.here());
+          __builtin_nontemporal_store(dg, rdg.here());
+        }
+        rdx.advance();
+        rdg.advance();
+      }
     } else {
       for (int lo = 0; lo < count;) {  // from one sequence's first token to the next one's
         if (m.first >> lo & 1) {
@@ -187,7 +207,15 @@ __global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArg
         const int lo = sooner ? 32 - __builtin_clz(sooner) : 0;
 #pragma unroll
         for (int i = L - 1; i >= 0; --i)
-          if (i >= lo && i < hi) grads(i);
+          if (i >= lo && i < hi) {
+            T dx;
+            G dg;
+            grads(i, dx, dg);
+            if (mine) {
+              *in_row(static_cast<T *>(a.dx) + (size_t)(t0 + i) * a.D, c) = dx;
+              *in_row(static_cast<G *>(a.dg) + (size_t)(t0 + i) * a.D, c) = dg;
+            }
+          }
         if ((m.first >> lo & 1) && a.ds0 && mine) *in_row(a.ds0 + (size_t)m.starts(lo) * a.D, c) = e;
         hi = lo;
       }
