@@ -287,6 +287,10 @@ hipError_t glr_dispatch(const A &a, const GlrForm &f, hipStream_t s) {
   return f.gate_bf16 ? forms(Launch<bf16_t, bf16_t>()) : forms(Launch<bf16_t, float>());
 }
 
+// Compute units, and a call's tiles of `tokens` tokens x 64 channels.
+inline long glr_cus(const GlrArgs &a) { return a.cus > 0 ? a.cus : 256; }
+inline long glr_tiles(const GlrArgs &a, long tokens) { return ((long)a.T + tokens - 1) / tokens * (((long)a.D + 63) / 64); }
+
 // Clears the words and the counter, checks the offsets, writes the status.
 hipError_t launch_glr_setup(const GlrArgs &, size_t words, uint32_t cols, hipStream_t);
 

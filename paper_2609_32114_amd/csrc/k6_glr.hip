@@ -2,14 +2,12 @@
 // channel over packed sequences (a_t = e^g_t, w_t = 1 or 1 - a_t), and its step for
 // single tokens.
 //
-// The forward pass is the scan of glr.h over tiles of 256 tokens x 64 channels:
-// eight waves of 32 tokens, a lane to a channel.  It is bound by HBM:
+// The forward pass is the scan of glr.h over tiles of 64 to 512 tokens x 64
+// channels, in long calls eight waves of 32 tokens, a lane to a channel.  It is bound by HBM:
 // x and g are read once and h written once, for some 15 operations an element.
 #include "glr.h"
 
 namespace hagdn {
-
-constexpr int kGlrWaves = 8;
 
 // Empties `words` words and clears the columns' counters, checks the sequence offsets
 // (workgroup 0) and writes the status.
@@ -23,9 +21,8 @@ __global__ __launch_bounds__(256) void glr_setup_kernel(GlrArgs a, size_t words,
   }
 }
 
-template <typename T, typename G, bool RAW, bool CONVEX, int L>
-__global__ __launch_bounds__(kGlrWaves * 64, 4) void glr_forward_kernel(GlrArgs a, uint32_t tiles, uint32_t cols) {
-  constexpr int W = kGlrWaves;
+template <typename T, typename G, bool RAW, bool CONVEX, int L, int W>
+__global__ __launch_bounds__(W * 64, 4) void glr_forward_kernel(GlrArgs a, uint32_t tiles, uint32_t cols) {
   __shared__ float sA[W][64], sB[W][64], sIn[64];
   __shared__ int sIds[W][2 * L], sReset[W];
   __shared__ int32_t sCu[kLdsOffsets + 1];
@@ -213,32 +210,36 @@ hipError_t launch_glr_setup(const GlrArgs &a, size_t words, uint32_t cols, hipSt
 }
 
 template <typename T, typename G> struct Forward {
-  template <bool RAW, bool CONVEX, int L> static hipError_t tiled(const GlrArgs &a, hipStream_t s) {
-    constexpr int kTile = kGlrWaves * L;
+  template <bool RAW, bool CONVEX, int L, int W> static hipError_t tiled(const GlrArgs &a, hipStream_t s) {
+    constexpr int kTile = W * L;
     const long tiles = a.T > 0 ? ((long)a.T + kTile - 1) / kTile : 1, cols = ((long)a.D + 63) / 64;
     if (tiles * cols > 0xffff0000l) return hipErrorInvalidValue;  // the turns' range
     if (tiles > 1) {
       const hipError_t e = launch_glr_setup(a, (size_t)tiles * a.D, (uint32_t)cols, s);
       if (e != hipSuccess) return e;
     }
-    const long resident = 2l * (a.cus > 0 ? a.cus : 256);
+    const long resident = 16 / W * glr_cus(a);  // 16 waves a CU
     const unsigned grid = (unsigned)(tiles * cols < resident ? tiles * cols : resident);
-    hipLaunchKernelGGL((glr_forward_kernel<T, G, RAW, CONVEX, L>), dim3(grid), dim3(kGlrWaves * 64), 0, s, a,
-                       (uint32_t)tiles, (uint32_t)cols);
+    hipLaunchKernelGGL((glr_forward_kernel<T, G, RAW, CONVEX, L, W>), dim3(grid), dim3(W * 64), 0, s, a, (uint32_t)tiles,
+                       (uint32_t)cols);
     return hipGetLastError();
   }
+  // Up to 256 tokens a call is one tile, which needs no setup kernel and a launch less (512
+  // in one tile of 16 x 32 take longer than the setup: 400 x 2048 14.7 us and 11.2).
+  // Beyond, few tiles keep the chain of states short, but there should be as many as CUs.
+  // Tiles of 128 tokens instead of 256, us a call: 777 x 1280 11.2 and 14.6, 2048 x 2048
+  // fp32 17.4 and 20.4, 8192 x 256 17.9 and 19.1; but 4096 x 2048 (512 tiles of 256) 25.9
+  // and 23.2, 32768 x 2048 157 and 119.  Where a long call has few channels its tiles all
+  // wait for each other: 50000 x 64 in tiles of 128, 256 and 512 54, 34 and 27.
   template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
-    // Tokens a wave: as few tiles as keep the chain of states short, but as many as there
-    // are CUs.  Tiles of 128 tokens instead of 256, us a call: 777 x 1280 11.2 and 14.6,
-    // 2048 x 2048 fp32 17.4 and 20.4, 8192 x 256 17.9 and 19.1; but 4096 x 2048 (512 tiles
-    // of 256) 25.9 and 23.2, 32768 x 2048 157 and 119, and 50000 x 64, whose 196 tiles of
-    // 256 all wait for each other, 54 and 34.
-    const long items = ((long)a.T + 255) / 256 * (((long)a.D + 63) / 64);
-    if (a.T <= 64) return tiled<RAW, CONVEX, 8>(a, s);
-    if (a.T <= 128 || (a.T > 256 && a.T <= 8192 && items <= a.cus)) return tiled<RAW, CONVEX, 16>(a, s);
-    return tiled<RAW, CONVEX, 32>(a, s);
+    if (a.T <= 64) return tiled<RAW, CONVEX, 8, 8>(a, s);
+    if (a.T <= 128) return tiled<RAW, CONVEX, 16, 8>(a, s);
+    if (a.T <= 256) return tiled<RAW, CONVEX, 16, 16>(a, s);
+    if (glr_tiles(a, 256) > glr_cus(a)) return tiled<RAW, CONVEX, 32, 8>(a, s);
+    return a.T <= 8192 ? tiled<RAW, CONVEX, 16, 8>(a, s) : tiled<RAW, CONVEX, 32, 16>(a, s);
   }
 };
+
 template <typename T, typename G> struct Step {
   template <bool RAW, bool CONVEX, int V> static hipError_t wide(const GlrStepArgs &a, hipStream_t s) {
     const uint32_t cols = (uint32_t)a.D / V, items = cols * (uint32_t)a.N;  // N x D < 2^31

@@ -11,12 +11,9 @@
 
 namespace hagdn {
 
-constexpr int kBackWaves = 8, kBackRun = 16;
-static_assert(kBackWaves * kBackRun == kGlrGroup, "a tile starts at a saved state");
-
-template <typename T, typename G, bool RAW, bool CONVEX>
-__global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArgs a, uint32_t tiles, uint32_t cols) {
-  constexpr int L = kBackRun, W = kBackWaves;
+template <typename T, typename G, bool RAW, bool CONVEX, int L, int W>
+__global__ __launch_bounds__(W * 64, 4) void glr_backward_kernel(GlrArgs a, uint32_t tiles, uint32_t cols) {
+  static_assert(W * L % kGlrGroup == 0, "a tile starts at a saved state");
   __shared__ float sA[W][64], sF[W][64], sR[W][64], sIn[64];
   __shared__ int sIds[W][2 * L], sFirst[W], sLast[W], sEnded;
   __shared__ int32_t sCu[kLdsOffsets + 1];
@@ -45,7 +42,7 @@ __global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArg
     if (tile == 0) pass_empty(a.cu, a.N, a.T, ok, a.dfinal, a.ds0, a.D, at);
 
     // the wave's tokens; rows past the end are loaded from the last one
-    const long t0 = (long)tile * kGlrGroup + wave * L;
+    const long t0 = (long)tile * (W * L) + wave * L;
     const int count = (int)min((long)L, max(0l, (long)a.T - t0));
     T x[L], y[L];  // y: dh
     G g[L];
@@ -72,7 +69,7 @@ __global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArg
         if (i + 1 < count) rx.advance(), rg.advance(), ry.advance();
       }
     }
-    float s = *in_row(a.ckpt + (size_t)tile * a.D, c);
+    float s = *in_row(a.ckpt + (size_t)tile * (W * L / kGlrGroup) * a.D, c);
     const Marks<L> m = find_marks<L>(cu, a.T, t0, sIds[wave]);
     // The last sequence that starts here is the only one to reach past the wave's tokens,
     // the first that ends here the only one to come from before them; its dfinal is read
@@ -225,18 +222,25 @@ __global__ __launch_bounds__(kBackWaves * 64, 4) void glr_backward_kernel(GlrArg
 }
 
 template <typename T, typename G> struct Backward {
-  template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
-    const long tiles = a.T > 0 ? ((long)a.T + kGlrGroup - 1) / kGlrGroup : 1, cols = ((long)a.D + 63) / 64;
+  template <bool RAW, bool CONVEX, int L, int W> static hipError_t tiled(const GlrArgs &a, hipStream_t s) {
+    constexpr int kTile = W * L;
+    const long tiles = a.T > 0 ? ((long)a.T + kTile - 1) / kTile : 1, cols = ((long)a.D + 63) / 64;
     if (tiles * cols > 0xffff0000l) return hipErrorInvalidValue;  // the turns' range
     if (tiles > 1) {
       const hipError_t e = launch_glr_setup(a, (size_t)tiles * a.D, (uint32_t)cols, s);
       if (e != hipSuccess) return e;
     }
-    const long resident = 2l * (a.cus > 0 ? a.cus : 256);
+    const long resident = 16 / W * glr_cus(a);  // 16 waves a CU
     const unsigned grid = (unsigned)(tiles * cols < resident ? tiles * cols : resident);
-    hipLaunchKernelGGL((glr_backward_kernel<T, G, RAW, CONVEX>), dim3(grid), dim3(kBackWaves * 64), 0, s, a, (uint32_t)tiles,
+    hipLaunchKernelGGL((glr_backward_kernel<T, G, RAW, CONVEX, L, W>), dim3(grid), dim3(W * 64), 0, s, a, (uint32_t)tiles,
                        (uint32_t)cols);
     return hipGetLastError();
+  }
+  // Tiles of 128 tokens; of 256 where that makes one tile of a call, and where a long call
+  // has so few channels that its tiles all wait for each other (forward: k6_glr.hip).
+  template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
+    const bool narrow = a.T > 8192 && glr_tiles(a, 128) <= 2 * glr_cus(a);
+    return (a.T > 128 && a.T <= 256) || narrow ? tiled<RAW, CONVEX, 16, 16>(a, s) : tiled<RAW, CONVEX, 16, 8>(a, s);
   }
 };
 

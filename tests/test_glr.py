@@ -120,6 +120,17 @@ def test_widths(D):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lens,D", [((3000, 0, 2500, 1, 700), 704), ((255, 257, 256, 1, 5600), 1001), ((6000,), 768)])
+def test_wide_calls(lens, D):
+    """More tiles of 256 tokens than CUs: the largest tiles, several to a workgroup, with
+    sequences that end on, before and after their boundaries."""
+    for i, (dtype, gate) in enumerate(TYPES):
+        raw, convex = i == 1, i != 0
+        d = make(lens, D, dtype, gate, raw, 40 + i)
+        check(run(d, lens, raw, convex), expected(d, lens, raw, convex), dtype, gate, f"{lens} D={D} {dtype}/{gate}")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [5000, 20011])
 def test_long_sequences(T):
     """Channels that remember thousands of tokens, over many tiles."""
@@ -191,11 +202,12 @@ def test_extreme_gates():
 
 
 @pytest.mark.gpu
-def test_no_value_reaches_another_sequence():
+@pytest.mark.parametrize("lens,D", [((100, 77, 200, 1, 130), 70), ((20, 30, 40), 64), ((3000, 1500, 2000), 705),
+                                    ((6000, 5000), 33)])
+def test_no_value_reaches_another_sequence(lens, D):
     """NaN and infinities in one sequence's tokens, state and gradients leave the
     others' results as they were, bit for bit, wherever the tile boundaries fall."""
     import torch
-    lens, D = (100, 77, 200, 1, 130), 70
     d = make(lens, D, "bf16", "f32", False, 17)
     clean = run(d, lens, False, True)
     starts = np.concatenate([[0], np.cumsum(lens)])
@@ -228,6 +240,32 @@ def test_repeats_bit_for_bit():
         again = run(d, lens, False, False)
         for k, v in first.items():
             assert torch.equal(v, again[k]), k
+
+
+@pytest.mark.gpu
+def test_states_updated_in_place():
+    """s_final written over s0, and ds0 over dfinal, in packed calls whose sequences span
+    tiles, share them and are empty: the same bits as in buffers of their own."""
+    import torch
+    import paper_2609_32114_amd as P
+    lib = P.load_library()
+    for lens, D in (((300, 5, 0, 700, 2, 1, 129), 96), ((40, 3, 1, 20), 64), ((3000, 0, 2500, 1, 700), 705)):
+        T, N = sum(lens), len(lens)
+        d = {k: v.cuda() for k, v in make(lens, D, "bf16", "f32", False, 14).items()}
+        cu, st = offsets(lens), torch.cuda.current_stream().cuda_stream
+        h, final, saved = P.glr_prefill(d["x"], d["g"], initial_state=d["s0"], cu_seqlens=cu, output_checkpoints=True)
+        state = d["s0"].clone()
+        h2, _ = P.glr_prefill(d["x"], d["g"], initial_state=state, cu_seqlens=cu, final_out=state)
+        assert torch.equal(h, h2) and torch.equal(final, state)
+        want = P.glr_backward(d["dh"], d["x"], d["g"], saved, initial_state=d["s0"], dfinal=d["dfinal"], cu_seqlens=cu)
+        grad, dx, dg = d["dfinal"].clone(), torch.empty_like(d["x"]), torch.empty_like(d["g"])
+        ws = torch.empty(P.glr_workspace_size(T, D), dtype=torch.uint8, device="cuda")
+        p = lambda t: t.data_ptr()
+        rc = lib.glr_backward(p(d["dh"]), D, p(d["x"]), D, p(d["g"]), D, p(saved), p(d["s0"]), p(grad), p(cu), N, T, D, 1, 0,
+                              0, 0, p(dx), p(dg), p(grad), p(ws), ws.numel(), st)
+        assert rc == 0
+        for a, b in zip((dx, dg, grad), want):
+            assert torch.equal(a, b)
 
 
 @pytest.mark.gpu
@@ -387,7 +425,7 @@ def test_gradient_against_differences():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [90, 1500])
+@pytest.mark.parametrize("T", [90, 1500, 9001])
 def test_graph_replays(T):
     """Captured calls replayed on new inputs, with eager work between, match eager calls."""
     import torch
