@@ -219,11 +219,17 @@ int kda_decode(const void *q, const void *k, const void *v, const float *g,
  *   convex: 0: w_t = 1;  1: w_t = 1 - a_t (h is a running weighted mean of x).
  *   pre: 0, or HAGDN_PRE_GATE_SOFTPLUS: g holds raw values r and the log-gate is
  *   -softplus(r), that is a_t = 1 / (1 + e^r); dg is then the gradient of r.
- *   A finite g > 0 grows the state.  g = -inf (a = 0) forgets it, unless it is
- *   not finite.  No value of one sequence reaches another.
+ *   g <= 0 is expected; a positive g grows the state, and where the gates of a few
+ *   hundred tokens together pass e^88 results are unspecified.  g = -inf (a = 0)
+ *   forgets the state, unless it is not finite.  No value of one sequence reaches
+ *   another.
+ *   Results repeat bit for bit on one device.
  * Malformed cu_seqlens: no token is processed (h, dx, dg, checkpoints untouched;
  *   s_final receives s0 or zeros, ds0 dfinal or zeros) and hagdn_device_status()
- *   reports HAGDN_DEV_BAD_SEQLENS. */
+ *   reports HAGDN_DEV_BAD_SEQLENS.  HAGDN_DEV_WAIT_TIMEOUT, not expected: a tile of
+ *   tokens gave up waiting, after about a second, for the state of the tiles before
+ *   it; the outputs are invalid.
+ * hagdn_profile_begin/_end do not time these calls. */
 
 /* Bytes of workspace glr_prefill and glr_backward need (0 on invalid sizes). */
 size_t glr_workspace_size(int T_total, int D);

@@ -15,9 +15,10 @@
 //      its tokens again, from registers.
 // Workgroups take the tiles of their 64 channels in order from a counter, so a tile's
 // predecessors have all been taken by workgroups that run or have ended, and every wait
-// ends.  (One counter for the whole call costs some 33 ns a tile: 8192 tiles 272 us.)  The state
-// is always folded forward from a whole one through the same products, so that its
-// bits do not depend on how far back that one was: results repeat exactly.
+// ends.  (One counter for the whole call costs some 33 ns a tile: 8192 tiles 272 us.)
+// The state is always folded forward from a whole one through the same fused products,
+// so that its bits do not depend on how far back that one was: results repeat exactly.
+// A wait is bounded all the same (kLookLimit, HAGDN_DEV_WAIT_TIMEOUT).
 // The backward pass runs the same scan from the last tile to the first.
 #pragma once
 
@@ -248,7 +249,7 @@ __device__ __forceinline__ bool look(uint64_t *words, int D, uint32_t c, long ne
     if (k <= found) {
       const uint32_t high = (uint32_t)(w[k] >> 32);
       const float low = __uint_as_float((uint32_t)w[k]);
-      s = high == kState ? low : __uint_as_float(high) * s + low;
+      s = high == kState ? low : __builtin_fmaf(__uint_as_float(high), s, low);
     }
   return true;
 }

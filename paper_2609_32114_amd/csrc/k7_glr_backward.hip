@@ -3,10 +3,13 @@
 //   d_t = dh_t + e_{t+1},  dx_t = w_t d_t,  d(log a_t) = e_t (h_{t-1} - [convex] x_t).
 //
 // The scan of glr.h runs over e from the last tile to the first, eight waves of 16
-// tokens to a tile.  The states h_{t-1} are not read: each tile forms them again in fp32
-// from the saved state before its first token, in the same registers and with one more
-// map a wave in LDS, which costs three operations an element and saves reading h (and
-// its rounding).  Bound by HBM: x, g and dh are read once, dx and dg written once.
+// tokens to a tile of 64 channels.  The states h_{t-1} are not read: each tile forms them
+// again in fp32 from the saved state before its first token, in the same registers and
+// with one more map a wave in LDS, which costs three operations an element and saves
+// reading h, and its rounding.  Bound by HBM: x, g and dh are read once, dx and dg written
+// once.  32768 tokens x 2048 channels, bf16 with an fp32 gate: 191 us, 4.9 TB/s of the
+// 940 MB that must move; the gate in bf16 181 us (3.7 TB/s: the same two workgroups a CU
+// hold fewer bytes in flight).
 #include "glr.h"
 
 namespace hagdn {
@@ -143,7 +146,7 @@ __global__ __launch_bounds__(W * 64, 4) void glr_backward_kernel(GlrArgs a, uint
       }
       float e = 0.f;
       if (tile + 1 < tiles && !sEnded) e = look_back(a.words, a.D, c, (long)tile + 1, 1, (long)tiles - 1 - tile, a.status);
-      if (pass_on && !reset) publish(words, c, kState, A * e + R);
+      if (pass_on && !reset) publish(words, c, kState, __builtin_fmaf(A, e, R));
       sIn[lane] = e;
     }
     __syncthreads();

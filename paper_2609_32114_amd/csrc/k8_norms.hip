@@ -228,6 +228,8 @@ template <int LANES> constexpr int forward_threads() { return LANES > 256 ? LANE
 template <int LANES> constexpr int backward_threads() { return LANES > 512 ? LANES : 512; }
 
 // ---------------------------------------------------------------------- add_norm
+// One read of x and the stream, one write of y and the stream.  32768 rows of 2048 in
+// bf16 95 us, 5.6 TB/s; 4096 of them 16 us, with the stream in fp32 17; one row 2.1 us.
 template <typename T, typename R, int VE, int LANES, int C>
 __global__ __launch_bounds__(forward_threads<LANES>()) void add_norm_kernel(AddNormArgs a) {
   constexpr int kThreads = forward_threads<LANES>(), kRows = kThreads / LANES;
@@ -300,7 +302,10 @@ __global__ __launch_bounds__(forward_threads<LANES>()) void add_norm_kernel(AddN
 // q is taken from D's three terms' own sums, so that one round of sums serves the row.
 // The operands stay as they were loaded (bf16 ones two to a register), the weights in
 // registers for all of the workgroup's rows.  READS_X: a scale vector or post_weight is
-// there.
+// there.  8192 rows of 2048 in bf16 with both 50 us, 4.0 TB/s, of which 5 the sum over the
+// workgroups; without them 38 us, 4.4 TB/s.  Bound by the row's way through its sums and
+// barrier, which eight waves a CU overlap in part: sixteen, which spill, took 98 us, the
+// operands of two or three rows fetched ahead 51 and 53.
 template <typename T, typename R, int VE, int LANES, int C, bool READS_X>
 __global__ __launch_bounds__(backward_threads<LANES>(), LANES > 512 || !READS_X ? 4 : 2) void add_norm_backward_kernel(
     AddNormArgs a) {
@@ -433,6 +438,7 @@ __device__ __forceinline__ long head_row(uint32_t row, int H, int d, long stride
   return (long)t * stride + (long)(row - t * (uint32_t)H) * d;
 }
 
+// 32768 tokens x 16 heads of 128 in bf16 73 us, 5.5 TB/s.
 template <typename T, int VE, int LANES, int C>
 __global__ __launch_bounds__(forward_threads<LANES>()) void gate_norm_kernel(GateNormArgs a) {
   constexpr int kThreads = forward_threads<LANES>(), kRows = kThreads / LANES;
@@ -474,6 +480,8 @@ __global__ __launch_bounds__(forward_threads<LANES>()) void gate_norm_kernel(Gat
   }
 }
 
+// With n = o r and dn = dy act(z): do = r (w dn - o r^2 mean(o w dn)), dz = dy w n act'(z),
+// dw = sum dn n.  8192 tokens x 32 heads of 128 in bf16 68 us, 4.9 TB/s.
 template <typename T, int VE, int LANES, int C>
 __global__ __launch_bounds__(backward_threads<LANES>(), LANES > 512 || sizeof(T) == 2 ? 4 : 3) void gate_norm_backward_kernel(
     GateNormArgs a) {
