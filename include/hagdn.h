@@ -211,7 +211,7 @@ int kda_decode(const void *q, const void *k, const void *v, const float *g,
  *   Inputs (x, g, dh) may be column slices of a wider matrix: each has a row
  *   stride in ELEMENTS (>= 0; 0 repeats one row), channels being contiguous.
  *   Outputs are contiguous.  Pointers need only their element's alignment
- *   (workspace: 16 bytes).  D >= 1, any.
+ *   (workspace: 16 bytes).  D >= 1, any up to 2^28; N x D below 2^31 - 1.
  *   dtype is the type of x, h, dh and dx; gate_dtype that of g and dg:
  *   HAGDN_F32, or (with dtype bf16 only) HAGDN_BF16.  States, sums and gate
  *   arithmetic are fp32.

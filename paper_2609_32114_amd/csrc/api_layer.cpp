@@ -74,6 +74,7 @@ bool partly_aliased(const void *a, const void *b, size_t bytes) {
 int check_glr(int N, int T, int D, int dtype, int gate_dtype, int convex, int pre) {
   if (T < 0) return fail(HAGDN_EINVAL, "T_total must be >= 0 (got %d)", T);
   if (D < 1) return fail(HAGDN_EINVAL, "D must be >= 1 (got %d)", D);
+  if (D > (1 << 28)) return fail(HAGDN_EUNSUPPORTED, "D > 2^28 unsupported");  // 32-bit offsets within a row
   if ((size_t)N * (size_t)D >= 0x7fffffffu) return fail(HAGDN_EINVAL, "N x D too large (%d x %d)", N, D);
   if (convex != 0 && convex != 1) return fail(HAGDN_EINVAL, "convex must be 0 or 1 (got %d)", convex);
   if (pre & ~hagdn::kPreGateSoftplus) return fail(HAGDN_EINVAL, "unsupported preprocessing flags 0x%x", pre);

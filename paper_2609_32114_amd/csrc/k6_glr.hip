@@ -146,25 +146,23 @@ __global__ __launch_bounds__(W * 64, 4) void glr_forward_kernel(GlrArgs a, uint3
         if (mine) __builtin_nontemporal_store(Elt<T>::from_f32(s), rh.here());
         rh.advance();
       }
-      __syncthreads();  // LDS is used again in the next turn
-      continue;
-    }
-    // from one sequence's first token to the next one's
-    for (int lo = 0; lo < count;) {
-      if (m.first >> lo & 1) {
-        s = lo == start ? s0 : 0.f;
-        if (lo != start && a.s0) s = *in_row(a.s0 + (size_t)m.starts(lo) * a.D, c);
-      }
-      const uint32_t later = m.first & ~((2u << lo) - 1);
-      const int hi = later ? __builtin_ctz(later) : count;
-#pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (i >= lo && i < hi) {
-          s = k[i] * s + b[i];
-          if (mine) *in_row(static_cast<T *>(a.h) + (size_t)(t0 + i) * a.D, c) = Elt<T>::from_f32(s);
+    } else {
+      for (int lo = 0; lo < count;) {  // from one sequence's first token to the next one's
+        if (m.first >> lo & 1) {
+          s = lo == start ? s0 : 0.f;
+          if (lo != start && a.s0) s = *in_row(a.s0 + (size_t)m.starts(lo) * a.D, c);
         }
-      if ((m.last >> (hi - 1) & 1) && a.s_final && mine) *in_row(a.s_final + (size_t)m.ends(hi - 1) * a.D, c) = s;
-      lo = hi;
+        const uint32_t later = m.first & ~((2u << lo) - 1);
+        const int hi = later ? __builtin_ctz(later) : count;
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+          if (i >= lo && i < hi) {
+            s = k[i] * s + b[i];
+            if (mine) *in_row(static_cast<T *>(a.h) + (size_t)(t0 + i) * a.D, c) = Elt<T>::from_f32(s);
+          }
+        if ((m.last >> (hi - 1) & 1) && a.s_final && mine) *in_row(a.s_final + (size_t)m.ends(hi - 1) * a.D, c) = s;
+        lo = hi;
+      }
     }
     __syncthreads();  // LDS is used again in the next turn
   }

@@ -53,7 +53,7 @@ def test_glr_refusals(fn, d):
                  dict(g=None), dict(ws=None), dict(ws=F + 8), dict(cu=None), dict(cu=F + 2), dict(xs=-1), dict(gs=1 << 31),
                  dict(x=F + 1), dict(g=F + 2), dict(N=1 << 20, D=1 << 12), dict(s0=F + 2)):
         assert call(fn, d, **{"wsb": BIG, **over})[0] == EINVAL, over
-    for over in (dict(dtype=2), dict(gate=3), dict(dtype=0, gate=1)):
+    for over in (dict(dtype=2), dict(gate=3), dict(dtype=0, gate=1), dict(N=1, D=(1 << 28) + 1)):
         assert call(fn, d, **{"wsb": BIG, **over})[0] == EUNSUP, over
     outs = dict(h=None) if fn == "glr_prefill" else dict(dx=None)
     assert call(fn, d, **{"wsb": BIG, **outs})[0] == EINVAL

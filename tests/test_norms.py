@@ -165,12 +165,21 @@ def test_add_norm_in_place():
     """The stream updated in place, forward and (as the gradient's buffer) backward."""
     import torch
     import paper_2609_32114_amd as P
-    for D in (100, 2048, 9000):
+    lib = P.load_library()
+    for D in (100, 1001, 2048, 9000):
         d = {k: v.cuda() for k, v in add_inputs(40, D, "bf16", "f32", 5).items()}
         y, r = P.add_norm(d["x"], d["w"], residual=d["res"], scale=0.5)
         stream = d["res"].clone()
         y2, r2 = P.add_norm(d["x"], d["w"], residual=stream, scale=0.5, residual_out=stream)
         assert r2 is stream and torch.equal(r, stream) and torch.equal(y, y2)
+        dx, dres, dw, _, _ = P.add_norm_backward(d["dy"], r, d["w"], dresidual=d["dres"], scale=0.5)
+        grad, dx2, dw2 = d["dres"].clone(), torch.empty_like(dx), torch.empty_like(dw)
+        ws = torch.empty(lib.hagdn_add_norm_workspace_size(40, D, 0, 0), dtype=torch.uint8, device="cuda")
+        p = lambda t: t.data_ptr()
+        rc = lib.hagdn_add_norm_backward(p(d["dy"]), D, p(grad), D, p(r), D, None, 0, p(d["w"]), None, None, 0.5, 1e-6, 40, D,
+                                         1, 0, p(dx2), p(grad), p(dw2), None, None, p(ws), ws.numel(),
+                                         torch.cuda.current_stream().cuda_stream)
+        assert rc == 0 and torch.equal(grad, dres) and torch.equal(dx2, dx) and torch.equal(dw2, dw)
 
 
 @pytest.mark.gpu
@@ -318,6 +327,42 @@ def test_beyond_two_gib():
     do, dz, _ = P.gate_norm_backward(y, o, r.view(T, 16, 128), wh)
     do1, dz1, _ = P.gate_norm_backward(y[-300:].contiguous(), o[-300:].contiguous(), r1.view(300, 16, 128), wh)
     assert torch.equal(do[-300:], do1) and torch.equal(dz[-300:], dz1)
+
+
+@pytest.mark.gpu
+def test_writes_stay_inside():
+    """Guard zones around every output and the workspace stay as they were."""
+    import torch
+    import paper_2609_32114_amd as P
+    lib = P.load_library()
+    st = torch.cuda.current_stream().cuda_stream
+    for T, D in ((3, 1), (5, 7), (9, 130), (4, 1001), (300, 2048), (2, 9001), (2, 16384)):
+        for dtype, res in TYPES:
+            d = {k: v.cuda() for k, v in add_inputs(T, D, dtype, res, 1).items()}
+            code, rcode, e, re = int(dtype == "bf16"), int(res == "bf16"), d["x"].element_size(), d["res"].element_size()
+            raw = {}
+
+            def guarded(name, nbytes):
+                raw[name] = (torch.full((2048 + nbytes + 2048,), 0xA5, dtype=torch.uint8, device="cuda"), nbytes)
+                return raw[name][0].data_ptr() + 2048
+
+            p = lambda k: d[k].data_ptr()
+            assert lib.hagdn_add_norm(p("x"), D, p("res"), D, p("w"), p("post"), p("vec"), 1.0, 1e-6, T, D, code, rcode,
+                                      guarded("y", T * D * e), guarded("r", T * D * re), st) == 0
+            n = lib.hagdn_add_norm_workspace_size(T, D, 1, 1)
+            assert lib.hagdn_add_norm_backward(p("dy"), D, p("dres"), D, p("res"), D, p("x"), D, p("w"), p("post"), p("vec"),
+                                               1.0, 1e-6, T, D, code, rcode, guarded("dx", T * D * e),
+                                               guarded("dres", T * D * re), guarded("dw", 4 * D), guarded("ds", 4 * D),
+                                               guarded("dp", 4 * D), guarded("ws", n), n, st) == 0
+            assert lib.hagdn_gate_norm(p("x"), D, p("dy"), D, p("w"), 1e-6, T, 1, D, code, 0, guarded("gy", T * D * e), st) == 0
+            n = lib.hagdn_gate_norm_workspace_size(T, 1, D)
+            assert lib.hagdn_gate_norm_backward(p("dy"), D, p("x"), D, p("dy"), D, p("w"), 1e-6, T, 1, D, code, 0,
+                                                guarded("do", T * D * e), guarded("dz", T * D * e), guarded("gw", 4 * D),
+                                                guarded("gws", n), n, st) == 0
+            torch.cuda.synchronize()
+            for name, (buf, nbytes) in raw.items():
+                v = buf.cpu().numpy()
+                assert (v[:2048] == 0xA5).all() and (v[2048 + nbytes:] == 0xA5).all(), (name, T, D, dtype)
 
 
 @pytest.mark.gpu
