@@ -414,12 +414,13 @@ __global__ __launch_bounds__(backward_threads<LANES>(), LANES > 512 || !READS_X 
       }
     }
   }
+  const bool alone = gridDim.x == 1;  // its sums are the gradients
   const int outs = 1 + (a.dscale != nullptr) + (a.dpost != nullptr);
   float *out = a.partial + (size_t)blockIdx.x * outs * a.D;
-  write_partial<VE, C, LANES, kRows>(aw, ch, out, lds);
+  write_partial<VE, C, LANES, kRows>(aw, ch, alone ? a.dw : out, lds);
   if constexpr (READS_X) {
-    if (a.dscale) write_partial<VE, C, LANES, kRows>(as, ch, out += a.D, lds);
-    if (a.dpost) write_partial<VE, C, LANES, kRows>(ap, ch, out += a.D, lds);
+    if (a.dscale) write_partial<VE, C, LANES, kRows>(as, ch, alone ? a.dscale : out += a.D, lds);
+    if (a.dpost) write_partial<VE, C, LANES, kRows>(ap, ch, alone ? a.dpost : out += a.D, lds);
   }
 }
 
@@ -563,7 +564,7 @@ __global__ __launch_bounds__(backward_threads<LANES>(), LANES > 512 || sizeof(T)
       }
     }
   }
-  write_partial<VE, C, LANES, kRows>(aw, ch, a.partial + (size_t)blockIdx.x * a.d, lds);
+  write_partial<VE, C, LANES, kRows>(aw, ch, gridDim.x == 1 ? a.dw : a.partial + (size_t)blockIdx.x * a.d, lds);
 }
 
 // -------------------------------------------------------------------- launches
@@ -594,6 +595,13 @@ static unsigned norm_grid(long rows, int per) {
   return (unsigned)(groups < (1l << 20) ? groups : 1l << 20);
 }
 
+// Workgroups of a backward pass, `per` rows at a time each: at most a.parts, never one
+// without rows, and one alone, which needs no second kernel, for what two would do.
+static int norm_parts_used(long rows, int per, int parts) {
+  const long groups = (rows + per - 1) / per;
+  return groups <= 2 ? 1 : (int)(groups < parts ? groups : parts);
+}
+
 template <typename T, typename R> struct AddNorm {
   const AddNormArgs &a;
   hipStream_t s;
@@ -607,12 +615,13 @@ template <typename T, typename R> struct AddNormBackward {
   const AddNormArgs &a;
   hipStream_t s;
   template <int VE, int LANES, int C> hipError_t go() const {
-    const dim3 grid(a.parts), block(backward_threads<LANES>());
+    const int parts = norm_parts_used(a.T, backward_threads<LANES>() / LANES, a.parts);
+    const dim3 grid(parts), block(backward_threads<LANES>());
     if (a.post || a.scale_vec) hipLaunchKernelGGL((add_norm_backward_kernel<T, R, VE, LANES, C, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((add_norm_backward_kernel<T, R, VE, LANES, C, false>), grid, block, 0, s, a);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : sum_parts(a.partial, a.parts, a.D, a.dw, a.dscale ? a.dscale : a.dpost,
-                                           a.dscale ? a.dpost : nullptr, s);
+    if (e != hipSuccess || parts == 1) return e;
+    return sum_parts(a.partial, parts, a.D, a.dw, a.dscale ? a.dscale : a.dpost, a.dscale ? a.dpost : nullptr, s);
   }
 };
 template <typename T> struct GateNorm {
@@ -628,9 +637,10 @@ template <typename T> struct GateNormBackward {
   const GateNormArgs &a;
   hipStream_t s;
   template <int VE, int LANES, int C> hipError_t go() const {
-    hipLaunchKernelGGL((gate_norm_backward_kernel<T, VE, LANES, C>), dim3(a.parts), dim3(backward_threads<LANES>()), 0, s, a);
+    const int parts = norm_parts_used((long)a.T * a.H, backward_threads<LANES>() / LANES, a.parts);
+    hipLaunchKernelGGL((gate_norm_backward_kernel<T, VE, LANES, C>), dim3(parts), dim3(backward_threads<LANES>()), 0, s, a);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : sum_parts(a.partial, a.parts, a.d, a.dw, nullptr, nullptr, s);
+    return e != hipSuccess || parts == 1 ? e : sum_parts(a.partial, parts, a.d, a.dw, nullptr, nullptr, s);
   }
 };
 
