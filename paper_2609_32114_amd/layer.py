@@ -59,20 +59,17 @@ def _matrix(name, t, what):
 
 
 def _rows(name, t, shape, di):
-    """Row stride in elements of a tensor whose rows (all but the first dimension)
-    are contiguous; checks its device and shape."""
-    if t.get_device() == di and t.shape == shape and t.is_contiguous() and di >= 0:
-        return t.stride(0)
+    """Row stride in elements of a matrix [T, D] or heads [T, H, d] whose rows (all but the
+    first dimension) are contiguous; checks its device and shape."""
     if t.get_device() != di or di < 0:
         raise ValueError(f"{name} must be on the GPU of the call's first tensor")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
-    inner = 1
-    for size, stride in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
-        if size != 1 and stride != inner:
-            raise ValueError(f"{name} must have contiguous rows (strides {t.stride()})")
-        inner *= size
-    return t.stride(0)
+    s = t.stride()
+    if s[-1] != 1 and shape[-1] != 1 or len(s) == 3 and s[1] != shape[2] and shape[1] != 1:
+        if not t.is_contiguous():  # (a tensor without elements is)
+            raise ValueError(f"{name} must have contiguous rows (strides {s})")
+    return s[0]
 
 
 def _fp32(name, t, shape, x):
@@ -85,7 +82,7 @@ def _workspace(workspace, size, x):
     """(tensor, bytes) of a call's workspace: the caller's, or a new one of size() bytes."""
     if workspace is None:
         n = size()
-        return torch.empty(n, dtype=torch.uint8, device=x.device), n
+        return x.new_empty(n, dtype=torch.uint8), n
     if workspace.get_device() != x.get_device() or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {x.device}")
     return workspace, workspace.numel() * workspace.element_size()
@@ -93,7 +90,7 @@ def _workspace(workspace, size, x):
 
 def _output(name, t, shape, dtype, x):
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=x.device)
+        return x.new_empty(shape, dtype=dtype)
     _check_buffer(name, t, x.device, dtype, shape)
     return t
 
@@ -101,7 +98,7 @@ def _output(name, t, shape, dtype, x):
 def _like(name, t, x):
     """A contiguous output of x's shape and type: t, or a new one."""
     if t is None:
-        return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
     _check_buffer(name, t, x.device, x.dtype, x.shape)
     return t
 
@@ -147,7 +144,7 @@ def glr_prefill(x, g, initial_state=None, cu_seqlens=None, convex=False, preproc
         _fp32("initial_state", initial_state, (N, D), x)
     h = _like("out", out, x)
     final = _output("final_out", final_out, (N, D), _F32, x) if output_final_state else None
-    saved = torch.empty((_groups(T), D), dtype=_F32, device=x.device) if output_checkpoints else None
+    saved = x.new_empty((_groups(T), D), dtype=_F32) if output_checkpoints else None
     ws, ws_bytes = _workspace(workspace, lambda: glr_workspace_size(T, D), x)
     _check(lib.glr_prefill(
         x.data_ptr(), xs, g.data_ptr(), gs, _ptr(initial_state), cu, N, T, D, dt, gt, int(convex), int(preprocess),
