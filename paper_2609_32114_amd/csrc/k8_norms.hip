@@ -226,6 +226,14 @@ static hipError_t sum_parts(const float *partial, int parts, int D, float *o0, f
 // apart; in the backward passes more rows together mean fewer partial sums.
 template <int LANES> constexpr int forward_threads() { return LANES > 256 ? LANES : 256; }
 template <int LANES> constexpr int backward_threads() { return LANES > 512 ? LANES : 512; }
+// Rows that a group of lanes takes through one round of sums in add_norm's backward: two,
+// where a row's way through its waves is long and both rows' operands are bf16 (8192 rows
+// of 2048 39 us against 41, with both vectors 49 against 51; 500 rows 14 against 16).  A
+// stream in fp32 loses by it (55 against 53, 66 against 64), all in fp32 spills (58
+// against 45); within one wave, up to 512 values a row, it makes no difference.
+template <typename T, typename R, int LANES> constexpr int rows_per_turn() {
+  return sizeof(T) == 2 && sizeof(R) == 2 && LANES >= 128 && LANES <= 512 ? 2 : 1;
+}
 
 // ---------------------------------------------------------------------- add_norm
 // One read of x and the stream, one write of y and the stream.  32768 rows of 2048 in
@@ -302,20 +310,22 @@ __global__ __launch_bounds__(forward_threads<LANES>()) void add_norm_kernel(AddN
 // q is taken from D's three terms' own sums, so that one round of sums serves the row.
 // The operands stay as they were loaded (bf16 ones two to a register), the weights in
 // registers for all of the workgroup's rows.  READS_X: a scale vector or post_weight is
-// there.  8192 rows of 2048 in bf16 with both 50 us, 4.0 TB/s, of which 5 the sum over the
-// workgroups; without them 38 us, 4.4 TB/s.  Bound by the row's way through its sums and
-// barrier, which eight waves a CU overlap in part: sixteen, which spill, took 98 us, the
-// operands of two or three rows fetched ahead 51 and 53.
+// there.  8192 rows of 2048 in bf16 with both 49 us, 4.1 TB/s, of which 5 the sum over the
+// workgroups; without them 39 us, 4.3 TB/s.  Bound by the rows' way through their sums and
+// barrier, which eight waves a CU overlap in part: sixteen, which spill, took 98 us; with
+// one row a turn 51, and the operands of two or three rows fetched ahead no less.
 template <typename T, typename R, int VE, int LANES, int C, bool READS_X>
-__global__ __launch_bounds__(backward_threads<LANES>(), LANES > 512 || !READS_X ? 4 : 2) void add_norm_backward_kernel(
-    AddNormArgs a) {
+__global__ __launch_bounds__(backward_threads<LANES>(),
+                             LANES > 512 || (!READS_X && rows_per_turn<T, R, LANES>() == 1) ? 4 : 2)
+void add_norm_backward_kernel(AddNormArgs a) {
   constexpr int kThreads = backward_threads<LANES>(), kRows = kThreads / LANES, kSums = READS_X ? 6 : 2;
-  HAGDN_ROW_SUMS(sums, LANES, kThreads, kSums);
+  constexpr int P = rows_per_turn<T, R, LANES>();
+  HAGDN_ROW_SUMS(sums, LANES, kThreads, P * kSums);
   __shared__ float lds[kRows > 1 ? kRows * LANES : 1];
   const float inv = 1.f / (float)a.D;
   Chunk<VE> ch[C];
   float aw[C][VE], as[C][VE], ap[C][VE];  // the weights' gradients
-  float w[C][VE], s[C][VE], p[C][VE];     // weight, scale, post_weight
+  float w[C][VE], s[C][VE], post[C][VE];  // weight, scale, post_weight
 #pragma unroll
   for (int j = 0; j < C; ++j) {
     ch[j] = Chunk<VE>((j * LANES + threadIdx.x % LANES) * VE, a.D);
@@ -326,91 +336,105 @@ __global__ __launch_bounds__(backward_threads<LANES>(), LANES > 512 || !READS_X 
   for (int j = 0; j < C; ++j) {
     ch[j].load(a.w, w[j]);
 #pragma unroll
-    for (int e = 0; e < VE; ++e) s[j][e] = a.scale, p[j][e] = 1.f;
+    for (int e = 0; e < VE; ++e) s[j][e] = a.scale, post[j][e] = 1.f;
     if (READS_X && a.scale_vec) ch[j].load(a.scale_vec, s[j]);
-    if (READS_X && a.post) ch[j].load(a.post, p[j]);
+    if (READS_X && a.post) ch[j].load(a.post, post[j]);
   }
   // the loop's bounds are those of the workgroup's first row: all lanes take every turn.
-  // A row's operands are fetched while the one before is worked on.
-  const long step = (long)gridDim.x * kRows, own = threadIdx.x / LANES;
-  Raw<R, VE> nr[C], nd[C];
-  Raw<T, VE> ng[C], nx[C];
-  auto fetch = [&](long row) {
-    row = min(row, (long)a.T - 1);
+  // The next turn's operands are fetched while one is worked on.
+  const long step = (long)gridDim.x * kRows * P, own = threadIdx.x / LANES;
+  Raw<R, VE> nr[P][C], nd[P][C];
+  Raw<T, VE> ng[P][C], nx[P][C];
+  auto fetch = [&](long first) {
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-      ch[j].fetch(static_cast<const R *>(a.res) + row * a.rs, nr[j]);
-      ch[j].fetch(static_cast<const T *>(a.dy) + row * a.dys, ng[j]);
-      if (a.dres) ch[j].fetch(static_cast<const R *>(a.dres) + row * a.drs, nd[j]);
-      if constexpr (READS_X) ch[j].fetch(static_cast<const T *>(a.x) + row * a.xs, nx[j]);
+    for (int p = 0; p < P; ++p) {
+      const long row = min(first + p * kRows + own, (long)a.T - 1);
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        ch[j].fetch(static_cast<const R *>(a.res) + row * a.rs, nr[p][j]);
+        ch[j].fetch(static_cast<const T *>(a.dy) + row * a.dys, ng[p][j]);
+        if (a.dres) ch[j].fetch(static_cast<const R *>(a.dres) + row * a.drs, nd[p][j]);
+        if constexpr (READS_X) ch[j].fetch(static_cast<const T *>(a.x) + row * a.xs, nx[p][j]);
+      }
     }
   };
-  if (a.T > 0) fetch((long)blockIdx.x * kRows + own);
-  for (long first = (long)blockIdx.x * kRows; first < a.T; first += step) {
-    const long row = first + own;
-    const bool live = row < a.T;
-    Raw<R, VE> r[C], d[C];  // r', dres
-    Raw<T, VE> g[C], x[C];  // dy, x
+  if (a.T > 0) fetch((long)blockIdx.x * kRows * P);
+  for (long first = (long)blockIdx.x * kRows * P; first < a.T; first += step) {
+    Raw<R, VE> r[P][C], d[P][C];  // r', dres
+    Raw<T, VE> g[P][C], x[P][C];  // dy, x
+    float v[P * kSums] = {};
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-      r[j] = nr[j], g[j] = ng[j], d[j] = nd[j];
-      if constexpr (READS_X) x[j] = nx[j];
-      Chunk<VE>::clear(r[j], ch[j].skip);
-      if constexpr (READS_X) Chunk<VE>::clear(x[j], ch[j].skip);
-      Chunk<VE>::clear(g[j], live ? ch[j].skip : VE);  // a row past the end adds nothing
-      Chunk<VE>::clear(d[j], live && a.dres ? ch[j].skip : VE);
-    }
-    if (first + step < a.T) fetch(row + step);
-    float v[kSums] = {};
+    for (int p = 0; p < P; ++p) {
+      const bool live = first + p * kRows + own < a.T;
 #pragma unroll
-    for (int j = 0; j < C; ++j)
-#pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const float re = r[j].get(e), wg = w[j][e] * g[j].get(e);
-        v[0] += re * re;
-        v[1] += re * wg;
-        if constexpr (READS_X) {
-          const float xe = x[j].get(e), xs = xe * (p[j][e] * s[j][e]);
-          v[2] += xe * xe;
-          v[3] += xs * d[j].get(e);
-          v[4] += xs * wg;
-          v[5] += xs * re;
-        }
+      for (int j = 0; j < C; ++j) {
+        r[p][j] = nr[p][j], g[p][j] = ng[p][j], d[p][j] = nd[p][j];
+        if constexpr (READS_X) x[p][j] = nx[p][j];
+        Chunk<VE>::clear(r[p][j], ch[j].skip);
+        if constexpr (READS_X) Chunk<VE>::clear(x[p][j], ch[j].skip);
+        Chunk<VE>::clear(g[p][j], live ? ch[j].skip : VE);  // a row past the end adds nothing
+        Chunk<VE>::clear(d[p][j], live && a.dres ? ch[j].skip : VE);
       }
+    }
+    if (first + step < a.T) fetch(first + step);
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      float *s6 = v + p * kSums;
+#pragma unroll
+      for (int j = 0; j < C; ++j)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const float re = r[p][j].get(e), wg = w[j][e] * g[p][j].get(e);
+          s6[0] += re * re;
+          s6[1] += re * wg;
+          if constexpr (READS_X) {
+            const float xe = x[p][j].get(e), xs = xe * (post[j][e] * s[j][e]);
+            s6[2] += xe * xe;
+            s6[3] += xs * d[p][j].get(e);
+            s6[4] += xs * wg;
+            s6[5] += xs * re;
+          }
+        }
+    }
     sums(v);
-    const float rr = rstd(v[0], inv, a.eps), m = rr * rr * rr * v[1] * inv;
-    float rx = 1.f, q = 0.f;
-    if constexpr (READS_X) {
-      if (a.post) {
-        rx = rstd(v[2], inv, a.eps);
-        q = rx * rx * (v[3] + rr * v[4] - m * v[5]) * inv;
-      }
-    }
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-      float out[VE], dx[VE];
-      r[j].keep_packed();
-      g[j].keep_packed();
-      d[j].keep_packed();
-      if constexpr (READS_X) x[j].keep_packed();
-#pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const float re = r[j].get(e), ge = g[j].get(e);
-        aw[j][e] += ge * (re * rr);
-        out[e] = d[j].get(e) + (rr * (w[j][e] * ge) - m * re);
-        const float du = s[j][e] * out[e];
-        if constexpr (READS_X) {
-          const float xe = x[j].get(e), xn = xe * rx;
-          as[j][e] += out[e] * xn * p[j][e];
-          ap[j][e] += du * xn;
-          dx[e] = rx * (p[j][e] * du - xe * q);
-        } else {
-          dx[e] = du;
+    for (int p = 0; p < P; ++p) {
+      const long row = first + p * kRows + own;
+      const float *s6 = v + p * kSums;
+      const float rr = rstd(s6[0], inv, a.eps), m = rr * rr * rr * s6[1] * inv;
+      float rx = 1.f, q = 0.f;
+      if constexpr (READS_X) {
+        if (a.post) {
+          rx = rstd(s6[2], inv, a.eps);
+          q = rx * rx * (s6[3] + rr * s6[4] - m * s6[5]) * inv;
         }
       }
-      if (live) {
-        if (a.dres_out) ch[j].store(static_cast<R *>(a.dres_out) + row * a.D, out);
-        ch[j].store(static_cast<T *>(a.dx) + row * a.D, dx);
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        float out[VE], dx[VE];
+        r[p][j].keep_packed();
+        g[p][j].keep_packed();
+        d[p][j].keep_packed();
+        if constexpr (READS_X) x[p][j].keep_packed();
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const float re = r[p][j].get(e), ge = g[p][j].get(e);
+          aw[j][e] += ge * (re * rr);
+          out[e] = d[p][j].get(e) + (rr * (w[j][e] * ge) - m * re);
+          const float du = s[j][e] * out[e];
+          if constexpr (READS_X) {
+            const float xe = x[p][j].get(e), xn = xe * rx;
+            as[j][e] += out[e] * xn * post[j][e];
+            ap[j][e] += du * xn;
+            dx[e] = rx * (post[j][e] * du - xe * q);
+          } else {
+            dx[e] = du;
+          }
+        }
+        if (row < a.T) {
+          if (a.dres_out) ch[j].store(static_cast<R *>(a.dres_out) + row * a.D, out);
+          ch[j].store(static_cast<T *>(a.dx) + row * a.D, dx);
+        }
       }
     }
   }
@@ -615,7 +639,8 @@ template <typename T, typename R> struct AddNormBackward {
   const AddNormArgs &a;
   hipStream_t s;
   template <int VE, int LANES, int C> hipError_t go() const {
-    const int parts = norm_parts_used(a.T, backward_threads<LANES>() / LANES, a.parts);
+    const int parts = norm_parts_used(a.T, backward_threads<LANES>() / LANES * rows_per_turn<T, R, LANES>(),
+                                       a.parts);
     const dim3 grid(parts), block(backward_threads<LANES>());
     if (a.post || a.scale_vec) hipLaunchKernelGGL((add_norm_backward_kernel<T, R, VE, LANES, C, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((add_norm_backward_kernel<T, R, VE, LANES, C, false>), grid, block, 0, s, a);
