@@ -15,7 +15,8 @@
 //      its tokens again, from registers.
 // Workgroups take the tiles of their 64 channels in order from a counter, so a tile's
 // predecessors have all been taken by workgroups that run or have ended, and every wait
-// ends.  (One counter for the whole call costs some 33 ns a tile: 8192 tiles 272 us.)
+// ends.  (Lanes past the last channel follow a channel of their own column: glr_channel.
+// One counter for the whole call costs some 33 ns a tile: 8192 tiles 272 us.)
 // The state is always folded forward from a whole one through the same fused products,
 // so that its bits do not depend on how far back that one was: results repeat exactly.
 // A wait is bounded all the same (kLookLimit, HAGDN_DEV_WAIT_TIMEOUT).

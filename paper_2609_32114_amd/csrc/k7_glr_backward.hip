@@ -41,7 +41,7 @@ __global__ __launch_bounds__(W * 64, 4) void glr_backward_kernel(GlrArgs a, uint
     __syncthreads();
     const uint32_t tile = tiles - 1 - __builtin_amdgcn_readfirstlane(sNext);
     const bool mine = at < (uint32_t)a.D;
-    const uint32_t c = mine ? at : 0;  // lanes past the last channel compute the first one's, and store nothing
+    const uint32_t c = glr_channel(at, (uint32_t)a.D);  // lanes that are not `mine` store nothing
     if (tile == 0) pass_empty(a.cu, a.N, a.T, ok, a.dfinal, a.ds0, a.D, at);
 
     // the wave's tokens; rows past the end are loaded from the last one

@@ -41,6 +41,11 @@ constexpr size_t kGlrHeader = 256;          // bytes before the counters
 constexpr size_t kGlrCounterStride = 32;    // counters lie in memory lines of their own
 inline size_t glr_counter_bytes(int D) { return ((size_t)D + 63) / 64 * kGlrCounterStride * sizeof(uint32_t); }
 
+// The channel a lane of the scan works on.  Lanes past the last channel, which store and
+// publish nothing, follow a channel of their own column of 64 (the last one), so that a
+// tile waits for tiles of its own column only.  at: 64 column + lane; D >= 1.
+__host__ __device__ inline uint32_t glr_channel(uint32_t at, uint32_t D) { return at < D ? at : D - 1; }
+
 struct GlrStepArgs {
   const void *x, *g;
   long xs, gs;
