@@ -396,3 +396,27 @@ def test_graph_replays():
         for a, b in zip(out, want[i]):
             assert torch.equal(a, b)
         call(sets[2])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,res", TYPES, ids=lambda t: t)
+@pytest.mark.parametrize("D", [7, 64, 200, 2048, 5000, 9000])
+def test_add_norm_row_scales(D, dtype, res):
+    """Rows of root mean squares from 1e-14 to 1e14 without an eps: norms and their
+    gradients are representable throughout, whatever a power of the reciprocal root is."""
+    d = add_inputs(10, D, dtype, res, D + 1)
+    rows = 10.0 ** np.array([-14, -7, 0, 7, 14, -14, 14, -3, 3, 13])[:, None]
+    for k in ("x", "res"):
+        d[k] = rounded(np64(d[k]) * rows, dtype if k == "x" else res)
+    for post, vector in ((False, False), (True, True), (True, False), (False, True)):
+        add_case(d, dtype, res, post, vector, dresidual=False, eps=0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [7, 128, 2048, 9000])
+def test_gate_norm_row_scales(d, dtype):
+    i = gate_inputs(10, 1, d, dtype, d)
+    rows = 10.0 ** np.array([-14, -7, 0, 7, 14, -14, 14, -3, 3, 13])[:, None, None]
+    i["o"] = rounded(np64(i["o"]) * rows, dtype)
+    gate_case(i, dtype, "silu", eps=0.0)
