@@ -452,11 +452,14 @@ void add_norm_backward_kernel(AddNormArgs a) {
 }
 
 // --------------------------------------------------------------------- gate_norm
-// act(z) and its derivative, from e^-z: 1 / (1 + e^-z) is 0 where that overflows.
+// act(z) and its derivative, from t = e^-z: s = 1 / (1 + t) is 0 where t overflows.  Its
+// complement is t s, since 1 - s would cancel for open gates; the minimum, which passes
+// over a NaN, makes it 1 where t s is infinity times 0.
 __device__ __forceinline__ void activation(bool silu, float z, float &f, float &df) {
-  const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+  const float t = __builtin_amdgcn_exp2f(z * -1.44269504f), s = __builtin_amdgcn_rcpf(1.f + t);
+  const float rest = fminf(t * s, 1.f);
   f = silu ? z * s : s;
-  df = silu ? s * (1.f + z * (1.f - s)) : s * (1.f - s);
+  df = f * rest + (silu ? s : 0.f);  // s (1 + z (1 - s)), or s (1 - s)
 }
 
 // Where a row (token, head) of a tensor [T, H, d] with a token stride begins.
