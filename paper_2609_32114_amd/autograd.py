@@ -7,7 +7,8 @@
 The arguments of the functions of the same (or, for glr, the prefill's) name; both
 directions run in the library's kernels.  Kept for the backward pass: the operands and
 the saved states (glr), the residual stream that add_norm returned, and x where a scale
-vector or post_weight is there.
+vector or post_weight is there.  There are first derivatives only: differentiating the
+gradients again (create_graph=True, then a second backward pass) raises.
 """
 
 from __future__ import annotations
@@ -20,6 +21,25 @@ from . import layer
 def _rows(t):
     """A gradient as the kernels take it: rows of contiguous elements."""
     return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+
+
+class _Gradients(torch.autograd.Function):
+    """The kernels' gradients as results of all that they are formed from: their own
+    derivative, which no kernel computes, is an error and not zero."""
+
+    @staticmethod
+    def forward(ctx, kernels, *args):
+        return kernels(*args)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the recurrence and the block norms have no second derivative: their gradients come "
+                           "from kernels and cannot be differentiated again")
+
+
+def _gradients(kernels, *args):
+    """kernels(*args), as part of the backward pass's own graph where one is asked for."""
+    return _Gradients.apply(kernels, *args) if torch.is_grad_enabled() else kernels(*args)
 
 
 class _Glr(torch.autograd.Function):
@@ -38,7 +58,7 @@ class _Glr(torch.autograd.Function):
         convex, preprocess = ctx.how
         dh = torch.zeros_like(x) if dh is None else _rows(dh)
         dfinal = None if dfinal is None else dfinal.contiguous()
-        dx, dg, ds0 = layer.glr_backward(dh, x, g, saved, s0, dfinal, cu, convex, preprocess)
+        dx, dg, ds0 = _gradients(layer.glr_backward, dh, x, g, saved, s0, dfinal, cu, convex, preprocess)
         return dx, dg, ds0, None, None, None
 
 
@@ -62,8 +82,8 @@ class _AddNorm(torch.autograd.Function):
         if dy is None:
             dy = torch.zeros(res.shape, dtype=dtype, device=res.device)
         dres = None if dres is None else _rows(dres)
-        dx, dr, dw, ds, dp = layer.add_norm_backward(_rows(dy), res, weight, dres, x, vector if vector is not None else number,
-                                                     post_weight, eps)
+        dx, dr, dw, ds, dp = _gradients(layer.add_norm_backward, _rows(dy), res, weight, dres, x,
+                                        vector if vector is not None else number, post_weight, eps)
         return dx, dw, dr if has_residual else None, ds, dp, None
 
 
@@ -77,7 +97,7 @@ class _GateNorm(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         o, z, weight = ctx.saved_tensors
-        do, dz, dw = layer.gate_norm_backward(dy.contiguous(), o, z, weight, *ctx.how)
+        do, dz, dw = _gradients(layer.gate_norm_backward, dy.contiguous(), o, z, weight, *ctx.how)
         return do, dz, dw, None, None
 
 
