@@ -1,6 +1,6 @@
 """Differentiable forms of the gated linear recurrence and the block norms.
 
-    h, final = glr(x, g, initial_state=None, cu_seqlens=None, convex=False, preprocess=0)
+    h, final = glr(x, g, initial_state=None, cu_seqlens=None, convex=False, preprocess=0, workspace=None)
     y, res = add_norm(x, weight, residual=None, scale=1.0, post_weight=None, eps=1e-6)
     y = gate_norm(o, z, weight, activation="silu", eps=1e-6)
 
@@ -44,22 +44,23 @@ def _gradients(kernels, *args):
 
 class _Glr(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, g, initial_state, cu_seqlens, convex, preprocess):
+    def forward(ctx, x, g, initial_state, cu_seqlens, convex, preprocess, workspace):
         h, final, saved = layer.glr_prefill(x, g, initial_state, cu_seqlens, convex, preprocess,
-                                            output_checkpoints=True)
+                                            output_checkpoints=True, workspace=workspace)
         ctx.save_for_backward(x, g, saved, initial_state, cu_seqlens)
-        ctx.how = (convex, preprocess)
+        ctx.how = (convex, preprocess, workspace)
         ctx.set_materialize_grads(False)
         return h, final
 
     @staticmethod
     def backward(ctx, dh, dfinal):
         x, g, saved, s0, cu = ctx.saved_tensors
-        convex, preprocess = ctx.how
+        convex, preprocess, workspace = ctx.how
         dh = torch.zeros_like(x) if dh is None else _rows(dh)
         dfinal = None if dfinal is None else dfinal.contiguous()
-        dx, dg, ds0 = _gradients(layer.glr_backward, dh, x, g, saved, s0, dfinal, cu, convex, preprocess)
-        return dx, dg, ds0, None, None, None
+        dx, dg, ds0 = _gradients(layer.glr_backward, dh, x, g, saved, s0, dfinal, cu, convex, preprocess,
+                                  workspace)
+        return dx, dg, ds0, None, None, None, None
 
 
 class _AddNorm(torch.autograd.Function):
@@ -101,9 +102,10 @@ class _GateNorm(torch.autograd.Function):
         return do, dz, dw, None, None
 
 
-def glr(x, g, initial_state=None, cu_seqlens=None, convex=False, preprocess=0):
-    """Differentiable glr_prefill: (h, final state)."""
-    return _Glr.apply(x, g, initial_state, cu_seqlens, convex, preprocess)
+def glr(x, g, initial_state=None, cu_seqlens=None, convex=False, preprocess=0, workspace=None):
+    """Differentiable glr_prefill: (h, final state).  Both directions use ``workspace``
+    where one is given, and leave their device status in it."""
+    return _Glr.apply(x, g, initial_state, cu_seqlens, convex, preprocess, workspace)
 
 
 def add_norm(x, weight, residual=None, scale=1.0, post_weight=None, eps=1e-6):

@@ -133,7 +133,9 @@ def glr_prefill(x, g, initial_state=None, cu_seqlens=None, convex=False, preproc
     """Gated linear recurrence h_t = a_t h_{t-1} + w_t x_t over packed sequences, with
     a_t = exp(g_t) (PRE_GATE_SOFTPLUS: g holds raw values, a_t = 1 / (1 + e^g)) and
     w_t = 1, or 1 - a_t where ``convex``.  Returns (h, final state [N, D] fp32 or
-    None); with ``output_checkpoints`` also the states that glr_backward takes."""
+    None); with ``output_checkpoints`` also the states that glr_backward takes.
+    Malformed cu_seqlens are found on the device: h is then left as it was allocated,
+    and device_status(workspace) of the caller's own workspace says so."""
     lib = load_library()
     shape, di = _matrix("x", x, "[T, D]")
     T, D = shape
@@ -156,7 +158,8 @@ def glr_backward(dh, x, g, checkpoints, initial_state=None, dfinal=None, cu_seql
                  workspace=None):
     """Gradients of glr_prefill from that of h (``dh``) and of the final state
     (``dfinal``): (dx, dg, gradient of the initial state, or None without one).
-    ``checkpoints`` is what the forward call returned."""
+    ``checkpoints`` is what the forward call returned.  ``workspace``: as for
+    glr_prefill."""
     lib = load_library()
     shape, di = _matrix("x", x, "[T, D]")
     T, D = shape

@@ -145,3 +145,20 @@ def test_norm_after_a_delta_rule_mixer():
     rows = lambda t: t.double().cpu().numpy().reshape(-1, d)
     want = ref.gate_norm(rows(o), rows(z), w.double().cpu().numpy(), True, 1e-6)
     assert ref.excess(y, want["y"], "bf16") <= 1.0
+
+
+def test_glr_device_status():
+    """Malformed offsets show in the status of the caller's workspace, after either direction."""
+    import torch
+    import paper_2609_32114_amd as P
+    from paper_2609_32114_amd import autograd
+    T, D = 700, 70
+    x, g = _inputs((T, D), (T, D))
+    ws = torch.full((P.glr_workspace_size(T, D),), 0xFF, dtype=torch.uint8, device="cuda")
+    for last, code in ((T - 1, P.DEV_BAD_SEQLENS), (T, P.DEV_OK)):
+        cu = torch.tensor([0, 300, last], dtype=torch.int32, device="cuda")
+        h, final = autograd.glr(x, g, cu_seqlens=cu, workspace=ws)
+        assert P.device_status(ws) == code
+        ws.fill_(0xFF)
+        final.sum().backward()
+        assert P.device_status(ws) == code

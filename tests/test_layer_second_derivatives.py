@@ -56,7 +56,7 @@ def stand_ins(monkeypatch):
     def gate_norm_backward(dy, o, z, w, activation, eps):
         return tuple(_grads(lambda *a: _gate(*a, activation, eps), (o, z, w), (dy,)))
 
-    def glr_backward(dh, x, g, saved, s0, dfinal, cu, convex, preprocess):
+    def glr_backward(dh, x, g, saved, s0, dfinal, cu, convex, preprocess, workspace):
         d = _grads(_glr, (x, g, s0), (dh, dfinal))
         return next(d), next(d), None if s0 is None else next(d)
 
@@ -65,7 +65,7 @@ def stand_ins(monkeypatch):
     monkeypatch.setattr(layer, "add_norm", add_norm)
     monkeypatch.setattr(layer, "add_norm_backward", add_norm_backward)
     monkeypatch.setattr(layer, "glr_prefill", torch.no_grad()(
-        lambda x, g, s0, cu, convex, pre, output_checkpoints: _glr(x, g, s0) + (torch.zeros(1, x.shape[1]),)))
+        lambda x, g, s0, cu, convex, pre, output_checkpoints, workspace: _glr(x, g, s0) + (torch.zeros(1, x.shape[1]),)))
     monkeypatch.setattr(layer, "glr_backward", glr_backward)
     return "cpu"
 
