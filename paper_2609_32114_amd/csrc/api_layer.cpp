@@ -81,7 +81,8 @@ int check_glr(int N, int T, int D, int dtype, int gate_dtype, int convex, int pr
   return check_dtypes(dtype, gate_dtype, "gate");
 }
 
-// Workspace of a call: the header, the counters and the words of the smallest tiles.
+// Workspace of a call in either direction: the header and, where some tiles' words are
+// needed, the counters and the words of the smallest tiles.
 size_t glr_bytes(int T, int D) {
   const size_t tiles = ((size_t)T + hagdn::kGlrLeastTile - 1) / hagdn::kGlrLeastTile;
   return hagdn::kGlrHeader + (tiles > 1 ? hagdn::glr_counter_bytes(D) + tiles * (size_t)D * 8 : 0);  // below 2^60

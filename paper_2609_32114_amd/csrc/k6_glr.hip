@@ -219,6 +219,7 @@ template <typename T, typename G> struct Forward {
     constexpr int kTile = W * L;
     const long tiles = a.T > 0 ? ((long)a.T + kTile - 1) / kTile : 1, cols = ((long)a.D + 63) / 64;
     if (tiles * cols > 0xffff0000l) return hipErrorInvalidValue;  // the turns' range
+    if (tiles > 1 && kTile < kGlrLeastTile) return hipErrorInvalidValue;  // the workspace's words
     if (tiles > 1) {
       const hipError_t e = launch_glr_setup(a, (size_t)tiles * a.D, (uint32_t)cols, s);
       if (e != hipSuccess) return e;

@@ -35,8 +35,9 @@ struct GlrArgs {
   uint64_t *words;
 };
 
-// The smallest tile of the kernels, in tokens; a call of one tile needs no words.
-constexpr int kGlrLeastTile = 64;
+// The smallest tile of a call that has several, in tokens (calls of up to 64 tokens take one
+// of 64); a call of one tile needs no words.
+constexpr int kGlrLeastTile = 128;
 constexpr size_t kGlrHeader = 256;          // bytes before the counters
 constexpr size_t kGlrCounterStride = 32;    // counters lie in memory lines of their own
 inline size_t glr_counter_bytes(int D) { return ((size_t)D + 63) / 64 * kGlrCounterStride * sizeof(uint32_t); }

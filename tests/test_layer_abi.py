@@ -158,3 +158,13 @@ def test_binding_refusals_on_the_gpu():
     _cuda(lambda: P.gate_norm(x.view(4, 2, 4), b.view(4, 2, 4), z(4)), TypeError, "z must be")
     _cuda(lambda: P.gate_norm(x.view(4, 2, 4), x.view(4, 2, 4), z(4), activation="relu"), ValueError, "activation")
     _cuda(lambda: P.gate_norm(x, x, w), ValueError, "o must be")
+
+
+def test_glr_workspace_holds_what_a_call_uses():
+    """A header; beyond 128 tokens a counter's memory line per 64 channels, and a word per
+    channel of each tile, which has 128 tokens at least where a call has several."""
+    for T in (0, 1, 64, 65, 128, 129, 256, 1000, 32768, 100000):
+        for D in (1, 64, 65, 2048, 1 << 20):
+            tiles = (T + 127) // 128
+            want = 256 + ((D + 63) // 64 * 128 + tiles * D * 8 if tiles > 1 else 0)
+            assert P.glr_workspace_size(T, D) == want, (T, D)
