@@ -495,3 +495,45 @@ def test_writes_stay_inside():
         for name, (buf, nbytes) in raw.items():
             v = buf.cpu().numpy()
             assert (v[:2048] == 0xA5).all() and (v[2048 + nbytes:] == 0xA5).all(), (name, lens, D)
+
+
+# sequences that end on, before and after multiples of 256 and 512 tokens, and empty ones
+LONG_LENS = (511, 1, 513, 0, 512, 2000, 4096, 3, 1500, 0, 900)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,gate", TYPES, ids=lambda t: t)
+@pytest.mark.parametrize("D", [33, 67])
+def test_long_packed_calls_of_few_channels(D, dtype, gate):
+    """More than 8192 tokens in fewer tiles than CUs: the largest tiles, of 512 tokens
+    forward and 256 backward, with sequences that begin and end inside them."""
+    for i, (raw, convex) in enumerate([(False, False), (False, True), (True, False), (True, True)]):
+        d = make(LONG_LENS, D, dtype, gate, raw, 60 + i, s0=i != 2, slow=i == 3)
+        check(run(d, LONG_LENS, raw, convex), expected(d, LONG_LENS, raw, convex), dtype, gate,
+              f"long, D={D} {dtype}/{gate} raw={raw} convex={convex}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,D", [(LONG_LENS, 33), (LONG_LENS, 130), ((3000, 0, 2500, 1, 700), 705), ((2000,), 300)])
+def test_writes_of_long_calls_stay_inside(lens, D):
+    """Guard zones around the outputs and a workspace of just the size asked for."""
+    import torch
+    import paper_2609_32114_amd as P
+    lib = P.load_library()
+    T, N = sum(lens), len(lens)
+    t = {k: v.cuda() for k, v in make(lens, D, "bf16", "f32", False, 9).items()}
+    n = P.glr_workspace_size(T, D)
+    sizes = {"h": T * D * 2, "s": N * D * 4, "ck": (T + 127) // 128 * D * 4, "dx": T * D * 2, "dg": T * D * 4,
+             "ds0": N * D * 4, "ws": n}
+    raw = {k: torch.full((2048 + v + 2048,), 0xA5, dtype=torch.uint8, device="cuda") for k, v in sizes.items()}
+    o = {k: v.data_ptr() + 2048 for k, v in raw.items()}
+    cu, st = offsets(lens), torch.cuda.current_stream().cuda_stream
+    p = lambda k: t[k].data_ptr()
+    assert lib.glr_prefill(p("x"), D, p("g"), D, p("s0"), cu.data_ptr(), N, T, D, 1, 0, 0, 0, o["h"], o["s"], o["ck"],
+                           o["ws"], n, st) == 0
+    assert lib.glr_backward(p("dh"), D, p("x"), D, p("g"), D, o["ck"], p("s0"), p("dfinal"), cu.data_ptr(), N, T, D,
+                            1, 0, 0, 0, o["dx"], o["dg"], o["ds0"], o["ws"], n, st) == 0
+    torch.cuda.synchronize()
+    for k, buf in raw.items():
+        v = buf.cpu().numpy()
+        assert (v[:2048] == 0xA5).all() and (v[2048 + sizes[k]:] == 0xA5).all(), k
