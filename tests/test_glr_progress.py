@@ -5,11 +5,15 @@ kernels' own rule for the channels that a workgroup looks at."""
 import os
 import subprocess
 
-from test_host_sanitizers import CLANGXX, ROOT, _need
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CLANGXX = "/opt/rocm/llvm/bin/clang++"
 
 
 def test_every_wait_ends(tmp_path):
-    _need(CLANGXX)
+    if not os.path.exists(CLANGXX):
+        pytest.skip(f"{CLANGXX} not available")
     out = str(tmp_path / "progress")
     r = subprocess.run([CLANGXX, "-O2", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-isystem", "/opt/rocm/include", "-I",
                         os.path.join(ROOT, "paper_2609_32114_amd", "csrc"),
