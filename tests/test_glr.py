@@ -537,3 +537,38 @@ def test_writes_of_long_calls_stay_inside(lens, D):
     for k, buf in raw.items():
         v = buf.cpu().numpy()
         assert (v[:2048] == 0xA5).all() and (v[2048 + sizes[k]:] == 0xA5).all(), k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,D", [(7000, 33), (6000, 512), (1023, 40), (1024, 40)])
+def test_thousands_of_sequences_in_long_calls(N, D):
+    """More than 8192 tokens: pieces of 32 tokens that hold tens of sequences' ends, whose
+    offsets lie in LDS up to 1023 of them and in memory beyond."""
+    r = np.random.default_rng(N)
+    lens = tuple(int(n) for n in r.integers(0, 4 if N > 2000 else 20, N))
+    d = make(lens, D, "bf16", "f32", False, N)
+    check(run(d, lens, False, True), expected(d, lens, False, True), "bf16", "f32", f"N={N} D={D} T={sum(lens)}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("offset", [0, 1, 3])
+@pytest.mark.parametrize("D", [64, 67])
+def test_decode_from_slices(D, offset):
+    """Operands as column slices of a wider matrix at any offset, and one gate row for all."""
+    import torch
+    import paper_2609_32114_amd as P
+    N = 9
+    for dtype, gate in TYPES:
+        d = make((1,) * N, D, dtype, gate, False, D)
+        wide = {k: torch.full((N, 3 * D + 5), float("nan"), dtype=d[k].dtype, device="cuda") for k in "xg"}
+        for k, w in wide.items():
+            w[:, offset:offset + D] = d[k].cuda()
+        state = d["s0"].cuda()
+        h = P.glr_decode(*(wide[k][:, offset:offset + D] for k in "xg"), state)
+        want = expected(d, (1,) * N, False, False, backward=False)
+        assert ref.excess(h, want["h"], dtype) <= 1.0 and ref.excess(state, want["h"], "f32") <= 1.0
+        d["g"] = d["g"][:1].expand(N, D)
+        state = d["s0"].cuda()
+        h = P.glr_decode(d["x"].cuda(), d["g"][:1].cuda().expand(N, D), state)
+        want = expected(d, (1,) * N, False, False, backward=False)
+        assert ref.excess(h, want["h"], dtype) <= 1.0 and ref.excess(state, want["h"], "f32") <= 1.0
