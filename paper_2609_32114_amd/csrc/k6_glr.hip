@@ -6,11 +6,13 @@
 // long calls eight waves of 32 tokens, a lane to a channel, two workgroups a CU: what the
 // registers hold).  It is bound by HBM: x and g are read once and h written once, for some
 // 15 operations an element.  32768 tokens x 2048 channels, x in bf16 and g in fp32: 115 us,
-// 4.7 TB/s of the 537 MB that must move (a copy of 1 GiB 4.9 to 5.3 TB/s); the gate in bf16
-// 105 us.  What is left: a tile's loads, its wait for the state and its stores follow each
-// other, and two workgroups overlap them in part (of 119 us, at the time, 115 without the
-// wait and 100 without all but one in 32 of the stores).  Four or sixteen waves a
-// workgroup took 135 and 126 us there.
+// 4.7 TB/s of the 537 MB that must move (a copy of 1 GiB 4.9 to 5.3 TB/s), in convex form 121;
+// the gate in bf16 103 to 105 us, 3.9 TB/s; 32768 x 2000, whose rows do not begin at memory
+// lines, 163 us.  Of the forms of 32 tokens a wave, the raw convex ones and all bf16 ones but
+// those convex alone spill 4 to 7 of their 128 registers.  What is left: a tile's loads, its
+// wait for the state and its stores follow each other, and two workgroups overlap them in
+// part (of 119 us, at the time, 115 without the wait and 100 without all but one in 32 of the
+// stores).  Four or sixteen waves a workgroup took 135 and 126 us there.
 #include "glr.h"
 
 namespace hagdn {
@@ -235,8 +237,13 @@ template <typename T, typename G> struct Forward {
   // Beyond, few tiles keep the chain of states short, but there should be as many as CUs.
   // Tiles of 128 tokens instead of 256, us a call: 777 x 1280 11.2 and 14.6, 2048 x 2048
   // fp32 17.4 and 20.4, 8192 x 256 17.9 and 19.1; but 4096 x 2048 (512 tiles of 256) 25.9
-  // and 23.2, 32768 x 2048 157 and 119.  Where a long call has few channels its tiles all
-  // wait for each other: 50000 x 64 in tiles of 128, 256 and 512 54, 34 and 27.
+  // and 23.2, 32768 x 2048 157 and 119.  Of 64 instead of 128: 777 x 1280 10.6 and 11.2,
+  // 4096 x 256 16.8 and 15.0, 2048 x 2048 fp32 20.6 and 17.3.  Where a long call has few
+  // channels its tiles all wait for each other.  In tiles of 128, 256 (the better of 8 waves
+  // x 32 and 16 x 16) and 512:
+  //    8192 x 256   18.7  17.8  20.6      20000 x 128  27.2  21.2  22.0
+  //   10000 x 256   19.4  17.6  19.2      30000 x 128  36.3  25.7  23.6
+  //   16384 x 256   25.9  22.0  23.2      50000 x 64   52.9  33.5  27.4
   template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
     if (a.T <= 64) return tiled<RAW, CONVEX, 8, 8>(a, s);
     if (a.T <= 128) return tiled<RAW, CONVEX, 16, 8>(a, s);

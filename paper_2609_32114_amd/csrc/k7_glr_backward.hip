@@ -7,9 +7,10 @@
 // again in fp32 from the saved state before its first token, in the same registers and
 // with one more map a wave in LDS, which costs three operations an element and saves
 // reading h, and its rounding.  Bound by HBM: x, g and dh are read once, dx and dg written
-// once.  32768 tokens x 2048 channels, bf16 with an fp32 gate: 191 us, 4.9 TB/s of the
-// 940 MB that must move; the gate in bf16 181 us (3.7 TB/s: the same two workgroups a CU
-// hold fewer bytes in flight).
+// once.  32768 tokens x 2048 channels, bf16 with an fp32 gate: 190 us, 4.9 TB/s of the
+// 940 MB that must move, in convex form 202; the gate in bf16 163 us and, raw and convex,
+// 181 (4.1 and 3.7 TB/s: the same two workgroups a CU hold fewer bytes in flight).  The raw
+// and the convex forms spill 7 to 11 of their 128 registers.
 #include "glr.h"
 
 namespace hagdn {
@@ -241,7 +242,9 @@ template <typename T, typename G> struct Backward {
     return hipGetLastError();
   }
   // Tiles of 128 tokens; of 256 where that makes one tile of a call, and where a long call
-  // has so few channels that its tiles all wait for each other (forward: k6_glr.hip).
+  // has so few channels that its tiles all wait for each other (forward: k6_glr.hip).  Tiles
+  // of 128 and 256, us a call: 4096 x 256 15.9 and 17.1, 6000 x 128 17.4 and 17.5, 8192 x 256
+  // 20.3 and 19.4, 10000 x 256 22.2 and 20.2, 20000 x 128 30.6 and 24.5, 50000 x 64 57.9 and 37.7.
   template <bool RAW, bool CONVEX> static hipError_t go(const GlrArgs &a, hipStream_t s) {
     const bool narrow = a.T > 8192 && glr_tiles(a, 128) <= 2 * glr_cus(a);
     return (a.T > 128 && a.T <= 256) || narrow ? tiled<RAW, CONVEX, 16, 16>(a, s) : tiled<RAW, CONVEX, 16, 8>(a, s);

@@ -313,10 +313,12 @@ __global__ __launch_bounds__(forward_threads<LANES>()) void add_norm_kernel(AddN
 // serves the row.
 // The operands stay as they were loaded (bf16 ones two to a register), the weights in
 // registers for all of the workgroup's rows.  READS_X: a scale vector or post_weight is
-// there.  8192 rows of 2048 in bf16 with both 49 us, 4.1 TB/s, of which 5 the sum over the
-// workgroups; without them 39 us, 4.3 TB/s.  Bound by the rows' way through their sums and
-// barrier, which eight waves a CU overlap in part: sixteen, which spill, took 98 us; with
-// one row a turn 51, and the operands of two or three rows fetched ahead no less.
+// there.  8192 rows of 2048 in bf16 with both 48 us, 4.2 TB/s, of which 5 the sum over the
+// workgroups; without them 38 us, 4.4 TB/s.  2000 rows of 8192 68 us with both, 44 without;
+// of 16384, where a lane has two chunks and 1024 lanes leave it 128 registers, 400 (half a
+// KiB a lane spilled) and 82.  Bound by the rows' way through their sums and barrier, which
+// eight waves a CU overlap in part: at 8192 x 2048 sixteen, which spill, took 98 us; with one
+// row a turn 51, and the operands of two or three rows fetched ahead no less.
 template <typename T, typename R, int VE, int LANES, int C, bool READS_X>
 __global__ __launch_bounds__(backward_threads<LANES>(),
                              LANES > 512 || (!READS_X && rows_per_turn<T, R, LANES>() == 1) ? 4 : 2)
