@@ -92,7 +92,8 @@ typedef enum { HAGDN_F32 = 0, HAGDN_BF16 = 1 } hagdn_dtype;
 typedef enum {
   HAGDN_DEV_OK = 0,
   HAGDN_DEV_BAD_SEQLENS = 1,
-  HAGDN_DEV_WAIT_TIMEOUT = 2
+  HAGDN_DEV_WAIT_TIMEOUT = 2,
+  HAGDN_DEV_POOL_FULL = 3 /* hagdn_pool_fork: children without a free slot */
 } hagdn_device_code;
 
 /* Bytes of device workspace gdn_prefill needs for these sizes (0 if the
@@ -304,7 +305,11 @@ int hagdn_add_norm_backward(const void *dy, int64_t dy_stride, const void *dres,
  * and head, y = norm(o) weight act(z): o, z, y [T, H, d] dtype, weight [d].  o and z
  * (and dy) have a token stride in elements, a token's H x d elements being
  * contiguous.  activation: */
-typedef enum { HAGDN_ACT_SILU = 0, HAGDN_ACT_SIGMOID = 1 } hagdn_activation;
+typedef enum {
+  HAGDN_ACT_SILU = 0,
+  HAGDN_ACT_SIGMOID = 1, /* gate_norm only */
+  HAGDN_ACT_NONE = 2     /* the convolution only */
+} hagdn_activation;
 int hagdn_gate_norm(const void *o, int64_t o_stride, const void *z, int64_t z_stride,
                     const float *weight, float eps, int T, int H, int d, int dtype,
                     int activation, void *y, void *stream);
@@ -317,6 +322,143 @@ int hagdn_gate_norm_backward(const void *dy, int64_t dy_stride, const void *o,
                              const float *weight, float eps, int T, int H, int d, int dtype,
                              int activation, void *d_o, void *d_z, float *dweight,
                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Short causal convolution: the channelwise one of W taps that stands before a
+ * recurrent mixer (before q, k and v of the delta-rule layers, before the scan below),
+ * over packed sequences, with its backward pass and a step for single tokens,
+ *   p_t = bias + sum_j weight[:, j] x_{t-W+1+j},   y_t = act(p_t).
+ * The W - 1 inputs before a sequence are its window; the last W - 1 of window and
+ * sequence are the window that continues it.
+ * The conventions of the gated linear recurrence hold (row strides, element alignment,
+ * contiguous outputs, cu_seqlens NULL for N = 1, malformed ones), with
+ *   weight [D, W] and bias [D] (or NULL) fp32, W = 2 .. 8, D = 1 .. 2^28;
+ *   windows [N, W - 1, D] dtype, oldest input first; w0 NULL: zeros;
+ *   activation HAGDN_ACT_SILU or HAGDN_ACT_NONE.
+ * Sums are fp32.  Outputs must not overlap inputs (w_final not even w0 exactly: other
+ * workgroups read that window while one writes it).  Results repeat bit for bit. */
+
+/* Bytes of workspace (0 on invalid sizes); backward 1: of hagdn_conv_backward. */
+size_t hagdn_conv_workspace_size(int T_total, int D, int W, int backward);
+
+/* y [T, D] and, unless NULL, w_final [N, W - 1, D]. */
+int hagdn_conv_prefill(const void *x, int64_t x_stride, const float *weight, const float *bias,
+                       const void *w0, const int32_t *cu_seqlens, int N, int T_total, int D, int W,
+                       int dtype, int activation, void *y, void *w_final, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/* Backward, from dy and dfinal [N, W - 1, D] dtype (NULL: zero), the gradient of
+ * w_final: dx [T, D]; dweight [D, W] and dbias [D] (NULL without a bias) fp32; dw0
+ * [N, W - 1, D] dtype, or NULL. */
+int hagdn_conv_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                        const float *weight, const float *bias, const void *w0,
+                        const void *dfinal, const int32_t *cu_seqlens, int N, int T_total, int D,
+                        int W, int dtype, int activation, void *dx, float *dweight, float *dbias,
+                        void *dw0, void *workspace, size_t workspace_bytes, void *stream);
+
+/* One token for each of N sequences: the windows in the pool state [num_slots, W - 1, D]
+ * dtype move on in place; y [N, D].  slots as in gdn_decode (padding: a row of zeros). */
+int hagdn_conv_decode(const void *x, int64_t x_stride, const float *weight, const float *bias,
+                      void *state, const int32_t *slots, int num_slots, int N, int D, int W,
+                      int dtype, int activation, void *y, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Selective state space scan: a recurrent mixer of D channels with S states each, whose
+ * step sizes dt_t (a channel) and input and output maps B_t, C_t (S states, shared by the
+ * D / G channels of a group: channel d uses group d / (D / G)) depend on the token,
+ *   h_t = e^(dt_t A) h_{t-1} + dt_t x_t B_t,   y_t = (C_t . h_t + skip x_t) silu(z_t),
+ * over packed sequences, with its backward pass and a step for single tokens.
+ * The conventions of the gated linear recurrence hold, with
+ *   x, z, y [T, D] dtype; z NULL: no gate;
+ *   dt [T, D] dt_dtype: HAGDN_F32, or (with dtype bf16 only) HAGDN_BF16.  Under
+ *   pre = HAGDN_PRE_GATE_SOFTPLUS it holds raw values r: the step size is
+ *   log(1 + e^(r + dt_bias)); dt_bias [D] fp32 or NULL, and NULL without that flag;
+ *   B, C [T, G, S] dtype, a token's G x S elements contiguous (B_stride, C_stride:
+ *   between tokens);
+ *   A [D, S], skip [D] (or NULL) fp32;  S = 1 .. 64;  D % G == 0;
+ *   states [N, D, S] fp32; s0 NULL: zero.
+ * dt A <= 0 is expected: where a chunk of up to 256 tokens lets a state grow by e^88
+ * results are unspecified.  N x D x S below 2^31.  Sums and states are fp32.  Outputs must
+ * not overlap inputs (s_final not even s0 exactly, nor ds0 dfinal).  Results repeat bit
+ * for bit on one device.  No value of one sequence reaches another. */
+
+/* Bytes of workspace (0 on invalid sizes); backward 1: of ssm_backward. */
+size_t ssm_workspace_size(int T_total, int D, int S, int G, int backward);
+
+/* Forward.  checkpoints: NULL, or fp32 of ssm_checkpoints_size() elements, what
+ * ssm_backward needs of the forward pass (states before every 32nd token, for S > 16
+ * before every 16th and for S > 32 every 8th). */
+size_t ssm_checkpoints_size(int T_total, int D, int S);
+int ssm_prefill(const void *x, int64_t x_stride, const void *dt, int64_t dt_stride,
+                const float *A, const void *B, int64_t B_stride, const void *C, int64_t C_stride,
+                const float *skip, const void *z, int64_t z_stride, const float *dt_bias,
+                const float *s0, const int32_t *cu_seqlens, int N, int T_total, int D, int S, int G,
+                int dtype, int dt_dtype, int pre, void *y, float *s_final, float *checkpoints,
+                void *workspace, size_t workspace_bytes, void *stream);
+
+/* Backward, from dy and dfinal [N, D, S] fp32 (NULL: zero): the gradients of the inputs
+ * in their types, contiguous: dx, ddt (of dt as given), dz (NULL without z), dB, dC
+ * [T, G, S]; fp32: dA [D, S], dskip [D] (NULL without skip), d_dt_bias [D] (NULL without
+ * dt_bias), ds0 [N, D, S] or NULL. */
+int ssm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                 const void *dt, int64_t dt_stride, const float *A, const void *B,
+                 int64_t B_stride, const void *C, int64_t C_stride, const float *skip,
+                 const void *z, int64_t z_stride, const float *dt_bias, const float *checkpoints,
+                 const float *s0, const float *dfinal, const int32_t *cu_seqlens, int N,
+                 int T_total, int D, int S, int G, int dtype, int dt_dtype, int pre, void *dx,
+                 void *ddt, float *dA, void *dB, void *dC, float *dskip, void *dz,
+                 float *d_dt_bias, float *ds0, void *workspace, size_t workspace_bytes,
+                 void *stream);
+
+/* One token for each of N sequences: state [num_slots, D, S] fp32 is updated in place;
+ * y [N, D].  slots as in gdn_decode (padding: a row of zeros). */
+int ssm_decode(const void *x, int64_t x_stride, const void *dt, int64_t dt_stride, const float *A,
+               const void *B, int64_t B_stride, const void *C, int64_t C_stride,
+               const float *skip, const void *z, int64_t z_stride, const float *dt_bias,
+               float *state, const int32_t *slots, int num_slots, int N, int D, int S, int G,
+               int dtype, int dt_dtype, int pre, void *y, void *stream);
+
+/* ------------------------------------------------------------------------
+ * State pools.  The decode entry points keep their sequences' states in rows of pools;
+ * these move rows, of many pools (the layers' states and windows) in one call.
+ *   pools       host array of device pointers, 1 .. 1024 of them; row r of pool p begins at
+ *               pools[p] + r x row_bytes[p], row_bytes >= 1.  Pools must not overlap each
+ *               other.  Any alignment (rows and pointers of 16 bytes are the fastest).
+ *   slots, tables  int32 DEVICE memory. */
+
+/* Row dst_slots[i] of every pool receives row src_slots[i], i < n; a NULL table: row i.
+ *   sources     NULL: rows of the same pools, as if all were read before any is written
+ *               (n at most 8192); else the rows are taken from these (src_rows rows of
+ *               row_bytes[p] each), which overlap no pool.
+ * A destination outside [0, dst_rows) is padding: nothing is copied.  A source outside
+ * [0, src_rows) gives a row of zeros, the state of a new sequence (without sources
+ * src_rows is taken as dst_rows).  No two entries may name one destination (which of the
+ * two it holds afterwards is unspecified, byte by byte). */
+int hagdn_pool_copy(void *const *pools, const void *const *sources, const size_t *row_bytes,
+                    int num_pools, const int32_t *dst_slots, const int32_t *src_slots, int n,
+                    int dst_rows, int src_rows, void *stream);
+
+/* Beam search's step: child i of M goes on from sequence parents[i] of N, whose state is
+ * in slot slots[..].  The first child of a slot stays in it; each other one, in order, gets
+ * the lowest slot that no child stays in, and a copy of its parent's rows.  So the
+ * slots of sequences that no child goes on from are free, like all that `slots` does not
+ * name: the children must be all that the pools hold.  new_slots [M] receives the
+ * children's slots, -1 for a parent outside [0, N) or in no slot of the pools, and for
+ * children beyond the free slots (hagdn_device_status: HAGDN_DEV_POOL_FULL).  new_slots
+ * must not overlap slots or parents.
+ * Rows that are free afterwards keep what they held. */
+size_t hagdn_pool_workspace_size(int num_slots);
+int hagdn_pool_fork(void *const *pools, const size_t *row_bytes, int num_pools,
+                    const int32_t *slots, int N, const int32_t *parents, int M, int num_slots,
+                    int32_t *new_slots, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The states that the table slots [N] names move to the front of the pools: with L live
+ * slots, those from L on move, in order, to the free ones below L.  new_slots [N] (it may be
+ * slots itself) receives the table after it; entries outside the pools (padding, ended
+ * sequences) stay as they are.  Entries that name one slot still name one. */
+int hagdn_pool_compact(void *const *pools, const size_t *row_bytes, int num_pools,
+                       const int32_t *slots, int N, int num_slots, int32_t *new_slots,
+                       void *workspace, size_t workspace_bytes, void *stream);
 
 /* Message for the last non-OK return on this host thread ("" if none). */
 const char *hagdn_last_error(void);

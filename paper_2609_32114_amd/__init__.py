@@ -23,7 +23,10 @@ pool in place.
 The operators around these layers are bound in ``layer.py``: a channelwise gated
 linear recurrence (``glr_prefill``, ``glr_backward``, ``glr_decode``) and the norms
 before and after a block (``add_norm``, ``gate_norm`` and their backward
-passes); ``autograd.py`` has differentiable forms of them.
+passes).  ``mixer.py`` binds a second family of mixers, a short causal convolution
+(``conv_*``) and a selective state space scan (``ssm_*``), and ``pools.py`` the copies,
+forks and compaction of state pools (``pool_*``).  ``autograd.py`` has
+differentiable forms of the recurrence, the norms, the convolution and the scan.
 """
 
 from __future__ import annotations
@@ -37,14 +40,17 @@ __all__ = ["gdn_prefill", "kda_prefill", "gdn_decode", "kda_decode", "workspace_
            "segment_chunks", "segment_chunks_for", "workspace_region", "measure_copy", "measure_mfma",
            "HagdnError",
            "glr_prefill", "glr_backward", "glr_decode", "glr_workspace_size", "add_norm", "add_norm_backward",
-           "gate_norm", "gate_norm_backward"]
+           "gate_norm", "gate_norm_backward",
+           "conv_prefill", "conv_backward", "conv_decode", "conv_workspace_size", "ssm_prefill", "ssm_backward",
+           "ssm_decode", "ssm_workspace_size", "ssm_checkpoints_size", "pool_copy", "pool_fork", "pool_compact",
+           "pool_workspace_size"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libhagdn.so")
 _lib = None
 
 HAGDN_F32, HAGDN_BF16 = 0, 1
-DEV_OK, DEV_BAD_SEQLENS, DEV_WAIT_TIMEOUT = 0, 1, 2
+DEV_OK, DEV_BAD_SEQLENS, DEV_WAIT_TIMEOUT, DEV_POOL_FULL = 0, 1, 2, 3
 # preprocessing flags (hagdn_pre_flags)
 PRE_QK_L2NORM, PRE_GATE_SOFTPLUS, PRE_BETA_SIGMOID = 1, 2, 4
 PRE_ALL = 7
@@ -100,6 +106,23 @@ _SYMBOLS = {
     "hagdn_gate_norm_workspace_size": (ctypes.c_size_t, [ctypes.c_int] * 3),
     "hagdn_gate_norm_backward": (ctypes.c_int, _ROWS * 3 + _P + [ctypes.c_float] + [ctypes.c_int] * 5 + _P * 4 +
                                  [ctypes.c_size_t] + _P),
+    "hagdn_conv_workspace_size": (ctypes.c_size_t, [ctypes.c_int] * 4),
+    "hagdn_conv_prefill": (ctypes.c_int, _ROWS + _P * 4 + [ctypes.c_int] * 6 + _P * 3 + [ctypes.c_size_t] + _P),
+    "hagdn_conv_backward": (ctypes.c_int, _ROWS * 2 + _P * 5 + [ctypes.c_int] * 6 + _P * 5 + [ctypes.c_size_t] + _P),
+    "hagdn_conv_decode": (ctypes.c_int, _ROWS + _P * 4 + [ctypes.c_int] * 6 + _P * 2),
+    "ssm_workspace_size": (ctypes.c_size_t, [ctypes.c_int] * 5),
+    "ssm_checkpoints_size": (ctypes.c_size_t, [ctypes.c_int] * 3),
+    "ssm_prefill": (ctypes.c_int, _ROWS * 2 + _P + _ROWS * 2 + _P + _ROWS + _P * 3 + [ctypes.c_int] * 8 + _P * 4 +
+                    [ctypes.c_size_t] + _P),
+    "ssm_backward": (ctypes.c_int, _ROWS * 3 + _P + _ROWS * 2 + _P + _ROWS + _P * 5 + [ctypes.c_int] * 8 + _P * 10 +
+                     [ctypes.c_size_t] + _P),
+    "ssm_decode": (ctypes.c_int, _ROWS * 2 + _P + _ROWS * 2 + _P + _ROWS + _P * 3 + [ctypes.c_int] * 8 + _P * 2),
+    "hagdn_pool_workspace_size": (ctypes.c_size_t, [ctypes.c_int]),
+    "hagdn_pool_copy": (ctypes.c_int, _P * 3 + [ctypes.c_int] + _P * 2 + [ctypes.c_int] * 3 + _P),
+    "hagdn_pool_fork": (ctypes.c_int, _P * 2 + [ctypes.c_int] + _P + [ctypes.c_int] + _P + [ctypes.c_int] * 2 + _P * 2 +
+                        [ctypes.c_size_t] + _P),
+    "hagdn_pool_compact": (ctypes.c_int, _P * 2 + [ctypes.c_int] + _P + [ctypes.c_int] * 2 + _P * 2 + [ctypes.c_size_t] +
+                           _P),
 }
 
 # workspace regions (hagdn_ws_region)
@@ -491,13 +514,19 @@ def profile_end():
 
 _LAYER = {"glr_prefill", "glr_backward", "glr_decode", "glr_workspace_size", "add_norm", "add_norm_backward",
           "gate_norm", "gate_norm_backward"}
+_MIXER = {"conv_prefill", "conv_backward", "conv_decode", "conv_workspace_size", "ssm_prefill", "ssm_backward",
+          "ssm_decode", "ssm_workspace_size", "ssm_checkpoints_size"}
+_POOLS = {"pool_copy", "pool_fork", "pool_compact", "pool_workspace_size"}
 
 
 def __getattr__(name):
-    """The operators of layer.py, bound on first use (that module imports torch)."""
-    if name not in _LAYER:
-        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
-    from . import layer
-    for n in _LAYER:
-        globals()[n] = getattr(layer, n)
-    return globals()[name]
+    """The operators of layer.py, mixer.py and pools.py, bound on first use (those modules
+    import torch)."""
+    for names, module in ((_LAYER, "layer"), (_MIXER, "mixer"), (_POOLS, "pools")):
+        if name in names:
+            import importlib
+            operators = importlib.import_module("." + module, __name__)
+            for n in names:
+                globals()[n] = getattr(operators, n)
+            return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,12 +1,16 @@
-"""Differentiable forms of the gated linear recurrence and the block norms.
+"""Differentiable forms of the gated linear recurrence, the block norms, the short
+convolution and the selective scan.
 
     h, final = glr(x, g, initial_state=None, cu_seqlens=None, convex=False, preprocess=0, workspace=None)
     y, res = add_norm(x, weight, residual=None, scale=1.0, post_weight=None, eps=1e-6)
     y = gate_norm(o, z, weight, activation="silu", eps=1e-6)
+    y, window = conv(x, weight, bias=None, initial_window=None, cu_seqlens=None, activation="silu", workspace=None)
+    y, final = ssm(x, dt, A, B, C, skip=None, z=None, dt_bias=None, initial_state=None, cu_seqlens=None,
+                   preprocess=0, workspace=None)
 
-The arguments of the functions of the same (or, for glr, the prefill's) name; both
-directions run in the library's kernels.  Kept for the backward pass: the operands and
-the saved states (glr), the residual stream that add_norm returned, and x where a scale
+The arguments of the functions of the same (or, for glr, conv and ssm, the prefill's) name;
+both directions run in the library's kernels.  Kept for the backward pass: the operands and
+the saved states (glr, ssm), the residual stream that add_norm returned, and x where a scale
 vector or post_weight is there.  There are first derivatives only: differentiating the
 gradients again (create_graph=True, then a second backward pass) raises.
 """
@@ -15,7 +19,7 @@ from __future__ import annotations
 
 import torch
 
-from . import layer
+from . import layer, mixer
 
 
 def _rows(t):
@@ -33,8 +37,8 @@ class _Gradients(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *grads):
-        raise RuntimeError("the recurrence and the block norms have no second derivative: their gradients come "
-                           "from kernels and cannot be differentiated again")
+        raise RuntimeError("the recurrence, the block norms, the convolution and the scan have no second derivative: "
+                           "their gradients come from kernels and cannot be differentiated again")
 
 
 def _gradients(kernels, *args):
@@ -102,6 +106,48 @@ class _GateNorm(torch.autograd.Function):
         return do, dz, dw, None, None
 
 
+class _Conv(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, initial_window, cu_seqlens, activation, workspace):
+        y, window = mixer.conv_prefill(x, weight, bias, initial_window, cu_seqlens, activation, workspace=workspace)
+        ctx.save_for_backward(x, weight, bias, initial_window, cu_seqlens)
+        ctx.how = (activation, workspace)
+        ctx.set_materialize_grads(False)
+        return y, window
+
+    @staticmethod
+    def backward(ctx, dy, dwindow):
+        x, weight, bias, w0, cu = ctx.saved_tensors
+        if dy is None and dwindow is None:
+            return None, None, None, None, None, None, None
+        dy = torch.zeros_like(x) if dy is None else _rows(dy)
+        dwindow = None if dwindow is None else dwindow.contiguous()
+        dx, dw, db, dw0 = _gradients(mixer.conv_backward, dy, x, weight, bias, w0, dwindow, cu, *ctx.how)
+        return dx, dw, db, dw0, None, None, None
+
+
+class _Ssm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, dt, A, B, C, skip, z, dt_bias, initial_state, cu_seqlens, preprocess, workspace):
+        y, final, saved = mixer.ssm_prefill(x, dt, A, B, C, skip, z, dt_bias, initial_state, cu_seqlens, preprocess,
+                                            output_checkpoints=True, workspace=workspace)
+        ctx.save_for_backward(x, dt, A, B, C, saved, skip, z, dt_bias, initial_state, cu_seqlens)
+        ctx.how = (preprocess, workspace)
+        ctx.set_materialize_grads(False)
+        return y, final
+
+    @staticmethod
+    def backward(ctx, dy, dfinal):
+        x, dt, A, B, C, saved, skip, z, dt_bias, s0, cu = ctx.saved_tensors
+        if dy is None and dfinal is None:
+            return (None,) * 12
+        dy = torch.zeros_like(x) if dy is None else _rows(dy)
+        dfinal = None if dfinal is None else dfinal.contiguous()
+        dx, ddt, dA, dB, dC, dskip, dz, dbias, ds0 = _gradients(
+            mixer.ssm_backward, dy, x, dt, A, B, C, saved, skip, z, dt_bias, s0, dfinal, cu, *ctx.how)
+        return dx, ddt, dA, dB, dC, dskip, dz, dbias, ds0, None, None, None
+
+
 def glr(x, g, initial_state=None, cu_seqlens=None, convex=False, preprocess=0, workspace=None):
     """Differentiable glr_prefill: (h, final state).  Both directions use ``workspace``
     where one is given, and leave their device status in it."""
@@ -116,3 +162,16 @@ def add_norm(x, weight, residual=None, scale=1.0, post_weight=None, eps=1e-6):
 def gate_norm(o, z, weight, activation="silu", eps=1e-6):
     """Differentiable gate_norm."""
     return _GateNorm.apply(o, z, weight, activation, eps)
+
+
+def conv(x, weight, bias=None, initial_window=None, cu_seqlens=None, activation="silu", workspace=None):
+    """Differentiable conv_prefill: (y, final window).  A ``workspace`` must suffice for
+    conv_backward."""
+    return _Conv.apply(x, weight, bias, initial_window, cu_seqlens, activation, workspace)
+
+
+def ssm(x, dt, A, B, C, skip=None, z=None, dt_bias=None, initial_state=None, cu_seqlens=None, preprocess=0,
+        workspace=None):
+    """Differentiable ssm_prefill: (y, final state).  A ``workspace`` must suffice for
+    ssm_backward."""
+    return _Ssm.apply(x, dt, A, B, C, skip, z, dt_bias, initial_state, cu_seqlens, preprocess, workspace)

@@ -1,0 +1,253 @@
+// k12_pool.hip -- copies between rows of state pools, and the plans that say which rows a
+// fork or a compaction moves.  Copies are bound by HBM: every moved byte is read once and
+// written once, all pools of a call in one launch.
+#include "device.h"
+#include "mixer.h"
+#include "prefill.h"
+
+namespace hagdn {
+
+template <int UNIT> struct Unit;
+template <> struct Unit<16> { using type = u32x4; };
+template <> struct Unit<8> { using type = uint64_t; };
+template <> struct Unit<4> { using type = uint32_t; };
+template <> struct Unit<2> { using type = uint16_t; };
+template <> struct Unit<1> { using type = uint8_t; };
+
+constexpr int kPieces = 8;  // units a thread moves at once
+
+// Row of entry i, or -1: none (a null table: row i).
+__device__ __forceinline__ int row_of(const int32_t *table, int rows, int i) {
+  const int r = table ? table[i] : i;
+  return r >= 0 && r < rows ? r : -1;
+}
+
+// Rows that no other entry of the call writes or reads: a workgroup moves a piece of one
+// row after another.  A source outside its rows gives zeros.
+template <int UNIT> __global__ __launch_bounds__(256) void pool_move_kernel(PoolCopyArgs a) {
+  using U = typename Unit<UNIT>::type;
+  constexpr uint64_t kSpan = 256 * kPieces;  // units of a piece
+  uint64_t pieces = 0;                       // of one entry, over all pools
+  for (int p = 0; p < a.count; ++p) pieces += (a.pools[p].row / UNIT + kSpan - 1) / kSpan;
+  const int n = a.moves ? a.moves[0] : a.n;
+  for (uint64_t item = blockIdx.x; item < pieces * n; item += gridDim.x) {
+    const int i = (int)(item / pieces);
+    uint64_t at = item - (uint64_t)i * pieces;
+    int p = 0;
+    for (;; ++p) {
+      const uint64_t here = (a.pools[p].row / UNIT + kSpan - 1) / kSpan;
+      if (at < here) break;
+      at -= here;
+    }
+    const int dst = a.moves ? a.moves[1 + 2 * i] : row_of(a.dst, a.dst_rows, i);
+    const int src = a.moves ? a.moves[2 + 2 * i] : row_of(a.src, a.src_rows, i);
+    if (dst < 0) continue;
+    const uint64_t units = a.pools[p].row / UNIT, first = at * kSpan + threadIdx.x;
+    const U *from = static_cast<const U *>(a.pools[p].from) + (src < 0 ? 0 : (uint64_t)src * units);
+    U *to = static_cast<U *>(a.pools[p].to) + (uint64_t)dst * units;
+    U v[kPieces] = {};
+    if (src >= 0) {
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k)
+        if (first + k * 256 < units) v[k] = __builtin_nontemporal_load(from + first + k * 256);
+    }
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+      if (first + k * 256 < units) __builtin_nontemporal_store(v[k], to + first + k * 256);
+  }
+}
+
+// Rows of the same pools, as if all were read before any is written: a workgroup has a span
+// of bytes of every entry's row, all of them in registers between its loads and its stores.
+template <int UNIT, int THREADS> __global__ __launch_bounds__(THREADS) void pool_shuffle_kernel(PoolCopyArgs a, uint32_t width) {
+  using U = typename Unit<UNIT>::type;
+  uint64_t spans = 0;
+  for (int p = 0; p < a.count; ++p) spans += (a.pools[p].row / UNIT + width - 1) / width;
+  for (uint64_t item = blockIdx.x; item < spans; item += gridDim.x) {
+    uint64_t at = item;
+    int p = 0;
+    for (;; ++p) {
+      const uint64_t here = (a.pools[p].row / UNIT + width - 1) / width;
+      if (at < here) break;
+      at -= here;
+    }
+    const uint64_t units = a.pools[p].row / UNIT;
+    U *pool = static_cast<U *>(a.pools[p].to);
+    U v[kPieces] = {};
+    int dst[kPieces];
+    uint64_t col[kPieces];
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const uint32_t e = k * THREADS + threadIdx.x, i = e / width;  // n x width <= THREADS x kPieces
+      col[k] = at * width + (e - i * width);
+      dst[k] = -1;
+      if (i >= (uint32_t)a.n || col[k] >= units) continue;
+      dst[k] = row_of(a.dst, a.dst_rows, (int)i);
+      const int src = row_of(a.src, a.src_rows, (int)i);
+      if (dst[k] >= 0 && src >= 0) v[k] = pool[(uint64_t)src * units + col[k]];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+      if (dst[k] >= 0) pool[(uint64_t)dst[k] * units + col[k]] = v[k];
+    __syncthreads();
+  }
+}
+
+// Exclusive prefix sums of one flag a thread over a workgroup of 1024, and their total.
+__device__ __forceinline__ int prefix(bool flag, int (&waves)[16], int &total) {
+  const uint64_t bits = __ballot(flag);
+  const int wave = threadIdx.x >> 6;
+  __syncthreads();  // the last call's sums have been read
+  if (lane_id() == 0) waves[wave] = __popcll(bits);
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    before += w < wave ? waves[w] : 0;
+    total += waves[w];
+  }
+  return before + __popcll(bits & ((1ull << lane_id()) - 1));
+}
+
+// The workgroup's stores and atomics in memory are done and seen by all of it.
+__device__ __forceinline__ void settle() {
+  __threadfence();
+  __syncthreads();
+}
+
+// mark[slot]: the first child that goes on from the parent there, or none.  That child
+// stays; the k-th of the others gets the k-th slot without a mark.
+constexpr int kNobody = 0x7fffffff;
+__global__ __launch_bounds__(1024) void pool_fork_plan_kernel(PoolPlanArgs a) {
+  __shared__ int sWaves[16];
+  const int t = threadIdx.x;
+  const auto source = [&](int i) {
+    const int p = a.parents[i];
+    return p >= 0 && p < a.N ? row_of(a.slots, a.num_slots, p) : -1;
+  };
+  for (int i = t; i < a.num_slots; i += 1024) a.mark[i] = kNobody;
+  settle();
+  for (int i = t; i < a.M; i += 1024) {
+    const int s = source(i);
+    if (s >= 0) atomicMin(a.mark + s, i);
+  }
+  settle();
+  int moves = 0, total;
+  for (int base = 0; base < a.M; base += 1024) {  // the sources, in the children's order
+    const int i = base + t, s = i < a.M ? source(i) : -1;
+    const bool moved = s >= 0 && a.mark[s] != i;
+    const int k = moves + prefix(moved, sWaves, total);
+    if (moved) a.moves[2 + 2 * k] = s;
+    moves += total;
+  }
+  int free_slots = 0;
+  for (int base = 0; base < a.num_slots && free_slots < moves; base += 1024) {  // the free slots, in their order
+    const int i = base + t;
+    const bool free_slot = i < a.num_slots && a.mark[i] == kNobody;
+    const int k = free_slots + prefix(free_slot, sWaves, total);
+    if (free_slot && k < moves) a.moves[1 + 2 * k] = i;
+    free_slots += total;
+  }
+  settle();
+  const int done = min(moves, free_slots);
+  int seen = 0;
+  for (int base = 0; base < a.M; base += 1024) {  // the children's slots
+    const int i = base + t, s = i < a.M ? source(i) : -1;
+    const bool moved = s >= 0 && a.mark[s] != i;
+    const int k = seen + prefix(moved, sWaves, total);
+    if (i < a.M) a.out[i] = !moved ? s : k < done ? a.moves[1 + 2 * k] : -1;
+    seen += total;
+  }
+  if (t == 0) {
+    a.moves[0] = done;
+    *a.status = moves > done ? kDevPoolFull : 0;
+  }
+}
+
+// mark[slot]: the slot that its state is in afterwards.
+__global__ __launch_bounds__(1024) void pool_compact_plan_kernel(PoolPlanArgs a) {
+  __shared__ int sWaves[16];
+  const int t = threadIdx.x;
+  for (int i = t; i < a.num_slots; i += 1024) a.mark[i] = -1;
+  settle();
+  for (int i = t; i < a.N; i += 1024) {
+    const int s = row_of(a.slots, a.num_slots, i);
+    if (s >= 0) a.mark[s] = s;
+  }
+  settle();
+  int live = 0, total;
+  for (int base = 0; base < a.num_slots; base += 1024) {
+    prefix(base + t < a.num_slots && a.mark[base + t] >= 0, sWaves, total);
+    live += total;
+  }
+  int holes = 0, moves = 0;
+  for (int base = 0; base < live; base += 1024) {  // free slots among the first `live`
+    const int i = base + t;
+    const bool hole = i < live && a.mark[i] < 0;
+    const int k = holes + prefix(hole, sWaves, total);
+    if (hole) a.moves[1 + 2 * k] = i;
+    holes += total;
+  }
+  settle();
+  for (int base = live; base < a.num_slots; base += 1024) {  // as many states lie beyond them
+    const int i = base + t;
+    const bool moved = i < a.num_slots && a.mark[i] >= 0;
+    const int k = moves + prefix(moved, sWaves, total);
+    if (moved) {
+      a.moves[2 + 2 * k] = i;
+      a.mark[i] = a.moves[1 + 2 * k];
+    }
+    moves += total;
+  }
+  settle();
+  for (int i = t; i < a.N; i += 1024) {
+    const int s = row_of(a.slots, a.num_slots, i);
+    a.out[i] = s >= 0 ? a.mark[s] : a.slots[i];
+  }
+  if (t == 0) {
+    a.moves[0] = moves;
+    *a.status = 0;
+  }
+}
+
+hipError_t launch_pool_fork_plan(const PoolPlanArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL(pool_fork_plan_kernel, dim3(1), dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t launch_pool_compact_plan(const PoolPlanArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL(pool_compact_plan_kernel, dim3(1), dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int UNIT> hipError_t pool_copy(const PoolCopyArgs &a, bool in_place, int cus, hipStream_t s) {
+  const uint64_t most = 16ull * (cus > 0 ? cus : 256);  // workgroups
+  if (!in_place) {
+    uint64_t pieces = 0;
+    for (int p = 0; p < a.count; ++p) pieces += (a.pools[p].row / UNIT + 256 * kPieces - 1) / (256 * kPieces);
+    const uint64_t items = pieces * (uint64_t)a.n;
+    hipLaunchKernelGGL((pool_move_kernel<UNIT>), dim3((unsigned)(items < most ? items : most)), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
+  const bool many = a.n > 256 * kPieces;
+  const uint32_t width = (many ? 1024u : 256u) * kPieces / (uint32_t)a.n;  // n <= kMaxMovesInPlace
+  uint64_t spans = 0;
+  for (int p = 0; p < a.count; ++p) spans += (a.pools[p].row / UNIT + width - 1) / width;
+  const dim3 grid((unsigned)(spans < most ? spans : most));
+  if (many) hipLaunchKernelGGL((pool_shuffle_kernel<UNIT, 1024>), grid, dim3(1024), 0, s, a, width);
+  else hipLaunchKernelGGL((pool_shuffle_kernel<UNIT, 256>), grid, dim3(256), 0, s, a, width);
+  return hipGetLastError();
+}
+
+hipError_t launch_pool_copy(const PoolCopyArgs &a, bool in_place, int cus, hipStream_t s) {
+  switch (a.unit) {
+    case 16: return pool_copy<16>(a, in_place, cus, s);
+    case 8: return pool_copy<8>(a, in_place, cus, s);
+    case 4: return pool_copy<4>(a, in_place, cus, s);
+    case 2: return pool_copy<2>(a, in_place, cus, s);
+    default: return pool_copy<1>(a, in_place, cus, s);
+  }
+}
+
+}  // namespace hagdn

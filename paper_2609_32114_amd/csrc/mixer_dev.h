@@ -1,0 +1,117 @@
+// mixer_dev.h -- device parts shared by the short convolution and the selective scan:
+// activations, elements at any alignment, and the walk over packed sequences.
+#pragma once
+
+#include "device.h"
+#include "mixer.h"
+#include "prefill.h"
+
+namespace hagdn {
+
+constexpr float kLog2e = 1.44269504f;
+
+// 1 / (1 + e^-v), and its complement, both from e^-|v|, so that nothing overflows and
+// neither loses digits.  The hardware's 2^x and reciprocal: an ulp each, and |v| 2^-24 of
+// the exponent's product.
+struct Logistic {
+  float s, rest;
+};
+__device__ __forceinline__ Logistic logistic(float v) {
+  const float t = __builtin_amdgcn_exp2f(-__builtin_fabsf(v) * kLog2e);
+  const float r = __builtin_amdgcn_rcpf(1.f + t), tr = t * r;
+  return {v > 0.f ? r : tr, v > 0.f ? tr : r};
+}
+__device__ __forceinline__ float silu(float v) { return v * logistic(v).s; }
+
+// log(1 + e^v) = max(v, 0) + log1p(t), t = e^-|v|, with log1p(t) = 2 artanh(r), r = t / (2 + t)
+// in [0, 1/3]: r times a polynomial in r^2 through the degree 5 Chebyshev nodes of
+// [0, 1/9] (relative error 2^-33).  Every term is positive, so that small results, steps of
+// 1e-3 and less, keep their digits.
+__device__ __forceinline__ float softplus(float v) {
+  const float t = __builtin_amdgcn_exp2f(-__builtin_fabsf(v) * kLog2e);
+  const float r = t * __builtin_amdgcn_rcpf(2.f + t), q = r * r;
+  float p = 0.24393908f;
+  p = __builtin_fmaf(p, q, 0.21398561f);
+  p = __builtin_fmaf(p, q, 0.28620207f);
+  p = __builtin_fmaf(p, q, 0.39998711f);
+  p = __builtin_fmaf(p, q, 0.66666679f);
+  p = __builtin_fmaf(p, q, 2.f);
+  return __builtin_fmaf(r, p, v > 0.f ? v : 0.f);
+}
+
+// V consecutive elements, aligned as one of them is.
+template <typename T, int V> struct __attribute__((packed, aligned(sizeof(T)))) Pack {
+  T v[V];
+};
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_pack(const void *base, size_t at) {
+  return *reinterpret_cast<const Pack<T, V> *>(static_cast<const T *>(base) + at);
+}
+template <typename T, int V> __device__ __forceinline__ void store_pack(void *base, size_t at, const Pack<T, V> &p) {
+  *reinterpret_cast<Pack<T, V> *>(static_cast<T *>(base) + at) = p;
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Whether cu[0 .. N] are the offsets of N sequences over T tokens; every thread of the
+// workgroup takes part and gets the answer.
+__device__ __forceinline__ bool offsets_ok(const int32_t *cu, int N, int T) {
+  if (!cu) return true;
+  int bad = 0;
+  for (int i = threadIdx.x; i < N; i += blockDim.x) bad |= cu[i] > cu[i + 1];
+  if (threadIdx.x == 0) bad |= cu[0] != 0 || cu[N] != T;
+  return !__syncthreads_or(bad);
+}
+
+// The sequence that a token belongs to, followed from one token to the next by a whole
+// wave.  The offsets must have been checked.
+struct Cursor {
+  const int32_t *cu;  // null: one sequence of all tokens
+  int N, T;
+  int seq, start, end;  // uniform over the wave
+  // The sequence of token t < T.  Each round of the search the lanes divide the range by 64.
+  __device__ Cursor(const int32_t *cu_, int N_, int T_, int t) : cu(cu_), N(N_), T(T_), seq(0), start(0), end(T_) {
+    if (!cu) return;
+    int lo = 0, len = N;  // the last sequence that starts at or before t is in [lo, lo + len)
+    const int lane = lane_id();
+    while (len > 1) {
+      const int step = (len + 63) / 64;
+      const long at = (long)lane * step;
+      const bool below = at < len && cu[lo + at] <= t;
+      const int count = __popcll(__ballot(below));
+      const int skip = count > 1 ? (count - 1) * step : 0;
+      lo += skip;
+      len = min(step, len - skip);
+    }
+    seq = uniform(lo);
+    start = uniform(cu[seq]);
+    end = uniform(cu[seq + 1]);
+  }
+  // To the sequence of the token after this one's last (which must exist).
+  __device__ void next() {
+    start = end;
+    do {
+      ++seq;
+      end = uniform(cu[seq + 1]);
+    } while (end == start);
+  }
+  // To the sequence of the token before this one's first (which must exist).
+  __device__ void previous() {
+    end = start;
+    do {
+      --seq;
+      start = uniform(cu[seq]);
+    } while (end == start);
+  }
+};
+
+// Calls f(n) for each sequence without tokens (all of them where the offsets are
+// malformed); the whole wave calls.
+template <typename F> __device__ __forceinline__ void for_empty(const int32_t *cu, int N, int T, bool ok, F f) {
+  for (long base = 0; base < N; base += 64) {
+    const long n = base + lane_id();
+    const bool empty = n < N && (!ok || (cu ? cu[n] == cu[n + 1] : T == 0));
+    for (uint64_t left = __ballot(empty); left; left &= left - 1) f((int)base + __builtin_ctzll(left));
+  }
+}
+
+}  // namespace hagdn

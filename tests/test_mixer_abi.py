@@ -1,0 +1,172 @@
+"""The refusals of the convolution's, the scan's and the pools' entry points, which need no GPU:
+bad arguments are turned down on the host before anything is enqueued (fake,
+never-dereferenced device pointers)."""
+
+import ctypes
+import os
+
+import pytest
+
+import paper_2609_32114_amd as P
+
+pytestmark = pytest.mark.skipif(not os.path.exists(P.library_path()), reason="libhagdn.so not built")
+
+EINVAL, EUNSUP, EWS = 1, 2, 3
+BIG = 1 << 40
+F = [(i + 1) << 32 for i in range(40)]  # 16-byte aligned, far apart, never dereferenced
+
+
+def call(fn, defaults, **over):
+    args = dict(defaults)
+    assert set(over) <= set(args), set(over) - set(args)
+    args.update(over)
+    lib = P.load_library()
+    return getattr(lib, fn)(*args.values()), lib.hagdn_last_error().decode()
+
+
+CONV = dict(x=F[0], xs=64, w=F[1], b=F[2], w0=F[3], cu=F[4], N=2, T=10, D=64, W=4, dtype=1, act=0, y=F[5], wf=F[6], ws=F[7],
+            wsb=64, stream=None)  # the workspace is too small: a valid call stops there
+CONV_BACK = dict(dy=F[0], dys=64, x=F[1], xs=64, w=F[2], b=F[3], w0=F[4], df=F[5], cu=F[6], N=2, T=10, D=64, W=4, dtype=1, act=0,
+                 dx=F[7], dw=F[8], db=F[9], dw0=F[10], ws=F[11], wsb=64, stream=None)
+CONV_STEP = dict(x=F[0], xs=64, w=F[1], b=None, state=F[2], slots=None, pool=0, N=3, D=64, W=4, dtype=1, act=2, y=F[3],
+                 stream=None)
+SSM = dict(x=F[0], xs=64, dt=F[1], dts=64, A=F[2], B=F[3], Bs=16, C=F[4], Cs=16, skip=F[5], z=F[6], zs=64, bias=F[7], s0=F[8],
+           cu=F[9], N=2, T=10, D=64, S=16, G=1, dtype=1, st=0, pre=2, y=F[10], sf=F[11], ck=F[12], ws=F[13], wsb=64, stream=None)
+SSM_BACK = dict(dy=F[20], dys=64, x=F[0], xs=64, dt=F[1], dts=64, A=F[2], B=F[3], Bs=16, C=F[4], Cs=16, skip=F[5], z=F[6], zs=64,
+                bias=F[7], ck=F[12], s0=F[8], df=F[21], cu=F[9], N=2, T=10, D=64, S=16, G=1, dtype=1, st=0, pre=2, dx=F[22],
+                ddt=F[23], dA=F[24], dB=F[25], dC=F[26], dskip=F[27], dz=F[28], dbias=F[29], ds0=F[30], ws=F[13], wsb=64,
+                stream=None)
+SSM_STEP = dict(x=F[0], xs=64, dt=F[1], dts=64, A=F[2], B=F[3], Bs=16, C=F[4], Cs=16, skip=None, z=None, zs=0, bias=None,
+                state=F[5], slots=None, pool=0, N=3, D=64, S=16, G=1, dtype=1, st=1, pre=0, y=F[6], stream=None)
+
+
+def test_valid_calls_reach_the_workspace_check():
+    for fn, d in (("hagdn_conv_prefill", CONV), ("hagdn_conv_backward", CONV_BACK), ("ssm_prefill", SSM),
+                  ("ssm_backward", SSM_BACK)):
+        rc, msg = call(fn, d)
+        assert rc == EWS and "workspace too small" in msg, (fn, rc, msg)
+
+
+@pytest.mark.parametrize("fn,d", [("hagdn_conv_prefill", CONV), ("hagdn_conv_backward", CONV_BACK)], ids=["prefill", "backward"])
+def test_conv_refusals(fn, d):
+    for over in (dict(N=0), dict(T=-1), dict(D=0), dict(act=1), dict(act=3), dict(x=None), dict(w=None), dict(ws=None),
+                 dict(ws=F[7] + 8), dict(cu=None), dict(cu=F[4] + 2), dict(xs=-1), dict(xs=1 << 31), dict(x=F[0] + 1),
+                 dict(w=F[1] + 2), dict(w0=F[3] + 1)):
+        assert call(fn, d, **{"wsb": BIG, **over})[0] == EINVAL, over
+    for over in (dict(dtype=2), dict(W=1), dict(W=9), dict(W=-3), dict(D=(1 << 28) + 1)):
+        assert call(fn, d, **{"wsb": BIG, **over})[0] == EUNSUP, over
+    out = dict(y=None) if fn == "hagdn_conv_prefill" else dict(dx=None)
+    assert call(fn, d, **{"wsb": BIG, **out})[0] == EINVAL
+
+
+def test_conv_overlaps():
+    for over in (dict(wf=F[3]), dict(wf=F[3] + 64), dict(y=F[0]), dict(y=F[0] + 128), dict(y=F[0] - 128), dict(wf=F[5] + 2),
+                 dict(y=F[1] + 4), dict(wf=F[4])):
+        rc, msg = call("hagdn_conv_prefill", CONV, wsb=BIG, **over)
+        assert rc == EINVAL and "overlaps" in msg, over
+    for over in (dict(dw0=F[5]), dict(dx=F[0]), dict(dw=F[2]), dict(dx=F[1] + 64), dict(db=F[3]), dict(db=F[8]), dict(db=None)):
+        assert call("hagdn_conv_backward", CONV_BACK, wsb=BIG, **over)[0] == EINVAL, over
+
+
+def test_conv_decode_refusals():
+    for over in (dict(N=-1), dict(x=None), dict(state=None), dict(y=None), dict(slots=F[8], pool=0), dict(slots=F[8] + 2, pool=4),
+                 dict(y=F[2]), dict(state=F[0]), dict(N=1 << 20, D=1 << 12), dict(xs=-2), dict(act=1)):
+        assert call("hagdn_conv_decode", CONV_STEP, **over)[0] == EINVAL, over
+    assert call("hagdn_conv_decode", CONV_STEP, dtype=5)[0] == EUNSUP
+    assert call("hagdn_conv_decode", CONV_STEP, N=0, x=None, y=None, state=None)[0] == 0
+
+
+@pytest.mark.parametrize("fn,d", [("ssm_prefill", SSM), ("ssm_backward", SSM_BACK)], ids=["prefill", "backward"])
+def test_ssm_refusals(fn, d):
+    for over in (dict(N=0), dict(T=-1), dict(D=0), dict(S=0), dict(G=0), dict(G=3), dict(G=-1), dict(pre=1), dict(pre=4),
+                 dict(pre=0), dict(x=None), dict(dt=None), dict(A=None), dict(B=None), dict(C=None), dict(ws=None),
+                 dict(ws=F[13] + 8), dict(cu=None), dict(xs=-1), dict(Bs=1 << 31), dict(zs=-4), dict(x=F[0] + 1),
+                 dict(dt=F[1] + 2), dict(B=F[3] + 1), dict(N=1 << 20, D=1 << 12)):
+        assert call(fn, d, **{"wsb": BIG, **over})[0] == EINVAL, over
+    for over in (dict(dtype=2), dict(st=3), dict(dtype=0, st=1), dict(S=65), dict(N=1, D=(1 << 28) + 1, S=1)):
+        assert call(fn, d, **{"wsb": BIG, **over})[0] == EUNSUP, over
+    outs = ("y",) if fn == "ssm_prefill" else ("dx", "ddt", "dA", "dB", "dC", "dskip", "dz", "dbias", "ck")
+    for name in outs:
+        assert call(fn, d, **{"wsb": BIG, name: None})[0] == EINVAL, name
+
+
+def test_ssm_overlaps():
+    for over in (dict(sf=F[8]), dict(sf=F[8] + 16), dict(y=F[0]), dict(y=F[6] + 64), dict(ck=F[10]), dict(y=F[3])):
+        assert call("ssm_prefill", SSM, wsb=BIG, **over)[0] == EINVAL, over
+    for over in (dict(ds0=F[21]), dict(dx=F[20]), dict(ddt=F[1]), dict(dz=F[6]), dict(dB=F[25], dC=F[25]), dict(dA=F[2]),
+                 dict(ds0=F[8])):
+        assert call("ssm_backward", SSM_BACK, wsb=BIG, **over)[0] == EINVAL, over
+
+
+def test_ssm_decode_refusals():
+    for over in (dict(N=-1), dict(x=None), dict(state=None), dict(y=None), dict(slots=F[8], pool=0), dict(bias=F[9]),
+                 dict(y=F[5]), dict(state=F[3]), dict(N=1 << 20, D=1 << 12), dict(Cs=-2), dict(G=5)):
+        assert call("ssm_decode", SSM_STEP, **over)[0] == EINVAL, over
+    for over in (dict(dtype=0), dict(S=65)):
+        assert call("ssm_decode", SSM_STEP, **over)[0] == EUNSUP, over
+    assert call("ssm_decode", SSM_STEP, N=0, x=None, y=None, state=None)[0] == 0
+
+
+def test_workspace_sizes():
+    lib = P.load_library()
+    assert P.ssm_workspace_size(0, 1, 1) > 0 and P.conv_workspace_size(0, 1, 2) > 0
+    assert P.ssm_workspace_size(100000, 2048, 16) > P.ssm_workspace_size(1000, 2048, 16)
+    assert P.ssm_workspace_size(1000, 2048, 16, backward=True) > P.ssm_workspace_size(1000, 2048, 16)
+    assert P.ssm_checkpoints_size(33, 10, 16) == 2 * 16 * 10 and P.ssm_checkpoints_size(0, 10, 16) == 0
+    assert P.ssm_checkpoints_size(33, 10, 17) == 3 * 32 * 10 and P.ssm_checkpoints_size(33, 10, 64) == 5 * 64 * 10
+    assert lib.ssm_workspace_size(-1, 64, 16, 1, 0) == 0 and lib.ssm_workspace_size(5, 64, 16, 3, 0) == 0
+    assert lib.hagdn_conv_workspace_size(5, 64, 1, 0) == 0 and lib.hagdn_pool_workspace_size(0) == 0
+    for bad in (lambda: P.ssm_workspace_size(5, 0, 16), lambda: P.conv_workspace_size(5, 64, 9),
+                lambda: P.pool_workspace_size((1 << 20) + 1)):
+        with pytest.raises(P.HagdnError):
+            bad()
+
+
+# ------------------------------------------------------------------------- pools
+def arrays(pools, sizes):
+    n = len(pools)
+    return (ctypes.c_void_p * n)(*pools), (ctypes.c_size_t * n)(*sizes)
+
+
+def copy(pools, sizes, sources=None, dst=F[30], src=F[31], n=3, rows=8, src_rows=8, count=None):
+    p, s = arrays(pools, sizes)
+    f = arrays(sources, sizes)[0] if sources is not None else None
+    lib = P.load_library()
+    return lib.hagdn_pool_copy(p, f, s, len(pools) if count is None else count, dst, src, n, rows, src_rows, None)
+
+
+def test_pool_copy_refusals():
+    lib = P.load_library()
+    assert copy([F[0]], [64], n=0) == 0 and copy([F[0]], [64], rows=0) == 0
+    for args in (dict(n=-1), dict(rows=-1), dict(count=0), dict(count=1025), dict(dst=F[30] + 2), dict(src=F[31] + 1),
+                 dict(dst=F[0] + 64)):
+        assert copy([F[0]], [64], **args) == EINVAL, args
+    assert copy([None], [64]) == EINVAL and copy([F[0]], [0]) == EINVAL and copy([F[0]], [1 << 41]) == EINVAL
+    assert copy([F[0]], [64], n=8193, rows=10000) == EUNSUP
+    assert copy([F[0]], [64], sources=[None]) == EINVAL and copy([F[0]], [64], sources=[F[1]], src_rows=-1) == EINVAL
+    # pools over each other, in any order, and over sources
+    assert copy([F[0], F[0]], [64, 64]) == EINVAL and copy([F[0], F[1], F[0] + 64 * 7], [64] * 3) == EINVAL
+    assert copy([F[0]], [64], sources=[F[0]]) == EINVAL and copy([F[0]], [64], sources=[F[0] - 64]) == EINVAL
+    assert copy([F[2], F[0]], [64, 64], sources=[F[1], F[2] + 64]) == EINVAL
+    # neighbours are none
+    assert copy([F[0], F[0] + 512, F[0] - 512], [64] * 3, n=0) == 0
+    # sources may overlap each other
+    assert copy([F[0], F[1]], [64, 64], sources=[F[2], F[2]], n=0) == 0
+    assert lib.hagdn_pool_copy(None, None, None, 1, None, None, 1, 1, 1, None) == EINVAL
+
+
+def test_pool_plan_refusals():
+    lib = P.load_library()
+    p, s = arrays([F[0]], [64])
+    fork = lambda **o: lib.hagdn_pool_fork(*{**dict(p=p, s=s, n=1, slots=F[1], N=3, parents=F[2], M=4, S=8, out=F[3], ws=F[4],
+                                                     wsb=BIG, stream=None), **o}.values())
+    compact = lambda **o: lib.hagdn_pool_compact(*{**dict(p=p, s=s, n=1, slots=F[1], N=3, S=8, out=F[3], ws=F[4], wsb=BIG,
+                                                           stream=None), **o}.values())
+    for f in (fork, compact):
+        for over in (dict(p=None), dict(s=None), dict(n=0), dict(slots=None), dict(slots=F[1] + 2), dict(out=None), dict(N=-1),
+                     dict(S=0), dict(ws=None), dict(ws=F[4] + 8), dict(out=F[1] + 4)):
+            assert f(**over) == EINVAL, over
+        assert f(wsb=100) == EWS and f(S=(1 << 20) + 1) == EUNSUP
+    for over in (dict(parents=None), dict(M=-1), dict(out=F[1]), dict(out=F[2])):
+        assert fork(**over) == EINVAL, over
+    assert fork(M=(1 << 20) + 1) == EUNSUP and compact(N=(1 << 20) + 1) == EUNSUP
