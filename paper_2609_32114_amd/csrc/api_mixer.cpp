@@ -128,15 +128,15 @@ int check_ssm(int T, int D, int S, int G, int dtype, int dt_dtype, int pre) {
   return HAGDN_OK;
 }
 
-// A call's chunks and the places of its workspace's parts (forward: the first four).
+// A call's chunks and the places of its workspace's parts (forward: the first three).
 struct SsmPlan {
   int chunk, chunks;
-  size_t bc, maps, sums, resets, dbc, dweights, bytes;
+  size_t maps, sums, resets, dbc, dweights, bytes;
 };
 SsmPlan ssm_plan(int T, int D, int S, int G, bool backward) {
   SsmPlan p = {};
   const size_t np = hagdn::ssm_padded(S);
-  p.chunk = hagdn::ssm_chunk(T, D, S, G, query_cus());
+  p.chunk = hagdn::ssm_chunk(T, D, G, query_cus(), backward);
   p.chunks = T > 0 ? (T - 1) / p.chunk + 1 : 1;
   const size_t between = p.chunks > 1 ? p.chunks : 0;  // one chunk leaves nothing to another
   size_t at = hagdn::kMixerHeader;
@@ -145,7 +145,6 @@ SsmPlan ssm_plan(int T, int D, int S, int G, bool backward) {
     at += pad256(n);
     return here;
   };
-  p.bc = take((size_t)T * G * 2 * np * 4);
   p.maps = take(between * np * D * 4);
   p.sums = take(between * D * 4);
   p.resets = take(between * 4);
@@ -173,7 +172,6 @@ void set_plan(hagdn::SsmArgs *a, const SsmPlan &p, void *ws) {
   a->chunks = p.chunks;
   a->cus = query_cus();
   a->status = reinterpret_cast<int *>(w);
-  a->bc = reinterpret_cast<float *>(w + p.bc);
   a->maps = reinterpret_cast<float *>(w + p.maps);
   a->sums = reinterpret_cast<float *>(w + p.sums);
   a->resets = reinterpret_cast<int *>(w + p.resets);
@@ -383,8 +381,7 @@ size_t ssm_workspace_size(int T_total, int D, int S, int G, int backward) {
 
 size_t ssm_checkpoints_size(int T_total, int D, int S) {
   if (check_ssm(T_total, D, S, 1, HAGDN_F32, HAGDN_F32, 0) != HAGDN_OK) return 0;
-  const size_t group = hagdn::ssm_group(S);
-  return ((size_t)T_total + group - 1) / group * hagdn::ssm_padded(S) * (size_t)D;
+  return ((size_t)T_total + hagdn::kSsmGroup - 1) / hagdn::kSsmGroup * hagdn::ssm_padded(S) * (size_t)D;
 }
 
 int ssm_prefill(const void *x, int64_t x_stride, const void *dt, int64_t dt_stride, const float *A, const void *B,

@@ -4,39 +4,19 @@
 
 namespace hagdn {
 
-// B and C as rows of fp32, padded with zeros; the first workgroup checks the offsets.
-template <typename T> __global__ __launch_bounds__(256) void ssm_setup_kernel(SsmArgs a, int padded) {
-  const size_t total = (size_t)a.T * a.G * 2 * padded;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
-    const size_t row = i / (2 * padded), t = row / a.G;  // padded: a power of two
-    const int e = (int)(i & (2 * padded - 1)), n = e & (padded - 1), g = (int)(row - t * a.G);
-    const T *src = e < padded ? static_cast<const T *>(a.B) + t * a.Bs : static_cast<const T *>(a.C) + t * a.Cs;
-    a.bc[i] = n < a.S ? Elt<T>::to_f32(src[g * a.S + n]) : 0.f;
-  }
-  if (blockIdx.x != 0) return;
-  const bool ok = offsets_ok(a.cu, a.N, a.T);
-  if (threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
-}
-hipError_t launch_ssm_setup(const SsmArgs &a, bool bf16, hipStream_t s) {
-  const int padded = ssm_padded(a.S);
-  const size_t total = (size_t)a.T * a.G * 2 * padded, blocks = (total + 1023) / 1024;
-  const dim3 grid((unsigned)(blocks < 1 ? 1 : blocks < 8192 ? blocks : 8192));
-  if (bf16) hipLaunchKernelGGL((ssm_setup_kernel<bf16_t>), grid, dim3(256), 0, s, a, padded);
-  else hipLaunchKernelGGL((ssm_setup_kernel<float>), grid, dim3(256), 0, s, a, padded);
-  return hipGetLastError();
-}
-
 constexpr int kSsmRows = 8;  // tokens whose rows are on their way at once; divides every chunk and group
 
-// A chunk's tokens: what it leaves of a zero state (OUT false), or its outputs.
+// A chunk's tokens: what it leaves of a zero state (OUT false), or its outputs.  The four
+// waves of a workgroup have four columns of a group and the same chunk.
 template <typename T, typename S, int NP, bool OUT>
-__global__ __launch_bounds__(256) void ssm_scan_kernel(SsmArgs a, uint32_t cols, uint32_t items) {
-  const uint32_t item = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (item >= items) return;
-  const int chunk = (int)(item / cols);
-  const Column col(item % cols, a);
+__global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan_kernel(SsmArgs a, uint32_t quads) {
+  using Stage = Maps<T, NP, OUT ? 3 : 1, kSsmRows, 256>;
+  __shared__ __align__(16) float sMaps[2][Stage::kAll];
+  const bool ok = ssm_offsets_ok(a);
+  const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads;
+  const int chunk = (int)(blockIdx.x / (quads * a.G));
+  const Column col(group, (quad - group * quads) * 4 + uniform(threadIdx.x >> 6), a);
   const uint32_t c = col.c;
-  const bool ok = uniform(*a.status) == 0;
   if (OUT && chunk == 0) pass_states(a, ok, a.s0, a.s_final, col);
   const int t0 = chunk * a.chunk, t1 = (int)min((long)t0 + a.chunk, (long)a.T);
   if (!ok || t0 >= t1) return;
@@ -50,55 +30,66 @@ __global__ __launch_bounds__(256) void ssm_scan_kernel(SsmArgs a, uint32_t cols,
   int first = q.start == t0 ? t0 : q.end;  // the next token that starts a sequence
   bool reset = false;
   float sum = 0.f;
-  for (int base = t0; base < t1; base += kSsmRows) {
+  Stage stage;
+  stage.fetch(a, group, t0, t1);
+  int turn = 0;
+  for (int base = t0; base < t1; base += kSsmRows, turn ^= 1) {
+    const int count = min(kSsmRows, t1 - base);
+    const float *rows = sMaps[turn];
     T x[kSsmRows], z[kSsmRows];
     S dt[kSsmRows];
-#pragma unroll
-    for (int i = 0; i < kSsmRows; ++i) {
-      const size_t t = min(base + i, t1 - 1);
-      x[i] = static_cast<const T *>(a.x)[t * a.xs + c];
-      dt[i] = static_cast<const S *>(a.dt)[t * a.dts + c];
-      if (OUT) z[i] = a.z ? static_cast<const T *>(a.z)[t * a.zs + c] : T(0);
-    }
-    if (OUT && a.ckpt && base % (512 / NP) == 0) store_states(a.ckpt + (size_t)(base / (512 / NP)) * NP * a.D, a, col, h);
-#pragma unroll
-    for (int i = 0; i < kSsmRows; ++i) {
-      const int t = base + i;
-      if (t >= t1) break;
-      if (t == first) {
-        if (t == q.end) q.next();
-        load_sequence(a.s0, q.seq, a, c, h);
+    load_tokens(a.x, a.xs, base, t1, c, x);
+    load_tokens(a.dt, a.dts, base, t1, c, dt);
+    if (OUT && a.z) load_tokens(a.z, a.zs, base, t1, c, z);
+    stage.put(sMaps[turn]);
+    __syncthreads();
+    if (base + kSsmRows < t1) stage.fetch(a, group, base + kSsmRows, t1);
+    if (OUT && a.ckpt && base % kSsmGroup == 0) store_states(a.ckpt + (size_t)(base / kSsmGroup) * NP * a.D, a, col, h);
+    float given[kSsmRows], step[kSsmRows], y[kSsmRows];
+    step_sizes(a, dt, bias, given, step);
+    for (int lo = 0; lo < count;) {  // from one sequence's first token to the next one's
+      if (base + lo == first) {
+        if (first == q.end) q.next();
+        load_sequence<NP>(a.s0, q.seq, a, c, h);
         first = q.end;
         reset = true;
       }
-      const float u = Elt<T>::to_f32(x[i]);
-      float step = Elt<S>::to_f32(dt[i]);
-      if (a.raw) step = softplus(step + bias);
-      const float in = step * u;
-      if (!OUT) sum += step;
-      const HAGDN_CONSTANT f32x16 *row = bc_row<NP>(a, t, col.group);
-      float y = skip * u;
+      const int hi = min(count, first - base);
 #pragma unroll
-      for (int k = 0; k < NP / 16; ++k) {
-        const f32x16 B = row[k], C = OUT ? row[NP / 16 + k] : f32x16(0.f);
+      for (int i = 0; i < kSsmRows; ++i)
+        if (i >= lo && i < hi) {
+          const float *row = rows + here(i * Stage::kRow);
+          const float v = here(step[i]);
+          const float u = Elt<T>::to_f32(x[i]), in = v * u;
+          if (!OUT) sum += v;
+          y[i] = skip * u;
 #pragma unroll
-        for (int n = 0; n < 16; ++n) {
-          float &s = h[16 * k + n];
-          s = __builtin_fmaf(__builtin_amdgcn_exp2f(step * A[16 * k + n]), s, in * B[n]);
-          if (OUT) y = __builtin_fmaf(C[n], s, y);
+          for (int n = 0; n < NP; n += 4) {
+            const f32x4 B = *reinterpret_cast<const f32x4 *>(row + n);
+            const f32x4 C = OUT ? *reinterpret_cast<const f32x4 *>(row + NP + n) : f32x4{};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float &s = h[n + k];
+              s = __builtin_fmaf(__builtin_amdgcn_exp2f(v * A[n + k]), s, in * B[k]);
+              if (OUT) y[i] = __builtin_fmaf(C[k], s, y[i]);
+            }
+          }
         }
+      if (OUT && base + hi == q.end) store_sequence<NP>(a.s_final, q.seq, a, col, h);
+      lo = hi;
+    }
+    if (OUT) {
+      if (a.z) {
+#pragma unroll
+        for (int i = 0; i < kSsmRows; ++i) y[i] *= silu(Elt<T>::to_f32(z[i]));
       }
-      if (OUT) {
-        if (a.z) y *= silu(Elt<T>::to_f32(z[i]));
-        if (col.mine) static_cast<T *>(a.y)[(size_t)t * a.D + c] = Elt<T>::from_f32(y);
-        if (t + 1 == q.end) store_sequence(a.s_final, q.seq, a, col, h);
-      }
+      store_tokens<T>(a.y, a, col, base, count, y);
     }
   }
   if (OUT) return;
   store_states(a.maps + (size_t)chunk * NP * a.D, a, col, h);
   if (col.mine) a.sums[(size_t)chunk * a.D + c] = sum;
-  if (item % cols == 0 && lane_id() == 0) a.resets[chunk] = reset;
+  if (quad == 0 && threadIdx.x == 0) a.resets[chunk] = reset;
 }
 
 // What enters each chunk, in place of what it leaves of nothing.  A workgroup has one state
@@ -154,23 +145,22 @@ hipError_t launch_ssm_carry(const SsmArgs &a, bool backward, hipStream_t s) {
 }
 
 hipError_t launch_ssm_forward(const SsmArgs &a, bool bf16, bool dt_bf16, hipStream_t s) {
-  hipError_t e = launch_ssm_setup(a, bf16, s);
-  if (e != hipSuccess) return e;
   return ssm_dispatch(a.S, bf16, dt_bf16, [&](auto t, auto st, auto np) {
     using T = decltype(t);
     using S = decltype(st);
     constexpr int NP = decltype(np)::value;
-    const uint32_t cols = (uint32_t)ssm_columns(a.D, a.G) * a.G;
-    const long all = (long)a.chunks * cols;
-    if (all > 0x3fffffffl) return hipErrorInvalidValue;
+    const uint32_t quads = (uint32_t)((ssm_columns(a.D, a.G) + 3) / 4);
+    const long each = (long)quads * a.G, all = a.chunks * each;
+    if (all > 0x7fffffffl) return hipErrorInvalidValue;
+    hipError_t e = a.N > kCheckInPlace ? launch_check_offsets(a.cu, a.N, a.T, a.status, s) : hipSuccess;
+    if (e != hipSuccess) return e;
     if (a.chunks > 1) {
-      const uint32_t items = (uint32_t)(all - cols);
-      hipLaunchKernelGGL((ssm_scan_kernel<T, S, NP, false>), dim3((items + 3) / 4), dim3(256), 0, s, a, cols, items);
-      hipError_t e = hipGetLastError();
+      hipLaunchKernelGGL((ssm_scan_kernel<T, S, NP, false>), dim3((unsigned)(all - each)), dim3(256), 0, s, a, quads);
+      e = hipGetLastError();
       if (e == hipSuccess) e = launch_ssm_carry(a, false, s);
       if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((ssm_scan_kernel<T, S, NP, true>), dim3(((uint32_t)all + 3) / 4), dim3(256), 0, s, a, cols, (uint32_t)all);
+    hipLaunchKernelGGL((ssm_scan_kernel<T, S, NP, true>), dim3((unsigned)all), dim3(256), 0, s, a, quads);
     return hipGetLastError();
   });
 }

@@ -13,13 +13,15 @@ constexpr int kBackRows = 8;
 
 // What a chunk passes back of a zero gradient.
 template <typename T, typename S, int NP>
-__global__ __launch_bounds__(256) void ssm_back_local_kernel(SsmArgs a, uint32_t cols, uint32_t items) {
-  const uint32_t item = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (item >= items) return;
-  const int chunk = 1 + (int)(item / cols);  // the first chunk passes nothing on
-  const Column col(item % cols, a);
+__global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back_local_kernel(SsmArgs a, uint32_t quads) {
+  using Stage = Maps<T, NP, 2, kBackRows, 256>;
+  __shared__ __align__(16) float sMaps[2][Stage::kAll];
+  const bool ok = ssm_offsets_ok(a);
+  const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads;
+  const int chunk = 1 + (int)(blockIdx.x / (quads * a.G));  // the first chunk passes nothing on
+  const Column col(group, (quad - group * quads) * 4 + uniform(threadIdx.x >> 6), a);
   const uint32_t c = col.c;
-  if (uniform(*a.status) != 0) return;
+  if (!ok) return;
   const int t0 = chunk * a.chunk, t1 = (int)min((long)t0 + a.chunk, (long)a.T);
   float A[NP], e[NP];
   load_rates(a, c, A);
@@ -29,44 +31,57 @@ __global__ __launch_bounds__(256) void ssm_back_local_kernel(SsmArgs a, uint32_t
   Cursor q(a.cu, a.N, a.T, t1 - 1);
   bool reset = false;
   float sum = 0.f;
-  for (int top = t1; top > t0; top -= kBackRows) {
+  int base = t0 + (t1 - 1 - t0) / kBackRows * kBackRows, turn = 0;
+  Stage stage;
+  stage.fetch(a, group, base, t1);
+  for (; base >= t0; base -= kBackRows, turn ^= 1) {
+    const int count = min(kBackRows, t1 - base);
+    const float *rows = sMaps[turn];
     T dy[kBackRows], z[kBackRows];
     S dt[kBackRows];
+    load_tokens(a.dy, a.dys, base, t1, c, dy);
+    load_tokens(a.dt, a.dts, base, t1, c, dt);
+    if (a.z) load_tokens(a.z, a.zs, base, t1, c, z);
+    stage.put(sMaps[turn]);
+    __syncthreads();
+    if (base > t0) stage.fetch(a, group, base - kBackRows, t1);
+    float given[kBackRows], step[kBackRows], d[kBackRows];
+    step_sizes(a, dt, bias, given, step);
 #pragma unroll
-    for (int i = 0; i < kBackRows; ++i) {
-      const size_t t = max(top - 1 - i, t0);
-      dy[i] = static_cast<const T *>(a.dy)[t * a.dys + c];
-      dt[i] = static_cast<const S *>(a.dt)[t * a.dts + c];
-      z[i] = a.z ? static_cast<const T *>(a.z)[t * a.zs + c] : T(0);
+    for (int i = 0; i < kBackRows; ++i) d[i] = Elt<T>::to_f32(dy[i]);
+    if (a.z) {
+#pragma unroll
+      for (int i = 0; i < kBackRows; ++i) d[i] *= silu(Elt<T>::to_f32(z[i]));
     }
-#pragma unroll
-    for (int i = 0; i < kBackRows; ++i) {
-      const int t = top - 1 - i;
-      if (t < t0) break;
-      if (t + 1 == q.start) q.previous();
-      if (t + 1 == q.end) {
-        load_sequence(a.dfinal, q.seq, a, c, e);
+    for (int hi = count; hi > 0;) {  // from one sequence's last token back to its first
+      if (base + hi == q.start) q.previous();
+      if (base + hi == q.end) {
+        load_sequence<NP>(a.dfinal, q.seq, a, c, e);
         reset = true;
       }
-      float d = Elt<T>::to_f32(dy[i]), step = Elt<S>::to_f32(dt[i]);
-      if (a.raw) step = softplus(step + bias);
-      if (a.z) d *= silu(Elt<T>::to_f32(z[i]));
-      sum += step;
-      const HAGDN_CONSTANT f32x16 *row = bc_row<NP>(a, t, col.group);
+      const int lo = max(0, q.start - base);
 #pragma unroll
-      for (int k = 0; k < NP / 16; ++k) {
-        const f32x16 C = row[NP / 16 + k];
+      for (int i = kBackRows - 1; i >= 0; --i)
+        if (i >= lo && i < hi) {
+          const float *row = rows + here(i * Stage::kRow);
+          const float u = here(step[i]);
+          sum += u;
 #pragma unroll
-        for (int n = 0; n < 16; ++n) {
-          float &v = e[16 * k + n];
-          v = __builtin_amdgcn_exp2f(step * A[16 * k + n]) * __builtin_fmaf(C[n], d, v);
+          for (int n = 0; n < NP; n += 4) {
+            const f32x4 C = *reinterpret_cast<const f32x4 *>(row + n);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              float &v = e[n + k];
+              v = __builtin_amdgcn_exp2f(u * A[n + k]) * __builtin_fmaf(C[k], d[i], v);
+            }
+          }
         }
-      }
+      hi = lo;
     }
   }
   store_states(a.maps + (size_t)chunk * NP * a.D, a, col, e);
   if (col.mine) a.sums[(size_t)chunk * a.D + c] = sum;
-  if (item % cols == 0 && lane_id() == 0) a.resets[chunk] = reset;
+  if (quad == 0 && threadIdx.x == 0) a.resets[chunk] = reset;
 }
 
 // Sums of 16 values over the wave's 64 lanes: value n to the lanes 4 n .. 4 n + 3.  Each
@@ -95,27 +110,35 @@ __device__ __forceinline__ float sum_lanes(const float (&in)[16]) {
   return s + dpp<0x4e>(s);                                                                             // lane ^ 2
 }
 
-// The forms for NP padded states: SUB tokens whose states are held in registers, four
-// times as many to a saved state, WAVES columns to a workgroup.  The states at the four
-// runs' starts lie in LDS.
+// The forms for NP padded states: kWaves columns to a workgroup.  In LDS: the states at the
+// starts of a group's four runs of 8 tokens, the group's B and C, and a run's sums of dB
+// and dC for each wave.
 template <int NP> struct BackForm {
-  static constexpr int kSub = 128 / NP, kGroup = 512 / NP, kWaves = NP == 64 ? 2 : 4;  // ssm_waves()
-  static constexpr size_t kStates = (size_t)kWaves * 4 * NP * 64, kSums = (size_t)kWaves * kGroup * 2 * NP;
-  static constexpr size_t kLds = (kStates + kSums) * sizeof(float);
+  static constexpr int kWaves = NP == 64 ? 2 : 4;  // ssm_waves()
+  static constexpr int kRuns = kSsmGroup / kBackRows;
+  static constexpr size_t kStates = (size_t)kWaves * kRuns * NP * 64, kSums = (size_t)kWaves * kBackRows * 2 * NP;
+  static constexpr size_t kMaps = (size_t)kSsmGroup * 2 * NP;
+  static constexpr size_t kLds = (kStates + kSums + kMaps) * sizeof(float);
 };
+constexpr int kSlice = 8;  // states whose run of 8 tokens is held in registers at once
 
+// A group of 32 tokens at a time, the last first: its states at every eighth token are formed
+// from the saved ones; then a run of 8 tokens at a time, the last first, and of 8 states of
+// it, goes forward again, its a_t h_{t-1} kept in registers, and back.
 template <typename T, typename S, int NP>
 __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void ssm_backward_kernel(SsmArgs a, uint32_t quads) {
   using F = BackForm<NP>;
+  using Stage = Maps<T, NP, 3, kSsmGroup, F::kWaves * 64>;
   extern __shared__ __align__(16) float lds[];
   const int wave = uniform(threadIdx.x >> 6), lane = lane_id();
-  float *starts = lds + (size_t)wave * 4 * NP * 64 + lane;  // [4][NP][64]
-  float *sums = lds + F::kStates;                            // [waves][group][2 NP]
-  const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads, in_group = quad % quads;
+  float *starts = lds + (size_t)wave * F::kRuns * NP * 64 + lane;  // [runs][NP][64]
+  float *sums = lds + F::kStates;                                   // [waves][8][2 NP]
+  float *maps = sums + F::kSums;                                    // [32][2 NP]
+  const bool ok = ssm_offsets_ok(a);
+  const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads, in_group = quad - group * quads;
   const int chunk = (int)(blockIdx.x / (quads * a.G));
   const Column col(group, in_group * F::kWaves + wave, a);
   const uint32_t c = col.c;
-  const bool ok = uniform(*a.status) == 0;
   if (chunk == 0) pass_states(a, ok, a.dfinal, a.ds0, col);
   const int t0 = chunk * a.chunk, t1 = ok ? (int)min((long)t0 + a.chunk, (long)a.T) : t0;
 
@@ -125,150 +148,183 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
   for (int n = 0; n < NP; ++n) e[n] = dA[n] = 0.f;
   if (ok && chunk + 1 < a.chunks) load_states(a.maps + (size_t)chunk * NP * a.D, a, c, e);
   const float bias = a.raw && a.bias ? a.bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
-  const auto step_at = [&](size_t t) { return Elt<S>::to_f32(static_cast<const S *>(a.dt)[t * a.dts + c]); };
-  const auto x_at = [&](size_t t) { return Elt<T>::to_f32(static_cast<const T *>(a.x)[t * a.xs + c]); };
 
-  for (int g0 = t0 + (t1 - 1 - t0) / F::kGroup * F::kGroup; t1 > t0 && g0 >= t0; g0 -= F::kGroup) {
-    const int g1 = min(g0 + F::kGroup, t1);
-    float h[NP];
-    load_states(a.ckpt + (size_t)(g0 / F::kGroup) * NP * a.D, a, c, h);
-    const int subs = (g1 - g0 + F::kSub - 1) / F::kSub;
-    {  // the states at the runs' starts
+  Stage stage;
+  for (int g0 = t0 + (t1 - 1 - t0) / kSsmGroup * kSsmGroup; t1 > t0 && g0 >= t0; g0 -= kSsmGroup) {
+    const int g1 = min(g0 + kSsmGroup, t1), runs = (g1 - g0 + kBackRows - 1) / kBackRows;
+    stage.fetch(a, group, g0, g1);
+    {
+      float h[NP];
+      load_states(a.ckpt + (size_t)(g0 / kSsmGroup) * NP * a.D, a, c, h);
+      stage.put(maps);  // the last group's have been read: its runs end at a barrier
+      __syncthreads();
       Cursor q(a.cu, a.N, a.T, g0);
       int first = q.start == g0 ? g0 : q.end;
-      for (int sub = 0; sub < subs; ++sub) {
+      for (int run = 0; run < runs; ++run) {
 #pragma unroll
-        for (int n = 0; n < NP; ++n) starts[(sub * NP + n) * 64] = h[n];
-        if (sub + 1 == subs) break;
-        const int s0 = g0 + sub * F::kSub;
-        float x[F::kSub], dt[F::kSub];
-#pragma unroll
-        for (int i = 0; i < F::kSub; ++i) {
-          x[i] = x_at(s0 + i);
-          dt[i] = step_at(s0 + i);
-        }
-#pragma unroll
-        for (int i = 0; i < F::kSub; ++i) {
-          const int t = s0 + i;
-          if (t == first) {
-            if (t == q.end) q.next();
-            load_sequence(a.s0, q.seq, a, c, h);
+        for (int n = 0; n < NP; ++n) starts[(run * NP + n) * 64] = h[n];
+        if (run + 1 == runs) break;
+        const int base = g0 + run * kBackRows;
+        T x[kBackRows];
+        S dt[kBackRows];
+        load_tokens(a.x, a.xs, base, t1, c, x);
+        load_tokens(a.dt, a.dts, base, t1, c, dt);
+        float given[kBackRows], step[kBackRows];
+        step_sizes(a, dt, bias, given, step);
+        for (int lo = 0; lo < kBackRows;) {
+          if (base + lo == first) {
+            if (first == q.end) q.next();
+            load_sequence<NP>(a.s0, q.seq, a, c, h);
             first = q.end;
           }
-          const float step = a.raw ? softplus(dt[i] + bias) : dt[i], in = step * x[i];
-          const HAGDN_CONSTANT f32x16 *row = bc_row<NP>(a, t, group);
+          const int hi = min(kBackRows, first - base);
 #pragma unroll
-          for (int k = 0; k < NP / 16; ++k) {
-            const f32x16 B = row[k];
+          for (int i = 0; i < kBackRows; ++i)
+            if (i >= lo && i < hi) {
+              const float *row = maps + here((run * kBackRows + i) * 2 * NP);
+              const float u = here(step[i]), in = u * Elt<T>::to_f32(x[i]);
 #pragma unroll
-            for (int n = 0; n < 16; ++n)
-              h[16 * k + n] = __builtin_fmaf(__builtin_amdgcn_exp2f(step * A[16 * k + n]), h[16 * k + n], in * B[n]);
-          }
+              for (int n = 0; n < NP; n += 4) {
+                const f32x4 B = *reinterpret_cast<const f32x4 *>(row + n);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  h[n + k] = __builtin_fmaf(__builtin_amdgcn_exp2f(u * A[n + k]), h[n + k], in * B[k]);
+              }
+            }
+          lo = hi;
         }
       }
     }
-    for (int sub = subs - 1; sub >= 0; --sub) {
-      const int s0 = g0 + sub * F::kSub, s1 = min(s0 + F::kSub, g1);
-      float x[F::kSub], v[F::kSub], step[F::kSub], dy[F::kSub], z[F::kSub];  // v: the step as given, with its bias
+    for (int run = runs - 1; run >= 0; --run) {
+      const int base = g0 + run * kBackRows, count = min(kBackRows, g1 - base);
+      const float *rows = maps + run * kBackRows * 2 * NP;
+      float x[kBackRows], given[kBackRows], step[kBackRows], d[kBackRows], dgate[kBackRows];
+      {
+        T xs[kBackRows], dys[kBackRows], zs[kBackRows];
+        S dts[kBackRows];
+        load_tokens(a.x, a.xs, base, g1, c, xs);
+        load_tokens(a.dt, a.dts, base, g1, c, dts);
+        load_tokens(a.dy, a.dys, base, g1, c, dys);
+        if (a.z) load_tokens(a.z, a.zs, base, g1, c, zs);
+        step_sizes(a, dts, bias, given, step);
 #pragma unroll
-      for (int i = 0; i < F::kSub; ++i) {
-        const size_t t = min(s0 + i, s1 - 1);
-        x[i] = x_at(t);
-        v[i] = step_at(t) + bias;
-        dy[i] = col.mine ? Elt<T>::to_f32(static_cast<const T *>(a.dy)[t * a.dys + c]) : 0.f;
-        z[i] = a.z ? Elt<T>::to_f32(static_cast<const T *>(a.z)[t * a.zs + c]) : 0.f;
-      }
-#pragma unroll
-      for (int n = 0; n < NP; ++n) h[n] = starts[(sub * NP + n) * 64];
-      Cursor q(a.cu, a.N, a.T, s0);
-      int first = q.start == s0 ? s0 : q.end;
-      float kept[F::kSub][NP];  // a_t h_{t-1}
-#pragma unroll
-      for (int i = 0; i < F::kSub; ++i) {
-        const int t = s0 + i;
-        step[i] = a.raw ? softplus(v[i]) : v[i];
-        if (t >= s1) break;
-        if (t == first) {
-          if (t == q.end) q.next();
-          load_sequence(a.s0, q.seq, a, c, h);
-          first = q.end;
+        for (int i = 0; i < kBackRows; ++i) {
+          x[i] = Elt<T>::to_f32(xs[i]);
+          d[i] = col.mine ? Elt<T>::to_f32(dys[i]) : 0.f;
         }
-        const float in = step[i] * x[i];
-        const HAGDN_CONSTANT f32x16 *row = bc_row<NP>(a, t, group);
+        if (a.z) {  // the gradient of the ungated output, and of z but for that output
 #pragma unroll
-        for (int k = 0; k < NP / 16; ++k) {
-          const f32x16 B = row[k];
-#pragma unroll
-          for (int m = 0; m < 16; ++m) {
-            const int n = 16 * k + m;
-            kept[i][n] = __builtin_amdgcn_exp2f(step[i] * A[n]) * h[n];
-            h[n] = __builtin_fmaf(in, B[m], kept[i][n]);
+          for (int i = 0; i < kBackRows; ++i) {
+            const float z = Elt<T>::to_f32(zs[i]);
+            const Logistic g = logistic(z);
+            dgate[i] = d[i] * (g.s * __builtin_fmaf(z, g.rest, 1.f));
+            d[i] *= z * g.s;
           }
         }
       }
+      float y[kBackRows], w[kBackRows], ds[kBackRows];
 #pragma unroll
-      for (int i = F::kSub - 1; i >= 0; --i) {
-        const int t = s0 + i;
-        if (t >= s1) continue;
-        if (t + 1 == q.start) q.previous();
-        if (t + 1 == q.end) load_sequence(a.dfinal, q.seq, a, c, e);
-        const float in = step[i] * x[i];
-        Logistic gate = {1.f, 0.f};
-        float d = dy[i];
-        if (a.z) {
-          gate = logistic(z[i]);
-          d *= z[i] * gate.s;
-        }
-        float y = skip * x[i], w = 0.f, ds = 0.f;
-        const HAGDN_CONSTANT f32x16 *row = bc_row<NP>(a, t, group);
+      for (int i = 0; i < kBackRows; ++i) {
+        y[i] = skip * x[i];
+        w[i] = ds[i] = 0.f;
+      }
+      const Cursor at(a.cu, a.N, a.T, base);
 #pragma unroll
-        for (int k = 0; k < NP / 16; ++k) {
-          const f32x16 B = row[k], C = row[NP / 16 + k];
-          float vB[16], vC[16];
+      for (int n0 = 0; n0 < NP; n0 += kSlice) {
+        float kept[kBackRows][kSlice], h[kSlice];  // kept: a_t h_{t-1}
 #pragma unroll
-          for (int m = 0; m < 16; ++m) {
-            const int n = 16 * k + m;
-            const float hn = __builtin_fmaf(in, B[m], kept[i][n]), dh = __builtin_fmaf(C[m], d, e[n]);
-            y = __builtin_fmaf(C[m], hn, y);
-            w = __builtin_fmaf(B[m], dh, w);
-            vC[m] = d * hn;
-            vB[m] = dh * in;
-            const float p = dh * kept[i][n];
-            ds = __builtin_fmaf(A[n], p, ds);
-            dA[n] = __builtin_fmaf(step[i], p, dA[n]);
-            e[n] = __builtin_amdgcn_exp2f(step[i] * A[n]) * dh;
+        for (int k = 0; k < kSlice; ++k) h[k] = starts[(run * NP + n0 + k) * 64];
+        Cursor q = at;
+        int first = q.start == base ? base : q.end;
+        for (int lo = 0; lo < count;) {
+          if (base + lo == first) {
+            if (first == q.end) q.next();
+            load_sequence<kSlice>(a.s0, q.seq, a, c, h, n0);
+            first = q.end;
           }
-          if (!col.mine) {
+          const int hi = min(count, first - base);
 #pragma unroll
-            for (int m = 0; m < 16; ++m) vB[m] = 0.f;
-          }
-          const float rB = sum_lanes(vB), rC = sum_lanes(vC);
-          if ((lane & 2) == 0)
-            sums[((size_t)wave * F::kGroup + (t - g0)) * (2 * NP) + (lane & 1) * NP + 16 * k + (lane >> 2)] = lane & 1 ? rC : rB;
+          for (int i = 0; i < kBackRows; ++i)
+            if (i >= lo && i < hi) {
+              const float *row = rows + here(i * 2 * NP + n0);
+              const float u = here(step[i]), in = u * x[i];
+#pragma unroll
+              for (int n = 0; n < kSlice; n += 4) {
+                const f32x4 B = *reinterpret_cast<const f32x4 *>(row + n);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  kept[i][n + k] = __builtin_amdgcn_exp2f(u * A[n0 + n + k]) * h[n + k];
+                  h[n + k] = __builtin_fmaf(in, B[k], kept[i][n + k]);
+                }
+              }
+            }
+          lo = hi;
         }
-        if (t == q.start) store_sequence(a.ds0, q.seq, a, col, e);
-        const float du = step[i] * w + skip * d;
-        float dv = x[i] * w + ds * (1.f / kLog2e);
-        if (a.raw) dv *= logistic(v[i]).s;
-        dskip = __builtin_fmaf(d, x[i], dskip);
-        dbias += dv;
-        if (col.mine) {
-          const size_t at = (size_t)t * a.D + c;
-          static_cast<T *>(a.dx)[at] = Elt<T>::from_f32(du);
-          static_cast<S *>(a.ddt)[at] = Elt<S>::from_f32(dv);
-          if (a.z) static_cast<T *>(a.dz)[at] = Elt<T>::from_f32(dy[i] * y * (gate.s * __builtin_fmaf(z[i], gate.rest, 1.f)));
+        for (int hi = count; hi > 0;) {
+          if (base + hi == q.start) q.previous();
+          if (base + hi == q.end) load_sequence<kSlice>(a.dfinal, q.seq, a, c, e + n0, n0);
+          const int lo = max(0, q.start - base);
+#pragma unroll
+          for (int i = kBackRows - 1; i >= 0; --i)
+            if (i >= lo && i < hi) {
+              const float *row = rows + here(i * 2 * NP + n0);
+              const float u = here(step[i]), in = u * x[i];
+              float terms[2 * kSlice];  // of dB and dC
+#pragma unroll
+              for (int m = 0; m < kSlice; m += 4) {
+                const f32x4 B = *reinterpret_cast<const f32x4 *>(row + m), C = *reinterpret_cast<const f32x4 *>(row + NP + m);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const int k = m + j, n = n0 + k;
+                  const float hn = __builtin_fmaf(in, B[j], kept[i][k]), dh = __builtin_fmaf(C[j], d[i], e[n]);
+                  y[i] = __builtin_fmaf(C[j], hn, y[i]);
+                  w[i] = __builtin_fmaf(B[j], dh, w[i]);
+                  terms[k] = col.mine ? dh * in : 0.f;
+                  terms[kSlice + k] = d[i] * hn;
+                  const float p = dh * kept[i][k];
+                  ds[i] = __builtin_fmaf(A[n], p, ds[i]);
+                  dA[n] = __builtin_fmaf(u, p, dA[n]);
+                  e[n] = __builtin_amdgcn_exp2f(u * A[n]) * dh;
+                }
+              }
+              const float sum = sum_lanes(terms);
+              if ((lane & 3) == 0)
+                sums[(wave * kBackRows + i) * 2 * NP + n0 + ((lane >> 2) & 7) + (lane >= 32 ? NP : 0)] = sum;
+            }
+          if (base + lo == q.start) store_sequence<kSlice>(a.ds0, q.seq, a, col, e + n0, n0);
+          hi = lo;
         }
       }
+      float dx[kBackRows], dv[kBackRows];
+#pragma unroll
+      for (int i = 0; i < kBackRows; ++i) {
+        dx[i] = __builtin_fmaf(skip, d[i], step[i] * w[i]);
+        dv[i] = __builtin_fmaf(ds[i], 1.f / kLog2e, x[i] * w[i]);
+        dgate[i] *= y[i];
+      }
+      if (a.raw) {
+#pragma unroll
+        for (int i = 0; i < kBackRows; ++i) dv[i] *= logistic(given[i]).s;
+      }
+#pragma unroll
+      for (int i = 0; i < kBackRows; ++i)
+        if (i < count) {
+          dskip = __builtin_fmaf(d[i], x[i], dskip);
+          dbias += dv[i];
+        }
+      store_tokens<T>(a.dx, a, col, base, count, dx);
+      store_tokens<S>(a.ddt, a, col, base, count, dv);
+      if (a.z) store_tokens<T>(a.dz, a, col, base, count, dgate);
+      __syncthreads();
+      for (int i = threadIdx.x; i < count * 2 * NP; i += F::kWaves * 64) {
+        float s = 0.f;
+#pragma unroll
+        for (int v = 0; v < F::kWaves; ++v) s += sums[v * kBackRows * 2 * NP + i];
+        const size_t t = base + i / (2 * NP);
+        a.dbc[(((size_t)in_group * a.T + t) * a.G + group) * (2 * NP) + i % (2 * NP)] = s;
+      }
+      __syncthreads();
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < (g1 - g0) * 2 * NP; i += F::kWaves * 64) {
-      float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < F::kWaves; ++w) s += sums[(size_t)w * F::kGroup * 2 * NP + i];
-      const size_t t = g0 + i / (2 * NP);
-      a.dbc[(((size_t)in_group * a.T + t) * a.G + group) * (2 * NP) + i % (2 * NP)] = s;
-    }
-    __syncthreads();
   }
   if (!col.mine) return;
   float *out = a.dweights + (size_t)chunk * (NP + 2) * a.D + c;
@@ -316,21 +372,19 @@ __global__ __launch_bounds__(1024) void ssm_sum_weights_kernel(SsmArgs a, int pa
 }
 
 hipError_t launch_ssm_backward(const SsmArgs &a, bool bf16, bool dt_bf16, hipStream_t s) {
-  hipError_t e = launch_ssm_setup(a, bf16, s);
-  if (e != hipSuccess) return e;
   return ssm_dispatch(a.S, bf16, dt_bf16, [&](auto t, auto st, auto np) {
     using T = decltype(t);
     using S = decltype(st);
     constexpr int NP = decltype(np)::value;
     using F = BackForm<NP>;
-    const uint32_t cols = (uint32_t)ssm_columns(a.D, a.G) * a.G;
-    const uint32_t quads = (uint32_t)ssm_quads(a.D, a.G, a.S);
-    const long all = (long)a.chunks * cols;
-    if (all > 0x3fffffffl) return hipErrorInvalidValue;
-    hipError_t e = hipSuccess;
+    const uint32_t fours = (uint32_t)((ssm_columns(a.D, a.G) + 3) / 4), quads = (uint32_t)ssm_quads(a.D, a.G, a.S);
+    const long all = (long)a.chunks * quads * a.G;
+    if (all > 0x7fffffffl) return hipErrorInvalidValue;
+    hipError_t e = a.N > kCheckInPlace ? launch_check_offsets(a.cu, a.N, a.T, a.status, s) : hipSuccess;
+    if (e != hipSuccess) return e;
     if (a.chunks > 1) {
-      const uint32_t items = (uint32_t)(all - cols);
-      hipLaunchKernelGGL((ssm_back_local_kernel<T, S, NP>), dim3((items + 3) / 4), dim3(256), 0, s, a, cols, items);
+      hipLaunchKernelGGL((ssm_back_local_kernel<T, S, NP>), dim3((unsigned)((a.chunks - 1l) * fours * a.G)), dim3(256), 0, s, a,
+                         fours);
       e = hipGetLastError();
       if (e == hipSuccess) e = launch_ssm_carry(a, true, s);
       if (e != hipSuccess) return e;
@@ -338,7 +392,7 @@ hipError_t launch_ssm_backward(const SsmArgs &a, bool bf16, bool dt_bf16, hipStr
     const void *kernel = reinterpret_cast<const void *>(&ssm_backward_kernel<T, S, NP>);
     e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)F::kLds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((ssm_backward_kernel<T, S, NP>), dim3((unsigned)((long)a.chunks * quads * a.G)), dim3(F::kWaves * 64),
+    hipLaunchKernelGGL((ssm_backward_kernel<T, S, NP>), dim3((unsigned)all), dim3(F::kWaves * 64),
                        F::kLds, s, a, quads);
     e = hipGetLastError();
     if (e != hipSuccess) return e;

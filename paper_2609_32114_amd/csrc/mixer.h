@@ -79,7 +79,7 @@ constexpr int kMaxStates = 64;
 // States a channel as the kernels hold them: the next of 16, 32 and 64.
 inline int ssm_padded(int S) { return S <= 16 ? 16 : S <= 32 ? 32 : 64; }
 // Tokens between two saved states of the scan (hagdn.h, ssm_prefill).
-inline int ssm_group(int S) { return 512 / ssm_padded(S); }
+constexpr int kSsmGroup = 32;
 
 struct SsmArgs {
   const void *x, *dt, *z, *B, *C, *dy;  // rows of D channels (B, C: of G x S), strides below; z may be null
@@ -97,7 +97,6 @@ struct SsmArgs {
   int cus;
   // workspace
   int *status;
-  float *bc;                            // [T][G][2][padded S]: B and C in fp32
   float *maps;                          // [chunks][padded S][D]: what a chunk leaves of nothing, then what enters it
   float *sums;                          // [chunks][D]: its step sizes' sum
   int *resets;                          // [chunks]: whether a sequence starts (backward: ends) in it
@@ -124,11 +123,12 @@ inline int ssm_waves(int S) { return S <= 32 ? 4 : 2; }
 inline long ssm_quads(int D, int G, int S) { return (ssm_columns(D, G) + ssm_waves(S) - 1) / ssm_waves(S); }
 
 // Tokens of a chunk: one wave goes over a chunk of a column.  As many chunks as give
-// every SIMD four waves, in powers of two from 32 (a group of saved states) to 256 tokens.
-inline int ssm_chunk(int T, int D, int S, int G, int cus) {
+// every SIMD four waves, in powers of two from 16 (backward: 32, a group of saved states) to 256
+// tokens.
+inline int ssm_chunk(int T, int D, int G, int cus, bool backward) {
   const long waves = 16l * (cus > 0 ? cus : 256);
   const long want = (long)T * ssm_columns(D, G) * G / waves;
-  int chunk = 32;
+  int chunk = backward ? kSsmGroup : 16;
   while (chunk < 256 && chunk < want) chunk *= 2;
   return chunk;
 }
@@ -136,9 +136,7 @@ inline int ssm_chunk(int T, int D, int S, int G, int cus) {
 hipError_t launch_ssm_forward(const SsmArgs &, bool bf16, bool dt_bf16, hipStream_t);
 hipError_t launch_ssm_backward(const SsmArgs &, bool bf16, bool dt_bf16, hipStream_t);
 hipError_t launch_ssm_step(const SsmStepArgs &, bool bf16, bool dt_bf16, hipStream_t);
-// Shared by both directions: B and C as fp32 rows, the offsets' check, the status; what
-// enters each chunk from what each leaves of nothing.
-hipError_t launch_ssm_setup(const SsmArgs &, bool bf16, hipStream_t);
+// Shared by both directions: what enters each chunk from what each leaves of nothing.
 hipError_t launch_ssm_carry(const SsmArgs &, bool backward, hipStream_t);
 
 // ------------------------------------------------------------------- state pools

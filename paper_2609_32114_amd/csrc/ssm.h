@@ -4,8 +4,10 @@
 // (per group of channels),
 //   h_t = a_t h_{t-1} + dt_t x_t B_t,  a_t = e^(dt_t A),   y_t = sum_n C_t h_t.
 // A lane holds one channel and all its states in registers, so that the sum over states
-// needs no other lane and B and C, which a wave's 64 channels share, come through scalar
-// registers.  Tokens are cut into chunks, one to a wave:
+// needs no other lane; B and C, which all channels of a group share, come through LDS, where
+// every lane reads the same word (through scalar registers, where each wave waits for its own
+// rows, the longest calls take 1.5 times as long).  Tokens are cut into chunks, one to a
+// wave:
 //   1. every chunk but the last goes from a zero state to what it leaves (and the sum of its
 //      step sizes, which gives its decay e^(A sum dt) without a product per token);
 //   2. what enters each chunk is folded from that, per channel and state;
@@ -15,64 +17,106 @@
 // independent of what enters, whatever that is.
 #pragma once
 
+#include "glr.h"  // row access
 #include "mixer_dev.h"
 
 namespace hagdn {
-
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-#ifdef __HIP_DEVICE_COMPILE__
-#define HAGDN_CONSTANT __attribute__((address_space(4)))
-#else
-#define HAGDN_CONSTANT
-#endif
 
 // A wave's 64 channels: a column of a group of channels.
 struct Column {
   uint32_t group, c;
   bool mine;  // lanes past the last channel follow it and store nothing
-  __device__ Column(uint32_t col, const SsmArgs &a) : Column(col / columns(a), col % columns(a), a) {}
   __device__ Column(uint32_t g, uint32_t col, const SsmArgs &a) : group(g) {
     const uint32_t width = (uint32_t)a.D / a.G, at = col * 64 + lane_id();
     mine = at < width;
     c = g * width + min(at, width - 1);
   }
-  __device__ static uint32_t columns(const SsmArgs &a) { return ((uint32_t)a.D / a.G + 63) / 64; }
 };
 
-// Rows of B and C of a token and group, in scalar registers: 16 states from 16 k on.
-template <int NP> __device__ __forceinline__ const HAGDN_CONSTANT f32x16 *bc_row(const SsmArgs &a, uint32_t t, uint32_t group) {
-  return (const HAGDN_CONSTANT f32x16 *)(a.bc + ((size_t)t * a.G + group) * (2 * NP));
+// B (WHAT 1), C (2) or both (3) of TOKENS tokens of one group as fp32 rows in LDS, padded
+// with zeros, for the columns that a workgroup goes over together.  The next tokens' are on
+// their way in registers meanwhile.
+template <typename T, int NP, int WHAT, int TOKENS, int THREADS> struct Maps {
+  static constexpr int kRow = WHAT == 3 ? 2 * NP : NP, kAll = TOKENS * kRow, kEach = (kAll + THREADS - 1) / THREADS;
+  T v[kEach];
+  __device__ void fetch(const SsmArgs &a, uint32_t group, int t, int end) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int at = e * THREADS + threadIdx.x, token = t + at / kRow, col = at % kRow, n = col % NP;
+      v[e] = T(0);
+      if (at < kAll && token < end && n < a.S) {
+        const bool isC = WHAT == 2 || col >= NP;
+        v[e] = (static_cast<const T *>(isC ? a.C : a.B) + (size_t)token * (isC ? a.Cs : a.Bs))[group * a.S + n];
+      }
+    }
+  }
+  __device__ void put(float *rows) const {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int at = e * THREADS + threadIdx.x;
+      if (at < kAll) rows[at] = Elt<T>::to_f32(v[e]);
+    }
+  }
+};
+
+// A value that the compiler cannot trace back over this place: work on one token is not to be
+// taken out of the loop over a run's sequences, where the work of all tokens at once does not
+// fit the registers.
+#ifdef __HIP_DEVICE_COMPILE__
+__device__ __forceinline__ float here(float v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+__device__ __forceinline__ int here(int v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
+#else
+__device__ __forceinline__ float here(float v) { return v; }
+__device__ __forceinline__ int here(int v) { return v; }
+#endif
+
+// The number of states, for conditions that are not to be kept in registers from one use to
+// the next.
+__device__ __forceinline__ int states(const SsmArgs &a) {
+  return here(a.S);
 }
 
 // log2(e) A of a channel; states past S never decay and are never fed.
 template <int NP> __device__ __forceinline__ void load_rates(const SsmArgs &a, uint32_t c, float (&r)[NP]) {
+  const int count = states(a);
 #pragma unroll
-  for (int n = 0; n < NP; ++n) r[n] = n < a.S ? a.A[(size_t)c * a.S + n] * kLog2e : 0.f;
+  for (int n = 0; n < NP; ++n) r[n] = n < count ? a.A[(size_t)c * a.S + n] * kLog2e : 0.f;
 }
 // Rows [NP][D] of states, at a channel.
 template <int NP> __device__ __forceinline__ void load_states(const float *rows, const SsmArgs &a, uint32_t c, float (&h)[NP]) {
+  const int count = states(a);
 #pragma unroll
-  for (int n = 0; n < NP; ++n) h[n] = n < a.S ? rows[(size_t)n * a.D + c] : 0.f;
+  for (int n = 0; n < NP; ++n) h[n] = n < count ? rows[(size_t)n * a.D + c] : 0.f;
 }
 template <int NP> __device__ __forceinline__ void store_states(float *rows, const SsmArgs &a, const Column &col, const float (&h)[NP]) {
+  const int count = states(a);
   if (!col.mine) return;
 #pragma unroll
   for (int n = 0; n < NP; ++n)
-    if (n < a.S) rows[(size_t)n * a.D + col.c] = h[n];
+    if (n < count) rows[(size_t)n * a.D + col.c] = h[n];
 }
-// A sequence's state [D][S] in its caller's order; null: zero.
-template <int NP> __device__ __forceinline__ void load_sequence(const float *s, int seq, const SsmArgs &a, uint32_t c, float (&h)[NP]) {
-  const float *row = s + ((size_t)seq * a.D + c) * a.S;
+// Some of a sequence's states, from the first-th on, in its caller's order [D][S]; null: zero.
+template <int NP>
+__device__ __forceinline__ void load_sequence(const float *s, int seq, const SsmArgs &a, uint32_t c, float *h, int first = 0) {
+  const int count = s ? states(a) - first : 0;
+  const float *row = s + ((size_t)seq * a.D + c) * a.S + first;
 #pragma unroll
-  for (int n = 0; n < NP; ++n) h[n] = s && n < a.S ? row[n] : 0.f;
+  for (int n = 0; n < NP; ++n) h[n] = n < count ? row[n] : 0.f;
 }
 template <int NP>
-__device__ __forceinline__ void store_sequence(float *s, int seq, const SsmArgs &a, const Column &col, const float (&h)[NP]) {
-  if (!s || !col.mine) return;
-  float *row = s + ((size_t)seq * a.D + col.c) * a.S;
+__device__ __forceinline__ void store_sequence(float *s, int seq, const SsmArgs &a, const Column &col, const float *h, int first = 0) {
+  const int count = s ? states(a) - first : 0;
+  if (count <= 0 || !col.mine) return;
+  float *row = s + ((size_t)seq * a.D + col.c) * a.S + first;
 #pragma unroll
   for (int n = 0; n < NP; ++n)
-    if (n < a.S) row[n] = h[n];
+    if (n < count) row[n] = h[n];
 }
 // States of the sequences without tokens pass through.
 __device__ __forceinline__ void pass_states(const SsmArgs &a, bool ok, const float *in, float *out, const Column &col) {
@@ -81,6 +125,47 @@ __device__ __forceinline__ void pass_states(const SsmArgs &a, bool ok, const flo
     const size_t at = ((size_t)seq * a.D + col.c) * a.S;
     for (int n = 0; n < a.S && col.mine; ++n) out[at + n] = in ? in[at + n] : 0.f;
   });
+}
+
+// Element c of N rows of a token matrix from t on, the last one before `end` in place of rows
+// from there on.
+template <typename T, int N>
+__device__ __forceinline__ void load_tokens(const void *rows, long stride, int t, int end, uint32_t c, T (&v)[N]) {
+  const T *p = static_cast<const T *>(rows) + (size_t)t * stride;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = *in_row(p, c);
+    p += t + i + 1 < end ? stride : 0;
+  }
+}
+// The first `count` of N values to rows from t on.
+template <typename T, int N>
+__device__ __forceinline__ void store_tokens(void *rows, const SsmArgs &a, const Column &col, int t, int count, const float (&v)[N]) {
+  if (!col.mine) return;
+  Rows<T> out(static_cast<T *>(rows) + (size_t)t * a.D, a.D, col.c);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (i < count) *out.here() = Elt<T>::from_f32(v[i]);
+    out.advance();
+  }
+}
+// Step sizes, in 32 bits, from what is given, which raw ones follow with their bias.
+template <typename S, int N>
+__device__ __forceinline__ void step_sizes(const SsmArgs &a, const S (&given)[N], float bias, float (&v)[N], float (&step)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) step[i] = v[i] = Elt<S>::to_f32(given[i]) + bias;
+  if (!a.raw) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i) step[i] = softplus(v[i]);
+}
+
+// Whether the offsets are right: asked here, or told by the kernel before.  The whole
+// workgroup calls; the call's first one tells the host.
+__device__ __forceinline__ bool ssm_offsets_ok(const SsmArgs &a) {
+  if (a.N > kCheckInPlace) return *a.status == 0;
+  const bool ok = offsets_ok(a.cu, a.N, a.T);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
+  return ok;
 }
 
 // The instance of a launcher for a call's types and padded states:
