@@ -377,7 +377,7 @@ int hagdn_conv_decode(const void *x, int64_t x_stride, const float *weight, cons
  *   between tokens);
  *   A [D, S], skip [D] (or NULL) fp32;  S = 1 .. 64;  D % G == 0;
  *   states [N, D, S] fp32; s0 NULL: zero.
- * dt A <= 0 is expected: where a chunk of up to 256 tokens lets a state grow by e^88
+ * dt A <= 0 is expected: where some 500 tokens together let a state grow by e^88
  * results are unspecified.  N x D x S below 2^31.  Sums and states are fp32.  Outputs must
  * not overlap inputs (s_final not even s0 exactly, nor ds0 dfinal).  Results repeat bit
  * for bit on one device.  No value of one sequence reaches another. */

@@ -136,7 +136,7 @@ struct SsmPlan {
 SsmPlan ssm_plan(int T, int D, int S, int G, bool backward) {
   SsmPlan p = {};
   const size_t np = hagdn::ssm_padded(S);
-  p.chunk = hagdn::ssm_chunk(T, D, G, query_cus(), backward);
+  p.chunk = hagdn::ssm_chunk(T, D, S, G, query_cus(), backward);
   p.chunks = T > 0 ? (T - 1) / p.chunk + 1 : 1;
   const size_t between = p.chunks > 1 ? p.chunks : 0;  // one chunk leaves nothing to another
   size_t at = hagdn::kMixerHeader;

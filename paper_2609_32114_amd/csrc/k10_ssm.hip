@@ -21,6 +21,14 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan
   const int t0 = chunk * a.chunk, t1 = (int)min((long)t0 + a.chunk, (long)a.T);
   if (!ok || t0 >= t1) return;
 
+  // x, dt, B and C of the first tokens are on their way before anything waits; z, which only
+  // the outputs need, is read in its turn
+  T x[kSsmRows], z[kSsmRows];
+  S dt[kSsmRows];
+  Stage stage;
+  load_tokens(a.dt, a.dts, t0, t1, c, dt);
+  load_tokens(a.x, a.xs, t0, t1, c, x);
+  stage.fetch(a, group, t0, t1);
   float A[NP], h[NP];
   load_rates(a, c, A);
   if (OUT && chunk > 0) load_states(a.maps + (size_t)chunk * NP * a.D, a, c, h);
@@ -30,23 +38,27 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan
   int first = q.start == t0 ? t0 : q.end;  // the next token that starts a sequence
   bool reset = false;
   float sum = 0.f;
-  Stage stage;
-  stage.fetch(a, group, t0, t1);
   int turn = 0;
   for (int base = t0; base < t1; base += kSsmRows, turn ^= 1) {
     const int count = min(kSsmRows, t1 - base);
-    const float *rows = sMaps[turn];
-    T x[kSsmRows], z[kSsmRows];
-    S dt[kSsmRows];
-    load_tokens(a.x, a.xs, base, t1, c, x);
-    load_tokens(a.dt, a.dts, base, t1, c, dt);
-    if (OUT && a.z) load_tokens(a.z, a.zs, base, t1, c, z);
     stage.put(sMaps[turn]);
     __syncthreads();
-    if (base + kSsmRows < t1) stage.fetch(a, group, base + kSsmRows, t1);
-    if (OUT && a.ckpt && base % kSsmGroup == 0) store_states(a.ckpt + (size_t)(base / kSsmGroup) * NP * a.D, a, col, h);
-    float given[kSsmRows], step[kSsmRows], y[kSsmRows];
+    if (col.idle) {
+      if (base + kSsmRows < t1) stage.fetch(a, group, base + kSsmRows, t1);
+      continue;
+    }
+    float u[kSsmRows], given[kSsmRows], step[kSsmRows], y[kSsmRows];
     step_sizes(a, dt, bias, given, step);
+#pragma unroll
+    for (int i = 0; i < kSsmRows; ++i) u[i] = Elt<T>::to_f32(x[i]);
+    if (OUT && a.z) load_tokens(a.z, a.zs, base, t1, c, z);
+    if (base + kSsmRows < t1) {
+      load_tokens(a.dt, a.dts, base + kSsmRows, t1, c, dt);
+      load_tokens(a.x, a.xs, base + kSsmRows, t1, c, x);
+      stage.fetch(a, group, base + kSsmRows, t1);
+    }
+    if (OUT && a.ckpt && base % kSsmGroup == 0) store_states(a.ckpt + (size_t)(base / kSsmGroup) * NP * a.D, a, col, h);
+    LdsRows rows(sMaps[0], turn * Stage::kAll);
     for (int lo = 0; lo < count;) {  // from one sequence's first token to the next one's
       if (base + lo == first) {
         if (first == q.end) q.next();
@@ -58,19 +70,18 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan
 #pragma unroll
       for (int i = 0; i < kSsmRows; ++i)
         if (i >= lo && i < hi) {
-          const float *row = rows + here(i * Stage::kRow);
-          const float v = here(step[i]);
-          const float u = Elt<T>::to_f32(x[i]), in = v * u;
-          if (!OUT) sum += v;
-          y[i] = skip * u;
+          rows.hold();
+          HAGDN_OPAQUE_VECTOR(step[i]);
+          const float in = step[i] * u[i];
+          if (!OUT) sum += step[i];
+          y[i] = skip * u[i];
 #pragma unroll
           for (int n = 0; n < NP; n += 4) {
-            const f32x4 B = *reinterpret_cast<const f32x4 *>(row + n);
-            const f32x4 C = OUT ? *reinterpret_cast<const f32x4 *>(row + NP + n) : f32x4{};
+            const f32x4 B = rows.four(i * Stage::kRow + n), C = OUT ? rows.four(i * Stage::kRow + NP + n) : f32x4{};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               float &s = h[n + k];
-              s = __builtin_fmaf(__builtin_amdgcn_exp2f(v * A[n + k]), s, in * B[k]);
+              s = __builtin_fmaf(__builtin_amdgcn_exp2f(step[i] * A[n + k]), s, in * B[k]);
               if (OUT) y[i] = __builtin_fmaf(C[k], s, y[i]);
             }
           }

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back
   stage.fetch(a, group, base, t1);
   for (; base >= t0; base -= kBackRows, turn ^= 1) {
     const int count = min(kBackRows, t1 - base);
-    const float *rows = sMaps[turn];
+    LdsRows rows(sMaps[0], turn * Stage::kAll);
     T dy[kBackRows], z[kBackRows];
     S dt[kBackRows];
     load_tokens(a.dy, a.dys, base, t1, c, dy);
@@ -45,6 +45,7 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back
     stage.put(sMaps[turn]);
     __syncthreads();
     if (base > t0) stage.fetch(a, group, base - kBackRows, t1);
+    if (col.idle) continue;
     float given[kBackRows], step[kBackRows], d[kBackRows];
     step_sizes(a, dt, bias, given, step);
 #pragma unroll
@@ -63,16 +64,16 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back
 #pragma unroll
       for (int i = kBackRows - 1; i >= 0; --i)
         if (i >= lo && i < hi) {
-          const float *row = rows + here(i * Stage::kRow);
-          const float u = here(step[i]);
-          sum += u;
+          rows.hold();
+          HAGDN_OPAQUE_VECTOR(step[i]);
+          sum += step[i];
 #pragma unroll
           for (int n = 0; n < NP; n += 4) {
-            const f32x4 C = *reinterpret_cast<const f32x4 *>(row + n);
+            const f32x4 C = rows.four(i * Stage::kRow + n);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               float &v = e[n + k];
-              v = __builtin_amdgcn_exp2f(u * A[n + k]) * __builtin_fmaf(C[k], d[i], v);
+              v = __builtin_amdgcn_exp2f(step[i] * A[n + k]) * __builtin_fmaf(C[k], d[i], v);
             }
           }
         }
@@ -149,6 +150,8 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
   if (ok && chunk + 1 < a.chunks) load_states(a.maps + (size_t)chunk * NP * a.D, a, c, e);
   const float bias = a.raw && a.bias ? a.bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
 
+  // waves of the workgroup that have channels
+  const int working = min(F::kWaves, (int)(((uint32_t)a.D / a.G + 63) / 64 - in_group * F::kWaves));
   Stage stage;
   for (int g0 = t0 + (t1 - 1 - t0) / kSsmGroup * kSsmGroup; t1 > t0 && g0 >= t0; g0 -= kSsmGroup) {
     const int g1 = min(g0 + kSsmGroup, t1), runs = (g1 - g0 + kBackRows - 1) / kBackRows;
@@ -160,7 +163,7 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
       __syncthreads();
       Cursor q(a.cu, a.N, a.T, g0);
       int first = q.start == g0 ? g0 : q.end;
-      for (int run = 0; run < runs; ++run) {
+      for (int run = 0; run < runs && !col.idle; ++run) {
 #pragma unroll
         for (int n = 0; n < NP; ++n) starts[(run * NP + n) * 64] = h[n];
         if (run + 1 == runs) break;
@@ -171,6 +174,7 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
         load_tokens(a.dt, a.dts, base, t1, c, dt);
         float given[kBackRows], step[kBackRows];
         step_sizes(a, dt, bias, given, step);
+        LdsRows rows(maps, run * kBackRows * 2 * NP);
         for (int lo = 0; lo < kBackRows;) {
           if (base + lo == first) {
             if (first == q.end) q.next();
@@ -181,14 +185,15 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
 #pragma unroll
           for (int i = 0; i < kBackRows; ++i)
             if (i >= lo && i < hi) {
-              const float *row = maps + here((run * kBackRows + i) * 2 * NP);
-              const float u = here(step[i]), in = u * Elt<T>::to_f32(x[i]);
+              rows.hold();
+              HAGDN_OPAQUE_VECTOR(step[i]);
+              const float in = step[i] * Elt<T>::to_f32(x[i]);
 #pragma unroll
               for (int n = 0; n < NP; n += 4) {
-                const f32x4 B = *reinterpret_cast<const f32x4 *>(row + n);
+                const f32x4 B = rows.four(i * 2 * NP + n);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                  h[n + k] = __builtin_fmaf(__builtin_amdgcn_exp2f(u * A[n + k]), h[n + k], in * B[k]);
+                  h[n + k] = __builtin_fmaf(__builtin_amdgcn_exp2f(step[i] * A[n + k]), h[n + k], in * B[k]);
               }
             }
           lo = hi;
@@ -197,129 +202,133 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
     }
     for (int run = runs - 1; run >= 0; --run) {
       const int base = g0 + run * kBackRows, count = min(kBackRows, g1 - base);
-      const float *rows = maps + run * kBackRows * 2 * NP;
-      float x[kBackRows], given[kBackRows], step[kBackRows], d[kBackRows], dgate[kBackRows];
-      {
-        T xs[kBackRows], dys[kBackRows], zs[kBackRows];
-        S dts[kBackRows];
-        load_tokens(a.x, a.xs, base, g1, c, xs);
-        load_tokens(a.dt, a.dts, base, g1, c, dts);
-        load_tokens(a.dy, a.dys, base, g1, c, dys);
-        if (a.z) load_tokens(a.z, a.zs, base, g1, c, zs);
-        step_sizes(a, dts, bias, given, step);
-#pragma unroll
-        for (int i = 0; i < kBackRows; ++i) {
-          x[i] = Elt<T>::to_f32(xs[i]);
-          d[i] = col.mine ? Elt<T>::to_f32(dys[i]) : 0.f;
-        }
-        if (a.z) {  // the gradient of the ungated output, and of z but for that output
+      if (!col.idle) {
+        LdsRows rows(maps, run * kBackRows * 2 * NP);
+        float x[kBackRows], given[kBackRows], step[kBackRows], d[kBackRows], dgate[kBackRows];
+        {
+          T xs[kBackRows], dys[kBackRows], zs[kBackRows];
+          S dts[kBackRows];
+          load_tokens(a.x, a.xs, base, g1, c, xs);
+          load_tokens(a.dt, a.dts, base, g1, c, dts);
+          load_tokens(a.dy, a.dys, base, g1, c, dys);
+          if (a.z) load_tokens(a.z, a.zs, base, g1, c, zs);
+          step_sizes(a, dts, bias, given, step);
 #pragma unroll
           for (int i = 0; i < kBackRows; ++i) {
-            const float z = Elt<T>::to_f32(zs[i]);
-            const Logistic g = logistic(z);
-            dgate[i] = d[i] * (g.s * __builtin_fmaf(z, g.rest, 1.f));
-            d[i] *= z * g.s;
+            x[i] = Elt<T>::to_f32(xs[i]);
+            d[i] = col.mine ? Elt<T>::to_f32(dys[i]) : 0.f;
+          }
+          if (a.z) {  // the gradient of the ungated output, and of z but for that output
+#pragma unroll
+            for (int i = 0; i < kBackRows; ++i) {
+              const float z = Elt<T>::to_f32(zs[i]);
+              const Logistic g = logistic(z);
+              dgate[i] = d[i] * (g.s * __builtin_fmaf(z, g.rest, 1.f));
+              d[i] *= z * g.s;
+            }
           }
         }
-      }
-      float y[kBackRows], w[kBackRows], ds[kBackRows];
+        float y[kBackRows], w[kBackRows], ds[kBackRows];
 #pragma unroll
-      for (int i = 0; i < kBackRows; ++i) {
-        y[i] = skip * x[i];
-        w[i] = ds[i] = 0.f;
-      }
-      const Cursor at(a.cu, a.N, a.T, base);
+        for (int i = 0; i < kBackRows; ++i) {
+          y[i] = skip * x[i];
+          w[i] = ds[i] = 0.f;
+        }
+        const Cursor at(a.cu, a.N, a.T, base);
 #pragma unroll
-      for (int n0 = 0; n0 < NP; n0 += kSlice) {
-        float kept[kBackRows][kSlice], h[kSlice];  // kept: a_t h_{t-1}
+        for (int n0 = 0; n0 < NP; n0 += kSlice) {
+          float kept[kBackRows][kSlice], h[kSlice];  // kept: a_t h_{t-1}
 #pragma unroll
-        for (int k = 0; k < kSlice; ++k) h[k] = starts[(run * NP + n0 + k) * 64];
-        Cursor q = at;
-        int first = q.start == base ? base : q.end;
-        for (int lo = 0; lo < count;) {
-          if (base + lo == first) {
-            if (first == q.end) q.next();
-            load_sequence<kSlice>(a.s0, q.seq, a, c, h, n0);
-            first = q.end;
+          for (int k = 0; k < kSlice; ++k) h[k] = starts[(run * NP + n0 + k) * 64];
+          Cursor q = at;
+          int first = q.start == base ? base : q.end;
+          for (int lo = 0; lo < count;) {
+            if (base + lo == first) {
+              if (first == q.end) q.next();
+              load_sequence<kSlice>(a.s0, q.seq, a, c, h, n0);
+              first = q.end;
+            }
+            const int hi = min(count, first - base);
+#pragma unroll
+            for (int i = 0; i < kBackRows; ++i)
+              if (i >= lo && i < hi) {
+                rows.hold();
+                HAGDN_OPAQUE_VECTOR(step[i]);
+                const float in = step[i] * x[i];
+#pragma unroll
+                for (int n = 0; n < kSlice; n += 4) {
+                  const f32x4 B = rows.four(i * 2 * NP + n0 + n);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) {
+                    kept[i][n + k] = __builtin_amdgcn_exp2f(step[i] * A[n0 + n + k]) * h[n + k];
+                    h[n + k] = __builtin_fmaf(in, B[k], kept[i][n + k]);
+                  }
+                }
+              }
+            lo = hi;
           }
-          const int hi = min(count, first - base);
+          for (int hi = count; hi > 0;) {
+            if (base + hi == q.start) q.previous();
+            if (base + hi == q.end) load_sequence<kSlice>(a.dfinal, q.seq, a, c, e + n0, n0);
+            const int lo = max(0, q.start - base);
 #pragma unroll
-          for (int i = 0; i < kBackRows; ++i)
-            if (i >= lo && i < hi) {
-              const float *row = rows + here(i * 2 * NP + n0);
-              const float u = here(step[i]), in = u * x[i];
+            for (int i = kBackRows - 1; i >= 0; --i)
+              if (i >= lo && i < hi) {
+                rows.hold();
+                HAGDN_OPAQUE_VECTOR(step[i]);
+                const float in = step[i] * x[i];
+                const float fed = col.mine ? in : 0.f;
+                float terms[2 * kSlice];  // of dB and dC
 #pragma unroll
-              for (int n = 0; n < kSlice; n += 4) {
-                const f32x4 B = *reinterpret_cast<const f32x4 *>(row + n);
+                for (int m = 0; m < kSlice; m += 4) {
+                  const f32x4 B = rows.four(i * 2 * NP + n0 + m), C = rows.four(i * 2 * NP + NP + n0 + m);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  kept[i][n + k] = __builtin_amdgcn_exp2f(u * A[n0 + n + k]) * h[n + k];
-                  h[n + k] = __builtin_fmaf(in, B[k], kept[i][n + k]);
+                  for (int j = 0; j < 4; ++j) {
+                    const int k = m + j, n = n0 + k;
+                    const float hn = __builtin_fmaf(in, B[j], kept[i][k]), dh = __builtin_fmaf(C[j], d[i], e[n]);
+                    y[i] = __builtin_fmaf(C[j], hn, y[i]);
+                    w[i] = __builtin_fmaf(B[j], dh, w[i]);
+                    terms[k] = dh * fed;
+                    terms[kSlice + k] = d[i] * hn;
+                    const float p = dh * kept[i][k];
+                    ds[i] = __builtin_fmaf(A[n], p, ds[i]);
+                    dA[n] = __builtin_fmaf(step[i], p, dA[n]);
+                    e[n] = __builtin_amdgcn_exp2f(step[i] * A[n]) * dh;
+                  }
                 }
+                const float sum = sum_lanes(terms);
+                if ((lane & 3) == 0)
+                  sums[(wave * kBackRows + i) * 2 * NP + n0 + ((lane >> 2) & 7) + (lane >= 32 ? NP : 0)] = sum;
               }
-            }
-          lo = hi;
+            if (base + lo == q.start) store_sequence<kSlice>(a.ds0, q.seq, a, col, e + n0, n0);
+            hi = lo;
+          }
         }
-        for (int hi = count; hi > 0;) {
-          if (base + hi == q.start) q.previous();
-          if (base + hi == q.end) load_sequence<kSlice>(a.dfinal, q.seq, a, c, e + n0, n0);
-          const int lo = max(0, q.start - base);
+        float dx[kBackRows], dv[kBackRows];
 #pragma unroll
-          for (int i = kBackRows - 1; i >= 0; --i)
-            if (i >= lo && i < hi) {
-              const float *row = rows + here(i * 2 * NP + n0);
-              const float u = here(step[i]), in = u * x[i];
-              float terms[2 * kSlice];  // of dB and dC
-#pragma unroll
-              for (int m = 0; m < kSlice; m += 4) {
-                const f32x4 B = *reinterpret_cast<const f32x4 *>(row + m), C = *reinterpret_cast<const f32x4 *>(row + NP + m);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  const int k = m + j, n = n0 + k;
-                  const float hn = __builtin_fmaf(in, B[j], kept[i][k]), dh = __builtin_fmaf(C[j], d[i], e[n]);
-                  y[i] = __builtin_fmaf(C[j], hn, y[i]);
-                  w[i] = __builtin_fmaf(B[j], dh, w[i]);
-                  terms[k] = col.mine ? dh * in : 0.f;
-                  terms[kSlice + k] = d[i] * hn;
-                  const float p = dh * kept[i][k];
-                  ds[i] = __builtin_fmaf(A[n], p, ds[i]);
-                  dA[n] = __builtin_fmaf(u, p, dA[n]);
-                  e[n] = __builtin_amdgcn_exp2f(u * A[n]) * dh;
-                }
-              }
-              const float sum = sum_lanes(terms);
-              if ((lane & 3) == 0)
-                sums[(wave * kBackRows + i) * 2 * NP + n0 + ((lane >> 2) & 7) + (lane >= 32 ? NP : 0)] = sum;
-            }
-          if (base + lo == q.start) store_sequence<kSlice>(a.ds0, q.seq, a, col, e + n0, n0);
-          hi = lo;
+        for (int i = 0; i < kBackRows; ++i) {
+          dx[i] = __builtin_fmaf(skip, d[i], step[i] * w[i]);
+          dv[i] = __builtin_fmaf(ds[i], 1.f / kLog2e, x[i] * w[i]);
+          dgate[i] *= y[i];
         }
-      }
-      float dx[kBackRows], dv[kBackRows];
+        if (a.raw) {
 #pragma unroll
-      for (int i = 0; i < kBackRows; ++i) {
-        dx[i] = __builtin_fmaf(skip, d[i], step[i] * w[i]);
-        dv[i] = __builtin_fmaf(ds[i], 1.f / kLog2e, x[i] * w[i]);
-        dgate[i] *= y[i];
-      }
-      if (a.raw) {
-#pragma unroll
-        for (int i = 0; i < kBackRows; ++i) dv[i] *= logistic(given[i]).s;
-      }
-#pragma unroll
-      for (int i = 0; i < kBackRows; ++i)
-        if (i < count) {
-          dskip = __builtin_fmaf(d[i], x[i], dskip);
-          dbias += dv[i];
+          for (int i = 0; i < kBackRows; ++i) dv[i] *= logistic(given[i]).s;
         }
-      store_tokens<T>(a.dx, a, col, base, count, dx);
-      store_tokens<S>(a.ddt, a, col, base, count, dv);
-      if (a.z) store_tokens<T>(a.dz, a, col, base, count, dgate);
+#pragma unroll
+        for (int i = 0; i < kBackRows; ++i)
+          if (i < count) {
+            dskip = __builtin_fmaf(d[i], x[i], dskip);
+            dbias += dv[i];
+          }
+        store_tokens<T>(a.dx, a, col, base, count, dx);
+        store_tokens<S>(a.ddt, a, col, base, count, dv);
+        if (a.z) store_tokens<T>(a.dz, a, col, base, count, dgate);
+      }
       __syncthreads();
       for (int i = threadIdx.x; i < count * 2 * NP; i += F::kWaves * 64) {
         float s = 0.f;
-#pragma unroll
-        for (int v = 0; v < F::kWaves; ++v) s += sums[v * kBackRows * 2 * NP + i];
+        for (int v = 0; v < working; ++v) s += sums[v * kBackRows * 2 * NP + i];
         const size_t t = base + i / (2 * NP);
         a.dbc[(((size_t)in_group * a.T + t) * a.G + group) * (2 * NP) + i % (2 * NP)] = s;
       }

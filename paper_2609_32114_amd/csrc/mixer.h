@@ -122,15 +122,21 @@ inline long ssm_columns(int D, int G) { return ((long)D / G + 63) / 64; }
 inline int ssm_waves(int S) { return S <= 32 ? 4 : 2; }
 inline long ssm_quads(int D, int G, int S) { return (ssm_columns(D, G) + ssm_waves(S) - 1) / ssm_waves(S); }
 
-// Tokens of a chunk: one wave goes over a chunk of a column.  As many chunks as give
-// every SIMD four waves, in powers of two from 16 (backward: 32, a group of saved states) to 256
-// tokens.
-inline int ssm_chunk(int T, int D, int G, int cus, bool backward) {
-  const long waves = 16l * (cus > 0 ? cus : 256);
-  const long want = (long)T * ssm_columns(D, G) * G / waves;
-  int chunk = backward ? kSsmGroup : 16;
-  while (chunk < 256 && chunk < want) chunk *= 2;
-  return chunk;
+// Tokens of a chunk: a workgroup goes over a chunk of its four columns.  The scan is bound by
+// its arithmetic, so that every CU should get as many workgroups as the others: one round of
+// what can be resident (four a CU; backward two, of most states one), or in calls where a
+// chunk would pass 512 tokens as few rounds as keep it below.  (17401 x 2048 tokens in 68 chunks
+// of 256, 2.1 workgroups a CU: outputs 230 us, backward 1022; in chunks of 136 and 288, 160 and
+// 730.)
+// Calls of up to 64 tokens are one chunk, which needs one launch instead of three.
+inline int ssm_chunk(int T, int D, int S, int G, int cus, bool backward) {
+  const long each = backward ? ssm_quads(D, G, S) * G : (ssm_columns(D, G) + 3) / 4 * G;
+  const long slots = (cus > 0 ? cus : 256) * (backward ? (S <= 16 ? 2l : 1l) : 4l);
+  const auto over = [](long a, long b) { return (a + b - 1) / b; };
+  const long total = (long)T * each, rounds = over(total + 1, slots * 512);
+  const int unit = backward ? kSsmGroup : 8, least = T <= 64 ? 64 : backward ? kSsmGroup : 16;
+  const long chunk = over(over(total, slots * rounds), unit) * unit;
+  return (int)(chunk < least ? least : chunk);
 }
 
 hipError_t launch_ssm_forward(const SsmArgs &, bool bf16, bool dt_bf16, hipStream_t);

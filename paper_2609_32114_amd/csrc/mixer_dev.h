@@ -36,7 +36,7 @@ __device__ __forceinline__ float softplus(float v) {
   p = __builtin_fmaf(p, q, 0.39998711f);
   p = __builtin_fmaf(p, q, 0.66666679f);
   p = __builtin_fmaf(p, q, 2.f);
-  return __builtin_fmaf(r, p, v > 0.f ? v : 0.f);
+  return __builtin_fmaf(r, p, __builtin_fmaxf(v, 0.f));  // (a NaN comes through r)
 }
 
 // V consecutive elements, aligned as one of them is.

@@ -26,9 +26,11 @@ namespace hagdn {
 struct Column {
   uint32_t group, c;
   bool mine;  // lanes past the last channel follow it and store nothing
+  bool idle;  // all of them: the wave only helps with what its workgroup shares
   __device__ Column(uint32_t g, uint32_t col, const SsmArgs &a) : group(g) {
     const uint32_t width = (uint32_t)a.D / a.G, at = col * 64 + lane_id();
     mine = at < width;
+    idle = col * 64 >= width;
     c = g * width + min(at, width - 1);
   }
 };
@@ -59,34 +61,55 @@ template <typename T, int NP, int WHAT, int TOKENS, int THREADS> struct Maps {
   }
 };
 
-// A value that the compiler cannot trace back over this place: work on one token is not to be
+// The compiler cannot trace a value back over this place: work on one token is not to be
 // taken out of the loop over a run's sequences, where the work of all tokens at once does not
 // fit the registers.
 #ifdef __HIP_DEVICE_COMPILE__
-__device__ __forceinline__ float here(float v) {
-  asm volatile("" : "+v"(v));
-  return v;
-}
-__device__ __forceinline__ int here(int v) {
-  asm volatile("" : "+s"(v));
-  return v;
-}
+#define HAGDN_OPAQUE_VECTOR(v) asm volatile("" : "+v"(v))
+#define HAGDN_OPAQUE_SCALAR(v) asm volatile("" : "+s"(v))
 #else
-__device__ __forceinline__ float here(float v) { return v; }
-__device__ __forceinline__ int here(int v) { return v; }
+#define HAGDN_OPAQUE_VECTOR(v)
+#define HAGDN_OPAQUE_SCALAR(v)
 #endif
+
+// Rows of floats in LDS at a lane's byte offset, which is opaque (above) in its own register,
+// so that the rows' distances become the accesses' constants.
+struct LdsRows {
+  const HAGDN_LDS char *base;
+  uint32_t at;
+  __device__ LdsRows(const float *p, uint32_t first) : base((const HAGDN_LDS char *)p), at(first * 4) { HAGDN_OPAQUE_VECTOR(at); }
+  __device__ void hold() { HAGDN_OPAQUE_VECTOR(at); }
+  __device__ f32x4 four(int i) const { return *(const HAGDN_LDS f32x4 *)(base + at + i * 4); }
+};
 
 // The number of states, for conditions that are not to be kept in registers from one use to
 // the next.
 __device__ __forceinline__ int states(const SsmArgs &a) {
-  return here(a.S);
+  int n = a.S;
+  HAGDN_OPAQUE_SCALAR(n);
+  return n;
+}
+
+// The first `count` of NP floats of a lane's row, the others zero.
+template <int NP> __device__ __forceinline__ void load_row(const float *row, int count, float *v) {
+  if (count >= NP) {
+#pragma unroll
+    for (int n = 0; n < NP; n += 4) {
+      const auto p = load_pack<float, 4>(row, n);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[n + k] = p.v[k];
+    }
+    return;
+  }
+#pragma unroll
+  for (int n = 0; n < NP; ++n) v[n] = n < count ? row[n] : 0.f;
 }
 
 // log2(e) A of a channel; states past S never decay and are never fed.
 template <int NP> __device__ __forceinline__ void load_rates(const SsmArgs &a, uint32_t c, float (&r)[NP]) {
-  const int count = states(a);
+  load_row<NP>(a.A + (size_t)c * a.S, states(a), r);
 #pragma unroll
-  for (int n = 0; n < NP; ++n) r[n] = n < count ? a.A[(size_t)c * a.S + n] * kLog2e : 0.f;
+  for (int n = 0; n < NP; ++n) r[n] *= kLog2e;
 }
 // Rows [NP][D] of states, at a channel.
 template <int NP> __device__ __forceinline__ void load_states(const float *rows, const SsmArgs &a, uint32_t c, float (&h)[NP]) {
@@ -104,16 +127,18 @@ template <int NP> __device__ __forceinline__ void store_states(float *rows, cons
 // Some of a sequence's states, from the first-th on, in its caller's order [D][S]; null: zero.
 template <int NP>
 __device__ __forceinline__ void load_sequence(const float *s, int seq, const SsmArgs &a, uint32_t c, float *h, int first = 0) {
-  const int count = s ? states(a) - first : 0;
-  const float *row = s + ((size_t)seq * a.D + c) * a.S + first;
-#pragma unroll
-  for (int n = 0; n < NP; ++n) h[n] = n < count ? row[n] : 0.f;
+  load_row<NP>(s + ((size_t)seq * a.D + c) * a.S + first, s ? states(a) - first : 0, h);
 }
 template <int NP>
 __device__ __forceinline__ void store_sequence(float *s, int seq, const SsmArgs &a, const Column &col, const float *h, int first = 0) {
   const int count = s ? states(a) - first : 0;
   if (count <= 0 || !col.mine) return;
   float *row = s + ((size_t)seq * a.D + col.c) * a.S + first;
+  if (count >= NP) {
+#pragma unroll
+    for (int n = 0; n < NP; n += 4) store_pack<float, 4>(row, n, Pack<float, 4>{{h[n], h[n + 1], h[n + 2], h[n + 3]}});
+    return;
+  }
 #pragma unroll
   for (int n = 0; n < NP; ++n)
     if (n < count) row[n] = h[n];
@@ -131,11 +156,11 @@ __device__ __forceinline__ void pass_states(const SsmArgs &a, bool ok, const flo
 // from there on.
 template <typename T, int N>
 __device__ __forceinline__ void load_tokens(const void *rows, long stride, int t, int end, uint32_t c, T (&v)[N]) {
-  const T *p = static_cast<const T *>(rows) + (size_t)t * stride;
+  Rows<const T> row(static_cast<const T *>(rows) + (size_t)t * stride, stride, c);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    v[i] = *in_row(p, c);
-    p += t + i + 1 < end ? stride : 0;
+    v[i] = *row.here();
+    if (t + i + 1 < end) row.advance();
   }
 }
 // The first `count` of N values to rows from t on.

@@ -7,7 +7,7 @@ relative.  A logistic function is off by (|v| + 5) EPS relative (the exponent's 
 an ulp each of exponential and reciprocal), its product or slope by 3 EPS more.  A step
 size log(1 + e^v) is off by (2 |v| + 8) EPS relative: v's own sum, the exponential, a quotient
 and a polynomial of six terms.  A decay e^(dt A) takes |dt A| times its exponent's error; where
-chunks of at most 256 tokens are folded, the exponent is a sum of so many step sizes, 128
+chunks of at most 520 tokens are folded, the exponent is a sum of so many step sizes, 260
 EPS more.  An error travels the way its value does, so its bound obeys the value's own
 recurrence over magnitudes; regrouping a recurrence into chunks at most doubles it.  A sum of n
 terms costs n EPS of the sum of magnitudes, one over 64 lanes and columns (D / 64 + 24) EPS,
@@ -103,7 +103,7 @@ def ssm(x, dt, A, B, C, lens, skip=None, z=None, bias=None, s0=None, raw=False, 
     Bd, Cd = B[:, group], C[:, group]
     rate = step[..., None] * A
     a = np.exp(rate)
-    ga = np.abs(rate) * (rstep[..., None] + 130 * EPS) + 3 * EPS
+    ga = np.abs(rate) * (rstep[..., None] + 262 * EPS) + 3 * EPS
     u = step * x
     eu = (rstep + EPS) * np.abs(u)
     h, eh = np.zeros((T, D, S)), np.zeros((T, D, S))
