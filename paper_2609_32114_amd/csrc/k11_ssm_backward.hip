@@ -85,30 +85,30 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back
   if (quad == 0 && threadIdx.x == 0) a.resets[chunk] = reset;
 }
 
-// Sums of 16 values over the wave's 64 lanes: value n to the lanes 4 n .. 4 n + 3.  Each
-// exchange halves the values that a lane still holds: 35 instructions instead of the 96 of
-// 16 separate sums.
+// Sums of N = 8 or 16 values over the wave's 64 lanes: value n to lanes 64 / N n and up.  Each
+// exchange halves the values that a lane still holds: 35 instructions for 16 values instead of
+// the 96 of separate sums.
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
   return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
 }
-__device__ __forceinline__ float sum_lanes(const float (&in)[16]) {
-  float v[8], w[4];
+template <int N> __device__ __forceinline__ float sum_lanes(float (&v)[N]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {  // halves of 32 lanes
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(in[i]), __float_as_uint(in[i + 8]), false, false);
+  for (int i = 0; i < N / 2; ++i) {  // halves of 32 lanes
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 2]), false, false);
     v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {  // rows of 16
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 4]), false, false);
-    w[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  for (int i = 0; i < N / 4; ++i) {  // rows of 16
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 4]), false, false);
+    v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
   const bool high8 = lane_id() & 8, high4 = lane_id() & 4;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) w[i] = (high8 ? w[i + 2] : w[i]) + dpp<0x128>(high8 ? w[i] : w[i + 2]);  // lane + 8 of 16
-  float s = (high4 ? w[1] : w[0]) + dpp<0x141>(high4 ? w[0] : w[1]);                                   // lane 7 - i of 8
-  s += dpp<0xb1>(s);                                                                                   // lane ^ 1
-  return s + dpp<0x4e>(s);                                                                             // lane ^ 2
+  for (int i = 0; i < N / 8; ++i)  // lane + 8 of 16
+    v[i] = (high8 ? v[i + N / 8] : v[i]) + dpp<0x128>(high8 ? v[i] : v[i + N / 8]);
+  float s = N == 16 ? (high4 ? v[1] : v[0]) + dpp<0x141>(high4 ? v[0] : v[1]) : v[0] + dpp<0x141>(v[0]);  // lane 7 - i of 8
+  s += dpp<0xb1>(s);         // lane ^ 1
+  return s + dpp<0x4e>(s);   // lane ^ 2
 }
 
 // The forms for NP padded states: kWaves columns to a workgroup.  In LDS: the states at the
@@ -134,7 +134,9 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
   const int wave = uniform(threadIdx.x >> 6), lane = lane_id();
   float *starts = lds + (size_t)wave * F::kRuns * NP * 64 + lane;  // [runs][NP][64]
   float *sums = lds + F::kStates;                                   // [waves][8][2 NP]
-  float *maps = sums + F::kSums;                                    // [32][2 NP]
+  float *maps = sums + F::kSums;                                    // [group][2 NP]
+  constexpr int kEach = 64 / (2 * kSlice);                          // lanes that get one of sum_lanes' sums
+  float *my_sums = sums + wave * kBackRows * 2 * NP + lane / kEach % kSlice + (lane >= 32 ? NP : 0);
   const bool ok = ssm_offsets_ok(a);
   const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads, in_group = quad - group * quads;
   const int chunk = (int)(blockIdx.x / (quads * a.G));
@@ -267,39 +269,37 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
               }
             lo = hi;
           }
+          const auto back = [&](int i) {
+            rows.hold();
+            HAGDN_OPAQUE_VECTOR(step[i]);
+            const float in = step[i] * x[i], fed = col.mine ? in : 0.f;
+            float terms[2 * kSlice];  // of dB and dC
+#pragma unroll
+            for (int m = 0; m < kSlice; m += 4) {
+              const f32x4 B = rows.four(i * 2 * NP + n0 + m), C = rows.four(i * 2 * NP + NP + n0 + m);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int k = m + j, n = n0 + k;
+                const float hn = __builtin_fmaf(in, B[j], kept[i][k]), dh = __builtin_fmaf(C[j], d[i], e[n]);
+                y[i] = __builtin_fmaf(C[j], hn, y[i]);
+                w[i] = __builtin_fmaf(B[j], dh, w[i]);
+                terms[k] = dh * fed;
+                terms[kSlice + k] = d[i] * hn;
+                const float p = dh * kept[i][k];
+                ds[i] = __builtin_fmaf(A[n], p, ds[i]);
+                dA[n] = __builtin_fmaf(step[i], p, dA[n]);
+                e[n] = __builtin_amdgcn_exp2f(step[i] * A[n]) * dh;
+              }
+            }
+            my_sums[i * 2 * NP + n0] = sum_lanes(terms);  // (by all lanes that have the same one)
+          };
           for (int hi = count; hi > 0;) {
             if (base + hi == q.start) q.previous();
             if (base + hi == q.end) load_sequence<kSlice>(a.dfinal, q.seq, a, c, e + n0, n0);
             const int lo = max(0, q.start - base);
 #pragma unroll
             for (int i = kBackRows - 1; i >= 0; --i)
-              if (i >= lo && i < hi) {
-                rows.hold();
-                HAGDN_OPAQUE_VECTOR(step[i]);
-                const float in = step[i] * x[i];
-                const float fed = col.mine ? in : 0.f;
-                float terms[2 * kSlice];  // of dB and dC
-#pragma unroll
-                for (int m = 0; m < kSlice; m += 4) {
-                  const f32x4 B = rows.four(i * 2 * NP + n0 + m), C = rows.four(i * 2 * NP + NP + n0 + m);
-#pragma unroll
-                  for (int j = 0; j < 4; ++j) {
-                    const int k = m + j, n = n0 + k;
-                    const float hn = __builtin_fmaf(in, B[j], kept[i][k]), dh = __builtin_fmaf(C[j], d[i], e[n]);
-                    y[i] = __builtin_fmaf(C[j], hn, y[i]);
-                    w[i] = __builtin_fmaf(B[j], dh, w[i]);
-                    terms[k] = dh * fed;
-                    terms[kSlice + k] = d[i] * hn;
-                    const float p = dh * kept[i][k];
-                    ds[i] = __builtin_fmaf(A[n], p, ds[i]);
-                    dA[n] = __builtin_fmaf(step[i], p, dA[n]);
-                    e[n] = __builtin_amdgcn_exp2f(step[i] * A[n]) * dh;
-                  }
-                }
-                const float sum = sum_lanes(terms);
-                if ((lane & 3) == 0)
-                  sums[(wave * kBackRows + i) * 2 * NP + n0 + ((lane >> 2) & 7) + (lane >= 32 ? NP : 0)] = sum;
-              }
+              if (i >= lo && i < hi) back(i);
             if (base + lo == q.start) store_sequence<kSlice>(a.ds0, q.seq, a, col, e + n0, n0);
             hi = lo;
           }

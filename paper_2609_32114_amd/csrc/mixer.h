@@ -79,7 +79,7 @@ constexpr int kMaxStates = 64;
 // States a channel as the kernels hold them: the next of 16, 32 and 64.
 inline int ssm_padded(int S) { return S <= 16 ? 16 : S <= 32 ? 32 : 64; }
 // Tokens between two saved states of the scan (hagdn.h, ssm_prefill).
-constexpr int kSsmGroup = 32;
+constexpr int kSsmGroup = 16;
 
 struct SsmArgs {
   const void *x, *dt, *z, *B, *C, *dy;  // rows of D channels (B, C: of G x S), strides below; z may be null

@@ -128,6 +128,9 @@ template <int NP> __device__ __forceinline__ void store_states(float *rows, cons
 template <int NP>
 __device__ __forceinline__ void load_sequence(const float *s, int seq, const SsmArgs &a, uint32_t c, float *h, int first = 0) {
   load_row<NP>(s + ((size_t)seq * a.D + c) * a.S + first, s ? states(a) - first : 0, h);
+  // Waited for here, where a sequence begins: else every token's first use of a state would
+  // wait for all loads and stores under way (they may be these).
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
 }
 template <int NP>
 __device__ __forceinline__ void store_sequence(float *s, int seq, const SsmArgs &a, const Column &col, const float *h, int first = 0) {
