@@ -105,8 +105,14 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan
 
 // What enters each chunk, in place of what it leaves of nothing.  A workgroup has one state
 // of 64 channels; its 16 waves take the chunks in 16 runs, fold their own, meet in LDS and
-// go over their run again.  The last chunk in the scan's order passes nothing on.
-template <bool BACKWARD> __global__ __launch_bounds__(1024) void ssm_carry_kernel(SsmArgs a, int padded) {
+// go over their run again.  The last chunk in the scan's order passes nothing on.  Runs of up to
+// kHeld chunks stay in registers for that.
+constexpr int kHeld = 8;
+struct Passed {  // by a chunk
+  float left, sum;
+  bool reset;
+};
+template <bool BACKWARD, bool HELD> __global__ __launch_bounds__(1024) void ssm_carry_kernel(SsmArgs a, int padded) {
   __shared__ float sState[16][64], sSum[16][64];
   __shared__ int sReset[16];
   if (*a.status != 0) return;
@@ -115,43 +121,59 @@ template <bool BACKWARD> __global__ __launch_bounds__(1024) void ssm_carry_kerne
   const int n = blockIdx.y;
   const float rate = a.A[(size_t)c * a.S + n] * kLog2e;
   const int share = (a.chunks + 15) / 16, lo = wave * share, hi = min(lo + share, a.chunks);
-  const auto row = [&](int i) { return BACKWARD ? a.chunks - 1 - i : i; };
+  const auto place = [&](int i) {
+    return a.maps + ((size_t)(BACKWARD ? a.chunks - 1 - i : i) * padded + n) * a.D + c;
+  };
+  const auto passed = [&](int i) {  // the last one's own is not there
+    const int k = BACKWARD ? a.chunks - 1 - i : i;
+    return i < min(hi, a.chunks - 1) ? Passed{*place(i), a.sums[(size_t)k * a.D + c], uniform(a.resets[k]) != 0} : Passed{0.f, 0.f, false};
+  };
+  const auto fold = [&](const Passed &p, float s) {
+    return p.reset ? p.left : __builtin_fmaf(__builtin_amdgcn_exp2f(rate * p.sum), s, p.left);
+  };
+  Passed held[kHeld];
   float state = 0.f, sum = 0.f;
   int reset = 0;
+  const auto gather = [&](const Passed &p) {
+    state = fold(p, state);
+    sum += p.sum;
+    reset |= p.reset;
+  };
+  if (HELD) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = passed(lo + i);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) gather(held[i]);
+  } else {
 #pragma unroll 4
-  for (int i = lo; i < min(hi, a.chunks - 1); ++i) {
-    const int k = row(i);
-    const float left = a.maps[((size_t)k * padded + n) * a.D + c], part = a.sums[(size_t)k * a.D + c];
-    const int r = uniform(a.resets[k]);
-    state = r ? left : __builtin_fmaf(__builtin_amdgcn_exp2f(rate * part), state, left);
-    sum += part;
-    reset |= r;
+    for (int i = lo; i < hi; ++i) gather(passed(i));
   }
   sState[wave][lane] = state;
   sSum[wave][lane] = sum;
   if (lane == 0) sReset[wave] = reset;
   __syncthreads();
   float s = 0.f;
-  for (int w = 0; w < wave; ++w)
-    s = sReset[w] ? sState[w][lane] : __builtin_fmaf(__builtin_amdgcn_exp2f(rate * sSum[w][lane]), s, sState[w][lane]);
+  for (int w = 0; w < wave; ++w) s = fold(Passed{sState[w][lane], sSum[w][lane], sReset[w] != 0}, s);
+  const auto give = [&](int i, const Passed &p) {
+    if (i < hi && at < (uint32_t)a.D) *place(i) = s;
+    s = fold(p, s);
+  };
+  if (HELD) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) give(lo + i, held[i]);
+  } else {
 #pragma unroll 4
-  for (int i = lo; i < hi; ++i) {
-    const int k = row(i);
-    float *p = a.maps + ((size_t)k * padded + n) * a.D + c;
-    float next = 0.f;
-    if (i + 1 < a.chunks) {
-      const float left = *p, part = a.sums[(size_t)k * a.D + c];
-      next = uniform(a.resets[k]) ? left : __builtin_fmaf(__builtin_amdgcn_exp2f(rate * part), s, left);
-    }
-    if (at < (uint32_t)a.D) *p = s;
-    s = next;
+    for (int i = lo; i < hi; ++i) give(i, passed(i));
   }
 }
 hipError_t launch_ssm_carry(const SsmArgs &a, bool backward, hipStream_t s) {
   const dim3 grid(((unsigned)a.D + 63) / 64, (unsigned)a.S);
   const int padded = ssm_padded(a.S);
-  if (backward) hipLaunchKernelGGL((ssm_carry_kernel<true>), grid, dim3(1024), 0, s, a, padded);
-  else hipLaunchKernelGGL((ssm_carry_kernel<false>), grid, dim3(1024), 0, s, a, padded);
+  const bool held = a.chunks <= 16 * kHeld;
+  if (backward && held) hipLaunchKernelGGL((ssm_carry_kernel<true, true>), grid, dim3(1024), 0, s, a, padded);
+  else if (backward) hipLaunchKernelGGL((ssm_carry_kernel<true, false>), grid, dim3(1024), 0, s, a, padded);
+  else if (held) hipLaunchKernelGGL((ssm_carry_kernel<false, true>), grid, dim3(1024), 0, s, a, padded);
+  else hipLaunchKernelGGL((ssm_carry_kernel<false, false>), grid, dim3(1024), 0, s, a, padded);
   return hipGetLastError();
 }
 

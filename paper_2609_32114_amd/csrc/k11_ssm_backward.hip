@@ -224,9 +224,9 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
 #pragma unroll
             for (int i = 0; i < kBackRows; ++i) {
               const float z = Elt<T>::to_f32(zs[i]);
-              const Logistic g = logistic(z);
-              dgate[i] = d[i] * (g.s * __builtin_fmaf(z, g.rest, 1.f));
-              d[i] *= z * g.s;
+              const float s = logistic(z);
+              dgate[i] = d[i] * silu_slope(z, s);
+              d[i] *= z * s;
             }
           }
         }
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
         }
         if (a.raw) {
 #pragma unroll
-          for (int i = 0; i < kBackRows; ++i) dv[i] *= logistic(given[i]).s;
+          for (int i = 0; i < kBackRows; ++i) dv[i] *= logistic(given[i]);
         }
 #pragma unroll
         for (int i = 0; i < kBackRows; ++i)

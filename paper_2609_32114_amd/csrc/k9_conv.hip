@@ -96,7 +96,8 @@ __device__ __forceinline__ void pass_windows(const ConvArgs &a, bool ok, const v
   });
 }
 
-constexpr int kConvRows = 8;  // rows on their way at once
+constexpr int kConvRows = 8;      // rows on their way at once
+constexpr int kConvBackRows = 4;  // and the next four
 
 template <typename T, int W, int V>
 __global__ __launch_bounds__(256) void conv_forward_kernel(ConvArgs a, uint32_t cols, uint32_t items) {
@@ -178,16 +179,25 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, uint32_t
         store_pack<T, V>(a.dw0, ((size_t)q.seq * (W - 1) + (W - 1 + pos - q.start)) * a.D + ch.c, r);
       }
     };
-    for (int base = t0; base < stop; base += kConvRows) {
-      Pack<T, V> rows[kConvRows], grads[kConvRows];
+    Pack<T, V> rows[kConvBackRows], grads[kConvBackRows], next_rows[kConvBackRows], next_grads[kConvBackRows];
+    const auto fetch = [&](int base) {
 #pragma unroll
-      for (int i = 0; i < kConvRows; ++i) {
+      for (int i = 0; i < kConvBackRows; ++i) {
         const size_t t = min(base + i, stop - 1);
-        rows[i] = load_pack<T, V>(a.x, t * a.xs + ch.c);
-        grads[i] = load_pack<T, V>(a.dy, t * a.dys + ch.c);
+        next_rows[i] = load_pack<T, V>(a.x, t * a.xs + ch.c);
+        next_grads[i] = load_pack<T, V>(a.dy, t * a.dys + ch.c);
       }
+    };
+    fetch(t0);
+    for (int base = t0; base < stop; base += kConvBackRows) {
 #pragma unroll
-      for (int i = 0; i < kConvRows; ++i) {
+      for (int i = 0; i < kConvBackRows; ++i) {
+        rows[i] = next_rows[i];
+        grads[i] = next_grads[i];
+      }
+      fetch(base + kConvBackRows);
+#pragma unroll
+      for (int i = 0; i < kConvBackRows; ++i) {
         const int t = base + i;
         if (t >= stop || (t >= t1 && t == q.end)) {  // a sequence that starts after the run is none of its
           base = stop;
@@ -209,8 +219,7 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, uint32_t
             float p = k.b[v];
 #pragma unroll
             for (int j = 0; j < W; ++j) p = __builtin_fmaf(k.w[j][v], h[j][v], p);
-            const Logistic s = logistic(p);
-            d *= s.s * __builtin_fmaf(p, s.rest, 1.f);
+            d *= silu_slope(p, logistic(p));
           }
 #pragma unroll
           for (int j = 0; j < W; ++j) acc[j][v] = __builtin_fmaf(k.w[j][v], d, j + 1 < W ? acc[j + 1][v] : 0.f);

@@ -134,7 +134,7 @@ inline int ssm_chunk(int T, int D, int S, int G, int cus, bool backward) {
   const long slots = (cus > 0 ? cus : 256) * (backward ? (S <= 16 ? 2l : 1l) : 4l);
   const auto over = [](long a, long b) { return (a + b - 1) / b; };
   const long total = (long)T * each, rounds = over(total + 1, slots * 512);
-  const int unit = backward ? kSsmGroup : 8, least = T <= 64 ? 64 : backward ? kSsmGroup : 16;
+  const int unit = backward ? kSsmGroup : 8, least = T <= 64 ? 64 : 16;
   const long chunk = over(over(total, slots * rounds), unit) * unit;
   return (int)(chunk < least ? least : chunk);
 }

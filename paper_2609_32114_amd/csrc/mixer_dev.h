@@ -10,18 +10,15 @@ namespace hagdn {
 
 constexpr float kLog2e = 1.44269504f;
 
-// 1 / (1 + e^-v), and its complement, both from e^-|v|, so that nothing overflows and
-// neither loses digits.  The hardware's 2^x and reciprocal: an ulp each, and |v| 2^-24 of
-// the exponent's product.
-struct Logistic {
-  float s, rest;
-};
-__device__ __forceinline__ Logistic logistic(float v) {
-  const float t = __builtin_amdgcn_exp2f(-__builtin_fabsf(v) * kLog2e);
-  const float r = __builtin_amdgcn_rcpf(1.f + t), tr = t * r;
-  return {v > 0.f ? r : tr, v > 0.f ? tr : r};
+// 1 / (1 + e^-v) by the hardware's 2^x and reciprocal: an ulp each, and |v| 2^-24 of the
+// exponent's product.  Below v = -87, where it is under the least normal number, it is 0.
+__device__ __forceinline__ float logistic(float v) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v));
 }
-__device__ __forceinline__ float silu(float v) { return v * logistic(v).s; }
+__device__ __forceinline__ float silu(float v) { return v * logistic(v); }
+// The derivative of silu from its logistic s: s (1 + v (1 - s)).  What 1 - s loses where s is near
+// one is |v| 2^-24 of the result.
+__device__ __forceinline__ float silu_slope(float v, float s) { return s * __builtin_fmaf(v, 1.f - s, 1.f); }
 
 // log(1 + e^v) = max(v, 0) + log1p(t), t = e^-|v|, with log1p(t) = 2 artanh(r), r = t / (2 + t)
 // in [0, 1/3]: r times a polynomial in r^2 through the degree 5 Chebyshev nodes of
