@@ -386,7 +386,7 @@ int hagdn_conv_decode(const void *x, int64_t x_stride, const float *weight, cons
 size_t ssm_workspace_size(int T_total, int D, int S, int G, int backward);
 
 /* Forward.  checkpoints: NULL, or fp32 of ssm_checkpoints_size() elements, what
- * ssm_backward needs of the forward pass (the states before every 32nd token). */
+ * ssm_backward needs of the forward pass (the states before every 16th token). */
 size_t ssm_checkpoints_size(int T_total, int D, int S);
 int ssm_prefill(const void *x, int64_t x_stride, const void *dt, int64_t dt_stride,
                 const float *A, const void *B, int64_t B_stride, const void *C, int64_t C_stride,

@@ -55,17 +55,17 @@ def conv_workspace_size(T: int, D: int, W: int, backward: bool = False) -> int:
 
 
 def _conv(x, weight, bias):
-    """(shape, device index, row stride, dtype code, W) of a call, its weights checked."""
+    """(shape, device index, row stride, dtype code, W, bias' pointer) of a call, its weights
+    checked."""
     shape, di = _matrix("x", x, "[T, D]")
     xs = _rows("x", x, shape, di)
     dt, _ = _types("x", x, "x", x)
     if weight.dim() != 2:
         raise ValueError(f"weight must be [D, W] (got {tuple(weight.shape)})")
-    W = weight.shape[1]
-    _fp32("weight", weight, (shape[1], W), x)
-    if bias is not None:
-        _fp32("bias", bias, (shape[1],), x)
-    return shape, di, xs, dt, W
+    D, W = shape[1], weight.shape[1]
+    if weight.dtype is not _F32 or weight.get_device() != di or weight.shape[0] != D or weight.stride() != (W, 1):
+        _fp32("weight", weight, (D, W), x)
+    return shape, di, xs, dt, W, _vector("bias", bias, D, x, di)
 
 
 def conv_prefill(x, weight, bias=None, initial_window=None, cu_seqlens=None, activation="silu",
@@ -77,7 +77,7 @@ def conv_prefill(x, weight, bias=None, initial_window=None, cu_seqlens=None, act
     then left as it was allocated, and device_status(workspace) of the caller's own workspace
     says so."""
     lib = load_library()
-    shape, di, xs, dt, W = _conv(x, weight, bias)
+    shape, di, xs, dt, W, pb = _conv(x, weight, bias)
     T, D = shape
     act = _activation(activation)
     N, cu = _sequences(cu_seqlens, di)
@@ -88,7 +88,7 @@ def conv_prefill(x, weight, bias=None, initial_window=None, cu_seqlens=None, act
     y = _like("out", out, x)
     final = _output("final_out", final_out, windows, x.dtype, x) if output_final_window else None
     _check(lib.hagdn_conv_prefill(
-        x.data_ptr(), xs, weight.data_ptr(), _ptr(bias), _ptr(initial_window), cu, N, T, D, W, dt, act, y.data_ptr(),
+        x.data_ptr(), xs, weight.data_ptr(), pb, _ptr(initial_window), cu, N, T, D, W, dt, act, y.data_ptr(),
         _ptr(final), ws.data_ptr(), ws_bytes, _stream(di)))
     return y, final
 
@@ -99,7 +99,7 @@ def conv_backward(dy, x, weight, bias=None, initial_window=None, dfinal=None, cu
     (``dfinal``, None: zero): (dx, dweight, dbias or None, gradient of the initial window, or
     None without one)."""
     lib = load_library()
-    shape, di, xs, dt, W = _conv(x, weight, bias)
+    shape, di, xs, dt, W, pb = _conv(x, weight, bias)
     T, D = shape
     act = _activation(activation)
     dys = _rows("dy", dy, shape, di)
@@ -115,7 +115,7 @@ def conv_backward(dy, x, weight, bias=None, initial_window=None, dfinal=None, cu
     dx, dw = _like("dx", None, x), torch.empty_like(weight)
     db = torch.empty_like(bias) if bias is not None else None
     _check(lib.hagdn_conv_backward(
-        dy.data_ptr(), dys, x.data_ptr(), xs, weight.data_ptr(), _ptr(bias), _ptr(initial_window), _ptr(dfinal), cu, N, T,
+        dy.data_ptr(), dys, x.data_ptr(), xs, weight.data_ptr(), pb, _ptr(initial_window), _ptr(dfinal), cu, N, T,
         D, W, dt, act, dx.data_ptr(), dw.data_ptr(), _ptr(db), _ptr(dw0), ws.data_ptr(), ws_bytes, _stream(di)))
     return dx, dw, db, dw0
 
@@ -125,7 +125,7 @@ def conv_decode(x, weight, state, bias=None, slots=None, activation="silu", out=
     [S, W - 1, D] (x's type) on in place (sequence n in slot slots[n], or n; a slot outside
     the pool is padding and gives a row of zeros) and returns y [N, D]."""
     lib = load_library()
-    shape, di, xs, dt, W = _conv(x, weight, bias)
+    shape, di, xs, dt, W, pb = _conv(x, weight, bias)
     N, D = shape
     act = _activation(activation)
     S = state.shape[0] if state.dim() == 3 else 0
@@ -133,7 +133,7 @@ def conv_decode(x, weight, state, bias=None, slots=None, activation="silu", out=
     _slots(slots, S, N, x)
     y = _like("out", out, x)
     _check(lib.hagdn_conv_decode(
-        x.data_ptr(), xs, weight.data_ptr(), _ptr(bias), state.data_ptr(), _ptr(slots), S, N, D, W, dt, act, y.data_ptr(),
+        x.data_ptr(), xs, weight.data_ptr(), pb, state.data_ptr(), _ptr(slots), S, N, D, W, dt, act, y.data_ptr(),
         _stream(di)))
     return y
 
@@ -150,44 +150,57 @@ def ssm_checkpoints_size(T: int, D: int, S: int) -> int:
     return load_library().ssm_checkpoints_size(T, D, S)
 
 
-def _maps(name, t, T, S, di):
-    """(groups, token stride) of B or C: [T, G, S], or [T, S] for one group."""
-    shape = t.shape
-    if len(shape) not in (2, 3) or shape[-1] != S:
-        raise ValueError(f"{name} must be [T, G, {S}] or [T, {S}] (got {tuple(shape)})")
-    return (shape[1] if len(shape) == 3 else 1), _rows(name, t, (T, *shape[1:]), di)
+def _row(name, t, shape, di, inner=1):
+    """The row stride of a matrix whose row's last elements, `inner` apart, follow each other;
+    _rows has the other cases and the messages."""
+    s = t.stride()
+    if s[-1] == 1 and (len(s) == 2 or s[1] == inner) and t.get_device() == di and t.shape == shape:
+        return s[0]
+    return _rows(name, t, shape, di)
 
 
-class _Ssm:
-    """The operands that all the scan's calls share, checked."""
-
-    def __init__(self, x, dt, A, B, C, skip, z, dt_bias):
-        shape, di = _matrix("x", x, "[T, D]")
-        T, D = shape
-        self.shape, self.device = shape, di
-        xs, dts = _rows("x", x, shape, di), _rows("dt", dt, shape, di)
-        self.types = _types("x", x, "dt", dt)
-        if A.dim() != 2:
-            raise ValueError(f"A must be [D, S] (got {tuple(A.shape)})")
-        S = A.shape[1]
-        _fp32("A", A, (D, S), x)
-        G, Bs = _maps("B", B, T, S, di)
+def _maps(B, C, T, S, x, di):
+    """(groups, the token strides of B and C): [T, G, S], or [T, S] for one group."""
+    shape = B.shape
+    if len(shape) not in (2, 3) or shape[0] != T or shape[-1] != S:
+        raise ValueError(f"B must be [{T}, G, {S}] or [{T}, {S}] (got {tuple(shape)})")
+    Bs, Cs = _row("B", B, shape, di, S), _row("C", C, shape, di, S)
+    if B.dtype is not x.dtype or C.dtype is not x.dtype:
         _same_type("B", B, x.dtype)
-        if C.shape != B.shape:
-            raise ValueError(f"C must have B's shape {tuple(B.shape)} (got {tuple(C.shape)})")
-        _, Cs = _maps("C", C, T, S, di)
         _same_type("C", C, x.dtype)
-        self.S, self.G = S, G
-        if skip is not None:
-            _fp32("skip", skip, (D,), x)
-        if dt_bias is not None:
-            _fp32("dt_bias", dt_bias, (D,), x)
-        zs = 0
-        if z is not None:
-            zs = _rows("z", z, shape, di)
+    return (shape[1] if len(shape) == 3 else 1), Bs, Cs
+
+
+def _vector(name, t, D, x, di):
+    """The pointer of an fp32 vector beside x, or of none."""
+    if t is None:
+        return None
+    if t.dtype is not _F32 or t.get_device() != di or t.shape != (D,) or t.stride() != (1,):
+        _fp32(name, t, (D,), x)
+    return t.data_ptr()
+
+
+def _operands(x, dt, A, B, C, skip, z, dt_bias):
+    """(shape of x, states, groups, device index, type codes, arguments) of what all the scan's
+    calls share, checked."""
+    shape, di = _matrix("x", x, "[T, D]")
+    T, D = shape
+    xs, dts = _rows("x", x, shape, di), _row("dt", dt, shape, di)
+    types = _types("x", x, "dt", dt)
+    if A.dim() != 2:
+        raise ValueError(f"A must be [D, S] (got {tuple(A.shape)})")
+    S = A.shape[1]
+    if A.dtype is not _F32 or A.get_device() != di or A.shape[0] != D or A.stride() != (S, 1):
+        _fp32("A", A, (D, S), x)
+    G, Bs, Cs = _maps(B, C, T, S, x, di)
+    zs = 0
+    if z is not None:
+        zs = _row("z", z, shape, di)
+        if z.dtype is not x.dtype:
             _same_type("z", z, x.dtype)
-        self.args = (x.data_ptr(), xs, dt.data_ptr(), dts, A.data_ptr(), B.data_ptr(), Bs, C.data_ptr(), Cs, _ptr(skip),
-                     _ptr(z), zs, _ptr(dt_bias))
+    return shape, S, G, di, types, (
+        x.data_ptr(), xs, dt.data_ptr(), dts, A.data_ptr(), B.data_ptr(), Bs, C.data_ptr(), Cs,
+        _vector("skip", skip, D, x, di), None if z is None else z.data_ptr(), zs, _vector("dt_bias", dt_bias, D, x, di))
 
 
 def ssm_prefill(x, dt, A, B, C, skip=None, z=None, dt_bias=None, initial_state=None, cu_seqlens=None, preprocess=0,
@@ -199,9 +212,8 @@ def ssm_prefill(x, dt, A, B, C, skip=None, z=None, dt_bias=None, initial_state=N
     cu_seqlens are found on the device: y is then left as it was allocated, and
     device_status(workspace) of the caller's own workspace says so."""
     lib = load_library()
-    p = _Ssm(x, dt, A, B, C, skip, z, dt_bias)
-    (T, D), S, G = p.shape, p.S, p.G
-    N, cu = _sequences(cu_seqlens, p.device)
+    (T, D), S, G, di, types, args = _operands(x, dt, A, B, C, skip, z, dt_bias)
+    N, cu = _sequences(cu_seqlens, di)
     if initial_state is not None:
         _fp32("initial_state", initial_state, (N, D, S), x)
     ws, ws_bytes = _workspace(workspace, lambda: ssm_workspace_size(T, D, S, G), x)
@@ -209,8 +221,8 @@ def ssm_prefill(x, dt, A, B, C, skip=None, z=None, dt_bias=None, initial_state=N
     final = _output("final_out", final_out, (N, D, S), _F32, x) if output_final_state else None
     saved = x.new_empty(ssm_checkpoints_size(T, D, S), dtype=_F32) if output_checkpoints else None
     _check(lib.ssm_prefill(
-        *p.args, _ptr(initial_state), cu, N, T, D, S, G, *p.types, int(preprocess), y.data_ptr(), _ptr(final), _ptr(saved),
-        ws.data_ptr(), ws_bytes, _stream(p.device)))
+        *args, _ptr(initial_state), cu, N, T, D, S, G, *types, int(preprocess), y.data_ptr(), _ptr(final), _ptr(saved),
+        ws.data_ptr(), ws_bytes, _stream(di)))
     return (y, final, saved) if output_checkpoints else (y, final)
 
 
@@ -220,11 +232,11 @@ def ssm_backward(dy, x, dt, A, B, C, checkpoints, skip=None, z=None, dt_bias=Non
     None: zero): (dx, ddt, dA, dB, dC, dskip, dz, gradient of dt_bias, of the initial state),
     None for what was not given.  ``checkpoints`` is what the forward call returned."""
     lib = load_library()
-    p = _Ssm(x, dt, A, B, C, skip, z, dt_bias)
-    (T, D), S, G = p.shape, p.S, p.G
-    dys = _rows("dy", dy, p.shape, p.device)
+    shape, S, G, di, types, args = _operands(x, dt, A, B, C, skip, z, dt_bias)
+    T, D = shape
+    dys = _row("dy", dy, shape, di)
     _same_type("dy", dy, x.dtype)
-    N, cu = _sequences(cu_seqlens, p.device)
+    N, cu = _sequences(cu_seqlens, di)
     _fp32("checkpoints", checkpoints, (ssm_checkpoints_size(T, D, S),), x)
     ds0 = None
     if initial_state is not None:
@@ -239,9 +251,9 @@ def ssm_backward(dy, x, dt, A, B, C, checkpoints, skip=None, z=None, dt_bias=Non
     dz = _like("dz", None, z) if z is not None else None
     dbias = torch.empty_like(dt_bias) if dt_bias is not None else None
     _check(lib.ssm_backward(
-        dy.data_ptr(), dys, *p.args, checkpoints.data_ptr(), _ptr(initial_state), _ptr(dfinal), cu, N, T, D, S, G, *p.types,
+        dy.data_ptr(), dys, *args, checkpoints.data_ptr(), _ptr(initial_state), _ptr(dfinal), cu, N, T, D, S, G, *types,
         int(preprocess), dx.data_ptr(), ddt.data_ptr(), dA.data_ptr(), dB.data_ptr(), dC.data_ptr(), _ptr(dskip), _ptr(dz),
-        _ptr(dbias), _ptr(ds0), ws.data_ptr(), ws_bytes, _stream(p.device)))
+        _ptr(dbias), _ptr(ds0), ws.data_ptr(), ws_bytes, _stream(di)))
     return dx, ddt, dA, dB, dC, dskip, dz, dbias, ds0
 
 
@@ -250,13 +262,12 @@ def ssm_decode(x, dt, A, B, C, state, slots=None, skip=None, z=None, dt_bias=Non
     fp32 state pool [slots, D, S] in place (sequence n in slot slots[n], or n; a slot outside
     the pool is padding and gives a row of zeros) and returns y [N, D]."""
     lib = load_library()
-    p = _Ssm(x, dt, A, B, C, skip, z, dt_bias)
-    (N, D), S, G = p.shape, p.S, p.G
+    (N, D), S, G, di, types, args = _operands(x, dt, A, B, C, skip, z, dt_bias)
     pool = state.shape[0] if state.dim() == 3 else 0
     _fp32("state", state, (pool, D, S), x)
     _slots(slots, pool, N, x)
     y = _like("out", out, x)
     _check(lib.ssm_decode(
-        *p.args, state.data_ptr(), _ptr(slots), pool, N, D, S, G, *p.types, int(preprocess), y.data_ptr(),
-        _stream(p.device)))
+        *args, state.data_ptr(), _ptr(slots), pool, N, D, S, G, *types, int(preprocess), y.data_ptr(),
+        _stream(di)))
     return y

@@ -112,8 +112,8 @@ def test_workspace_sizes():
     assert P.ssm_workspace_size(0, 1, 1) > 0 and P.conv_workspace_size(0, 1, 2) > 0
     assert P.ssm_workspace_size(100000, 2048, 16) > P.ssm_workspace_size(1000, 2048, 16)
     assert P.ssm_workspace_size(1000, 2048, 16, backward=True) > P.ssm_workspace_size(1000, 2048, 16)
-    assert P.ssm_checkpoints_size(33, 10, 16) == 2 * 16 * 10 and P.ssm_checkpoints_size(0, 10, 16) == 0
-    assert P.ssm_checkpoints_size(33, 10, 17) == 2 * 32 * 10 and P.ssm_checkpoints_size(33, 10, 64) == 2 * 64 * 10
+    assert P.ssm_checkpoints_size(33, 10, 16) == 3 * 16 * 10 and P.ssm_checkpoints_size(0, 10, 16) == 0
+    assert P.ssm_checkpoints_size(33, 10, 17) == 3 * 32 * 10 and P.ssm_checkpoints_size(33, 10, 64) == 3 * 64 * 10
     assert lib.ssm_workspace_size(-1, 64, 16, 1, 0) == 0 and lib.ssm_workspace_size(5, 64, 16, 3, 0) == 0
     assert lib.hagdn_conv_workspace_size(5, 64, 1, 0) == 0 and lib.hagdn_pool_workspace_size(0) == 0
     for bad in (lambda: P.ssm_workspace_size(5, 0, 16), lambda: P.conv_workspace_size(5, 64, 9),
