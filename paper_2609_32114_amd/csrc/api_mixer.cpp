@@ -238,28 +238,21 @@ int check_ranges(void *const *pools, const void *const *sources, const size_t *r
   return ranges_disjoint(r, n) ? HAGDN_OK : fail(HAGDN_EINVAL, "pools overlap each other or a source");
 }
 
-// The copies of all pools, in launches of up to kPoolsPerLaunch pools of one alignment.
+// The copies of all pools, in launches of up to kPoolsPerLaunch pools.
 int launch_copies(hagdn::PoolCopyArgs a, void *const *pools, const void *const *sources, const size_t *row_bytes,
                   int num_pools, bool in_place, hipStream_t s) {
   const int cus = query_cus();
-  for (int unit = 16; unit >= 1; unit /= 2) {
-    a.unit = unit;
-    a.count = 0;
-    const auto flush = [&]() {
-      const hipError_t e = a.count > 0 ? hagdn::launch_pool_copy(a, in_place, cus, s) : hipSuccess;
-      a.count = 0;
-      return e;
-    };
-    for (int p = 0; p < num_pools; ++p) {
-      const void *from = sources ? sources[p] : pools[p];
-      const uintptr_t bits = (uintptr_t)pools[p] | (uintptr_t)from | (uintptr_t)row_bytes[p];
-      const int aligned = bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : bits % 2 == 0 ? 2 : 1;
-      if (aligned != unit) continue;
-      a.pools[a.count++] = {pools[p], from, row_bytes[p]};
-      if (a.count == hagdn::kPoolsPerLaunch)
-        if (hipError_t e = flush()) return done(e);
+  for (int base = 0; base < num_pools; base += hagdn::kPoolsPerLaunch) {
+    a.count = num_pools - base < hagdn::kPoolsPerLaunch ? num_pools - base : hagdn::kPoolsPerLaunch;
+    for (int p = 0; p < a.count; ++p) {
+      void *to = pools[base + p];
+      const void *from = sources ? sources[base + p] : to;
+      const size_t row = row_bytes[base + p];
+      const uintptr_t bits = (uintptr_t)to | (uintptr_t)from | (uintptr_t)row;
+      const int unit = bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : bits % 2 == 0 ? 2 : 1;
+      a.pools[p] = {to, from, row / unit, unit};
     }
-    if (hipError_t e = flush()) return done(e);
+    if (hipError_t e = hagdn::launch_pool_copy(a, in_place, cus, s)) return done(e);
   }
   return HAGDN_OK;
 }

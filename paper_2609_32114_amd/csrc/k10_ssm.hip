@@ -12,7 +12,9 @@ template <typename T, typename S, int NP, bool OUT>
 __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan_kernel(SsmArgs a, uint32_t quads) {
   using Stage = Maps<T, NP, OUT ? 3 : 1, kSsmRows, 256>;
   __shared__ __align__(16) float sMaps[2][Stage::kAll];
-  const bool ok = ssm_offsets_ok(a);
+  __shared__ int32_t sCu[kCheckInPlace + 1];
+  Offsets32 cu;
+  const bool ok = stage_offsets(a.cu, a.N, a.T, a.status, sCu, cu);
   const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads;
   const int chunk = (int)(blockIdx.x / (quads * a.G));
   const Column col(group, (quad - group * quads) * 4 + uniform(threadIdx.x >> 6), a);
@@ -34,7 +36,7 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan
   if (OUT && chunk > 0) load_states(a.maps + (size_t)chunk * NP * a.D, a, c, h);
   else for (int n = 0; n < NP; ++n) h[n] = 0.f;
   const float bias = a.raw && a.bias ? a.bias[c] : 0.f, skip = OUT && a.skip ? a.skip[c] : 0.f;
-  Cursor q(a.cu, a.N, a.T, t0);
+  Cursor q(cu, t0);
   int first = q.start == t0 ? t0 : q.end;  // the next token that starts a sequence
   bool reset = false;
   float sum = 0.f;

@@ -16,7 +16,9 @@ template <typename T, typename S, int NP>
 __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back_local_kernel(SsmArgs a, uint32_t quads) {
   using Stage = Maps<T, NP, 2, kBackRows, 256>;
   __shared__ __align__(16) float sMaps[2][Stage::kAll];
-  const bool ok = ssm_offsets_ok(a);
+  __shared__ int32_t sCu[kCheckInPlace + 1];
+  Offsets32 cu;
+  const bool ok = stage_offsets(a.cu, a.N, a.T, a.status, sCu, cu);
   const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads;
   const int chunk = 1 + (int)(blockIdx.x / (quads * a.G));  // the first chunk passes nothing on
   const Column col(group, (quad - group * quads) * 4 + uniform(threadIdx.x >> 6), a);
@@ -28,7 +30,7 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back
 #pragma unroll
   for (int n = 0; n < NP; ++n) e[n] = 0.f;
   const float bias = a.raw && a.bias ? a.bias[c] : 0.f;
-  Cursor q(a.cu, a.N, a.T, t1 - 1);
+  Cursor q(cu, t1 - 1);
   bool reset = false;
   float sum = 0.f;
   int base = t0 + (t1 - 1 - t0) / kBackRows * kBackRows, turn = 0;
@@ -137,7 +139,9 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
   float *maps = sums + F::kSums;                                    // [group][2 NP]
   constexpr int kEach = 64 / (2 * kSlice);                          // lanes that get one of sum_lanes' sums
   float *my_sums = sums + wave * kBackRows * 2 * NP + lane / kEach % kSlice + (lane >= 32 ? NP : 0);
-  const bool ok = ssm_offsets_ok(a);
+  __shared__ int32_t sCu[kCheckInPlace + 1];
+  Offsets32 cu;
+  const bool ok = stage_offsets(a.cu, a.N, a.T, a.status, sCu, cu);
   const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads, in_group = quad - group * quads;
   const int chunk = (int)(blockIdx.x / (quads * a.G));
   const Column col(group, in_group * F::kWaves + wave, a);
@@ -163,7 +167,7 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
       load_states(a.ckpt + (size_t)(g0 / kSsmGroup) * NP * a.D, a, c, h);
       stage.put(maps);  // the last group's have been read: its runs end at a barrier
       __syncthreads();
-      Cursor q(a.cu, a.N, a.T, g0);
+      Cursor q(cu, g0);
       int first = q.start == g0 ? g0 : q.end;
       for (int run = 0; run < runs && !col.idle; ++run) {
 #pragma unroll
@@ -236,7 +240,7 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
           y[i] = skip * x[i];
           w[i] = ds[i] = 0.f;
         }
-        const Cursor at(a.cu, a.N, a.T, base);
+        const Cursor at(cu, base);
 #pragma unroll
         for (int n0 = 0; n0 < NP; n0 += kSlice) {
           float kept[kBackRows][kSlice], h[kSlice];  // kept: a_t h_{t-1}

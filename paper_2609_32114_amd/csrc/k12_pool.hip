@@ -7,12 +7,16 @@
 
 namespace hagdn {
 
-template <int UNIT> struct Unit;
-template <> struct Unit<16> { using type = u32x4; };
-template <> struct Unit<8> { using type = uint64_t; };
-template <> struct Unit<4> { using type = uint32_t; };
-template <> struct Unit<2> { using type = uint16_t; };
-template <> struct Unit<1> { using type = uint8_t; };
+// Calls f with a value of a pool's access type.
+template <typename F> __device__ __forceinline__ void with_unit(int unit, F f) {
+  switch (unit) {
+    case 16: f(u32x4{}); break;
+    case 8: f(uint64_t{}); break;
+    case 4: f(uint32_t{}); break;
+    case 2: f(uint16_t{}); break;
+    default: f(uint8_t{}); break;
+  }
+}
 
 constexpr int kPieces = 8;  // units a thread moves at once, at most
 
@@ -22,74 +26,78 @@ __device__ __forceinline__ int row_of(const int32_t *table, int rows, int i) {
   return r >= 0 && r < rows ? r : -1;
 }
 
+// The pool that piece `at` of an entry lies in, and the piece's place there; `each` units to a piece.
+__device__ __forceinline__ int find_pool(const PoolCopyArgs &a, uint32_t each, uint64_t &at) {
+  for (int p = 0;; ++p) {
+    const uint64_t here = (a.pools[p].units + each - 1) / each;
+    if (at < here || p + 1 == a.count) return p;
+    at -= here;
+  }
+}
+
 // Rows that no other entry of the call writes or reads: a workgroup moves `span` units of one
 // row after another.  A source outside its rows gives zeros.
-template <int UNIT> __global__ __launch_bounds__(256) void pool_move_kernel(PoolCopyArgs a, uint32_t span) {
-  using U = typename Unit<UNIT>::type;
-  uint64_t pieces = 0;  // of one entry, over all pools
-  for (int p = 0; p < a.count; ++p) pieces += (a.pools[p].row / UNIT + span - 1) / span;
+__global__ __launch_bounds__(256) void pool_move_kernel(PoolCopyArgs a, uint32_t span, uint64_t pieces) {
   const int n = a.moves ? a.moves[0] : a.n;
   for (uint64_t item = blockIdx.x; item < pieces * n; item += gridDim.x) {
     const int i = (int)(item / pieces);
     uint64_t at = item - (uint64_t)i * pieces;
-    int p = 0;
-    for (;; ++p) {
-      const uint64_t here = (a.pools[p].row / UNIT + span - 1) / span;
-      if (at < here) break;
-      at -= here;
-    }
+    const Pool &pool = a.pools[find_pool(a, span, at)];
     const int dst = a.moves ? a.moves[1 + 2 * i] : row_of(a.dst, a.dst_rows, i);
     const int src = a.moves ? a.moves[2 + 2 * i] : row_of(a.src, a.src_rows, i);
     if (dst < 0) continue;
-    const uint64_t units = a.pools[p].row / UNIT, first = at * span + threadIdx.x, end = min(units, (at + 1) * span);
-    const U *from = static_cast<const U *>(a.pools[p].from) + (src < 0 ? 0 : (uint64_t)src * units);
-    U *to = static_cast<U *>(a.pools[p].to) + (uint64_t)dst * units;
-    U v[kPieces] = {};
-    if (src >= 0) {
+    const uint64_t units = pool.units, first = at * span + threadIdx.x, end = min(units, (at + 1) * span);
+    with_unit(pool.unit, [&](auto u) {
+      using U = decltype(u);
+      const U *from = static_cast<const U *>(pool.from) + (src < 0 ? 0 : (uint64_t)src * units);
+      U *to = static_cast<U *>(pool.to) + (uint64_t)dst * units;
+      U v[kPieces] = {};
+      if (src >= 0) {
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k)
+          if (first + k * 256 < end) v[k] = __builtin_nontemporal_load(from + first + k * 256);
+      }
 #pragma unroll
       for (int k = 0; k < kPieces; ++k)
-        if (first + k * 256 < end) v[k] = __builtin_nontemporal_load(from + first + k * 256);
-    }
-#pragma unroll
-    for (int k = 0; k < kPieces; ++k)
-      if (first + k * 256 < end) __builtin_nontemporal_store(v[k], to + first + k * 256);
+        if (first + k * 256 < end) __builtin_nontemporal_store(v[k], to + first + k * 256);
+    });
   }
 }
 
 // Rows of the same pools, as if all were read before any is written: a workgroup has a span
-// of bytes of every entry's row, all of them in registers between its loads and its stores.
-template <int UNIT, int THREADS> __global__ __launch_bounds__(THREADS) void pool_shuffle_kernel(PoolCopyArgs a, uint32_t width) {
-  using U = typename Unit<UNIT>::type;
-  uint64_t spans = 0;
-  for (int p = 0; p < a.count; ++p) spans += (a.pools[p].row / UNIT + width - 1) / width;
+// of units of every entry's row, all of them in registers between its loads and its stores.
+template <int THREADS> __global__ __launch_bounds__(THREADS) void pool_shuffle_kernel(PoolCopyArgs a, uint32_t width, uint64_t spans) {
   for (uint64_t item = blockIdx.x; item < spans; item += gridDim.x) {
     uint64_t at = item;
-    int p = 0;
-    for (;; ++p) {
-      const uint64_t here = (a.pools[p].row / UNIT + width - 1) / width;
-      if (at < here) break;
-      at -= here;
-    }
-    const uint64_t units = a.pools[p].row / UNIT;
-    U *pool = static_cast<U *>(a.pools[p].to);
-    U v[kPieces] = {};
-    int dst[kPieces];
-    uint64_t col[kPieces];
+    const Pool &pool = a.pools[find_pool(a, width, at)];
+    const uint64_t units = pool.units, first = at * width;
+    with_unit(pool.unit, [&](auto u) {
+      using U = decltype(u);
+      U *rows = static_cast<U *>(pool.to), v[kPieces] = {};
+      // unit k of this thread: its entry, and where in the row it lies
+      const auto entry = [&](int k, uint64_t &col) {
+        const uint32_t e = k * THREADS + threadIdx.x, i = e / width;  // n x width <= THREADS x kPieces
+        col = first + (e - i * width);
+        return i < (uint32_t)a.n && col < units ? (int)i : -1;
+      };
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k) {
-      const uint32_t e = k * THREADS + threadIdx.x, i = e / width;  // n x width <= THREADS x kPieces
-      col[k] = at * width + (e - i * width);
-      dst[k] = -1;
-      if (i >= (uint32_t)a.n || col[k] >= units) continue;
-      dst[k] = row_of(a.dst, a.dst_rows, (int)i);
-      const int src = row_of(a.src, a.src_rows, (int)i);
-      if (dst[k] >= 0 && src >= 0) v[k] = pool[(uint64_t)src * units + col[k]];
-    }
-    __syncthreads();
+      for (int k = 0; k < kPieces; ++k) {
+        uint64_t col;
+        const int i = entry(k, col);
+        if (i < 0 || row_of(a.dst, a.dst_rows, i) < 0) continue;
+        const int src = row_of(a.src, a.src_rows, i);
+        if (src >= 0) v[k] = rows[(uint64_t)src * units + col];
+      }
+      __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k)
-      if (dst[k] >= 0) pool[(uint64_t)dst[k] * units + col[k]] = v[k];
-    __syncthreads();
+      for (int k = 0; k < kPieces; ++k) {
+        uint64_t col;
+        const int i = entry(k, col);
+        const int dst = i < 0 ? -1 : row_of(a.dst, a.dst_rows, i);
+        if (dst >= 0) rows[(uint64_t)dst * units + col] = v[k];
+      }
+      __syncthreads();
+    });
   }
 }
 
@@ -314,20 +322,20 @@ hipError_t launch_pool_compact_plan(const PoolPlanArgs &a, hipStream_t s) {
 // Long rows go 32 KiB (of 16-byte units) at a time; calls that move little in as many pieces as
 // give every CU four workgroups, of one unit a thread at least.  (One row of 144 KiB in pieces
 // of 32 KiB 6.6 us, 4.2 in pieces of 4 KiB.)
-template <int UNIT> hipError_t pool_copy(const PoolCopyArgs &a, bool in_place, int cus, hipStream_t s) {
+hipError_t launch_pool_copy(const PoolCopyArgs &a, bool in_place, int cus, hipStream_t s) {
   const uint64_t most = 16ull * (cus > 0 ? cus : 256);  // workgroups
   uint64_t units = 0;                                   // of one entry
-  for (int p = 0; p < a.count; ++p) units += a.pools[p].row / UNIT;
+  for (int p = 0; p < a.count; ++p) units += a.pools[p].units;
   const auto pieces = [&](uint64_t span) {
     uint64_t n = 0;
-    for (int p = 0; p < a.count; ++p) n += (a.pools[p].row / UNIT + span - 1) / span;
+    for (int p = 0; p < a.count; ++p) n += (a.pools[p].units + span - 1) / span;
     return n;
   };
   const uint64_t share = (units * (in_place ? 1 : (uint64_t)a.n) + most / 4 - 1) / (most / 4);
   if (!in_place) {
     const uint32_t span = (uint32_t)(share < 256 ? 256 : share > 256 * kPieces ? 256 * kPieces : (share + 255) / 256 * 256);
-    const uint64_t items = pieces(span) * (uint64_t)a.n;
-    hipLaunchKernelGGL((pool_move_kernel<UNIT>), dim3((unsigned)(items < most ? items : most)), dim3(256), 0, s, a, span);
+    const uint64_t each = pieces(span), items = each * (uint64_t)a.n;
+    hipLaunchKernelGGL(pool_move_kernel, dim3((unsigned)(items < most ? items : most)), dim3(256), 0, s, a, span, each);
     return hipGetLastError();
   }
   const bool many = a.n > 256 * kPieces;
@@ -336,19 +344,9 @@ template <int UNIT> hipError_t pool_copy(const PoolCopyArgs &a, bool in_place, i
   const uint32_t width = (uint32_t)(share < least ? (least < widest ? least : widest) : share < widest ? share : widest);
   const uint64_t spans = pieces(width);
   const dim3 grid((unsigned)(spans < most ? spans : most));
-  if (many) hipLaunchKernelGGL((pool_shuffle_kernel<UNIT, 1024>), grid, dim3(1024), 0, s, a, width);
-  else hipLaunchKernelGGL((pool_shuffle_kernel<UNIT, 256>), grid, dim3(256), 0, s, a, width);
+  if (many) hipLaunchKernelGGL((pool_shuffle_kernel<1024>), grid, dim3(1024), 0, s, a, width, spans);
+  else hipLaunchKernelGGL((pool_shuffle_kernel<256>), grid, dim3(256), 0, s, a, width, spans);
   return hipGetLastError();
-}
-
-hipError_t launch_pool_copy(const PoolCopyArgs &a, bool in_place, int cus, hipStream_t s) {
-  switch (a.unit) {
-    case 16: return pool_copy<16>(a, in_place, cus, s);
-    case 8: return pool_copy<8>(a, in_place, cus, s);
-    case 4: return pool_copy<4>(a, in_place, cus, s);
-    case 2: return pool_copy<2>(a, in_place, cus, s);
-    default: return pool_copy<1>(a, in_place, cus, s);
-  }
 }
 
 }  // namespace hagdn

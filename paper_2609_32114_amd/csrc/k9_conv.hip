@@ -7,21 +7,15 @@
 namespace hagdn {
 
 __global__ __launch_bounds__(256) void check_kernel(const int32_t *cu, int N, int T, int *status) {
-  const bool ok = offsets_ok(cu, N, T);
-  if (threadIdx.x == 0) *status = ok ? 0 : kDevBadSeqlens;
+  int bad = 0;
+  for (int i = threadIdx.x; i < N; i += 256) bad |= cu[i] > cu[i + 1];
+  if (threadIdx.x == 0) bad |= cu[0] != 0 || cu[N] != T;
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x == 0) *status = bad ? kDevBadSeqlens : 0;
 }
 hipError_t launch_check_offsets(const int32_t *cu, int N, int T, int *status, hipStream_t s) {
   hipLaunchKernelGGL(check_kernel, dim3(1), dim3(256), 0, s, cu, N, T, status);
   return hipGetLastError();
-}
-
-// Whether the offsets are right: asked here, or told by the kernel before.  The whole
-// workgroup calls; its first one tells the host.
-__device__ __forceinline__ bool conv_offsets_ok(const ConvArgs &a) {
-  if (a.N > kCheckInPlace) return *a.status == 0;
-  const bool ok = offsets_ok(a.cu, a.N, a.T);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
-  return ok;
 }
 
 // The channels of a lane: V from c on.  Lanes past the last channel, and the last one where
@@ -101,7 +95,9 @@ constexpr int kConvBackRows = 4;  // and the next four
 
 template <typename T, int W, int V>
 __global__ __launch_bounds__(256) void conv_forward_kernel(ConvArgs a, uint32_t cols, uint32_t items) {
-  const bool ok = conv_offsets_ok(a);
+  __shared__ int32_t sCu[kCheckInPlace + 1];
+  Offsets32 cu;
+  const bool ok = stage_offsets(a.cu, a.N, a.T, a.status, sCu, cu);
   const uint32_t item = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (item >= items) return;
   const uint32_t run = item / cols;
@@ -110,7 +106,7 @@ __global__ __launch_bounds__(256) void conv_forward_kernel(ConvArgs a, uint32_t 
   const int t0 = (int)min((long)run * a.run, (long)a.T), t1 = (int)min((long)t0 + a.run, (long)a.T);
   if (!ok || t0 >= t1) return;
   const Taps<T, W, V> k(a.w, a.b, ch.c);
-  Cursor q(a.cu, a.N, a.T, t0);
+  Cursor q(cu, t0);
   float h[W][V];
   load_history<T, W, V>(a, q.seq, q.start, t0, ch.c, h);
   for (int base = t0; base < t1; base += kConvRows) {
@@ -154,7 +150,9 @@ __global__ __launch_bounds__(256) void conv_forward_kernel(ConvArgs a, uint32_t 
 // its window, written by the wave of the sequence's first token.
 template <typename T, int W, int V>
 __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, uint32_t cols, uint32_t items) {
-  const bool ok = conv_offsets_ok(a);
+  __shared__ int32_t sCu[kCheckInPlace + 1];
+  Offsets32 cu;
+  const bool ok = stage_offsets(a.cu, a.N, a.T, a.status, sCu, cu);
   const uint32_t item = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (item >= items) return;
   const uint32_t run = item / cols;
@@ -165,7 +163,7 @@ __global__ __launch_bounds__(256) void conv_backward_kernel(ConvArgs a, uint32_t
   if (ok && t0 < t1) {
     const int stop = (int)min((long)t1 + W - 1, (long)a.T);
     const Taps<T, W, V> k(a.w, a.b, ch.c);
-    Cursor q(a.cu, a.N, a.T, t0);
+    Cursor q(cu, t0);
     float h[W][V], acc[W][V] = {};
     load_history<T, W, V>(a, q.seq, q.start, t0, ch.c, h);
     const auto emit = [&](int pos, const float (&g)[V]) {

@@ -128,13 +128,13 @@ inline long ssm_quads(int D, int G, int S) { return (ssm_columns(D, G) + ssm_wav
 // chunk would pass 512 tokens as few rounds as keep it below.  (17401 x 2048 tokens in 68 chunks
 // of 256, 2.1 workgroups a CU: outputs 230 us, backward 1022; in chunks of 136 and 288, 160 and
 // 730.)
-// Calls of up to 64 tokens are one chunk, which needs one launch instead of three.
+// Calls of up to 64 tokens of 16 states are one chunk, which needs one launch instead of three.
 inline int ssm_chunk(int T, int D, int S, int G, int cus, bool backward) {
   const long each = backward ? ssm_quads(D, G, S) * G : (ssm_columns(D, G) + 3) / 4 * G;
   const long slots = (cus > 0 ? cus : 256) * (backward ? (S <= 16 ? 2l : 1l) : 4l);
   const auto over = [](long a, long b) { return (a + b - 1) / b; };
   const long total = (long)T * each, rounds = over(total + 1, slots * 512);
-  const int unit = backward ? kSsmGroup : 8, least = T <= 64 ? 64 : 16;
+  const int unit = backward ? kSsmGroup : 8, least = (long)T * ssm_padded(S) <= 1024 ? 64 : 16;
   const long chunk = over(over(total, slots * rounds), unit) * unit;
   return (int)(chunk < least ? least : chunk);
 }
@@ -155,12 +155,12 @@ constexpr int kMaxMovesInPlace = 8192;    // rows of a copy within pools
 struct Pool {
   void *to;
   const void *from;
-  uint64_t row;  // bytes
+  uint64_t units;  // of a row
+  int unit;        // bytes of an access: 16, 8, 4, 2 or 1, what rows and pointers are aligned to
 };
 struct PoolCopyArgs {
   Pool pools[kPoolsPerLaunch];
   int count;                // of pools
-  int unit;                 // bytes of an access: 16, 8, 4, 2 or 1, what all rows are aligned to
   const int32_t *dst, *src;  // rows, or null: entry i is row i
   int n, dst_rows, src_rows;
   const int *moves;         // null, or {number of moves, dst, src, dst, src, ..}: instead of the tables

@@ -3,6 +3,7 @@
 #pragma once
 
 #include "device.h"
+#include "glr.h"  // row access
 #include "mixer.h"
 #include "prefill.h"
 
@@ -49,46 +50,67 @@ template <typename T, int V> __device__ __forceinline__ void store_pack(void *ba
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// Whether cu[0 .. N] are the offsets of N sequences over T tokens; every thread of the
-// workgroup takes part and gets the answer.
-__device__ __forceinline__ bool offsets_ok(const int32_t *cu, int N, int T) {
-  if (!cu) return true;
-  int bad = 0;
-  for (int i = threadIdx.x; i < N; i += blockDim.x) bad |= cu[i] > cu[i + 1];
-  if (threadIdx.x == 0) bad |= cu[0] != 0 || cu[N] != T;
-  return !__syncthreads_or(bad);
+// The sequence offsets, in LDS where up to kCheckInPlace sequences' fit: a sequence's end costs
+// a wave some 100 ns from there and a microsecond from memory.
+struct Offsets32 {
+  const int32_t *cu;  // null: one sequence of all tokens
+  int N, T;
+  const HAGDN_LDS int32_t *lds;
+  __device__ int operator[](int i) const { return uniform(lane_value(i)); }
+  __device__ int lane_value(int i) const {
+    if (N <= kCheckInPlace) return lds[i];
+    return cu[i];
+  }
+};
+// Fills the LDS copy and says whether cu[0 .. N] are the offsets of N sequences over T tokens:
+// asked here, where the call's first workgroup tells the host, or by the kernel before.  The
+// whole workgroup calls.
+__device__ __forceinline__ bool stage_offsets(const int32_t *cu, int N, int T, int *status, int32_t (&lds)[kCheckInPlace + 1],
+                                              Offsets32 &o) {
+  o = {cu, N, T, (const HAGDN_LDS int32_t *)lds};
+  if (cu && N > kCheckInPlace) return uniform(*status) == 0;
+  bool ok = true;
+  if (cu) {
+    for (int i = threadIdx.x; i <= N; i += blockDim.x) lds[i] = cu[i];
+    __syncthreads();
+    int bad = 0;
+    for (int i = threadIdx.x; i < N; i += blockDim.x) bad |= lds[i] > lds[i + 1];
+    if (threadIdx.x == 0) bad |= lds[0] != 0 || lds[N] != T;
+    ok = !__syncthreads_or(bad);
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = ok ? 0 : kDevBadSeqlens;
+  return ok;
 }
 
 // The sequence that a token belongs to, followed from one token to the next by a whole
 // wave.  The offsets must have been checked.
 struct Cursor {
-  const int32_t *cu;  // null: one sequence of all tokens
-  int N, T;
+  Offsets32 cu;
   int seq, start, end;  // uniform over the wave
   // The sequence of token t < T.  Each round of the search the lanes divide the range by 64.
-  __device__ Cursor(const int32_t *cu_, int N_, int T_, int t) : cu(cu_), N(N_), T(T_), seq(0), start(0), end(T_) {
-    if (!cu) return;
-    int lo = 0, len = N;  // the last sequence that starts at or before t is in [lo, lo + len)
+  __device__ Cursor(const Offsets32 &o, int t) : cu(o), seq(0), start(0), end(o.T) {
+    if (!cu.cu) return;
+    int lo = 0, len = cu.N;  // the last sequence that starts at or before t is in [lo, lo + len)
     const int lane = lane_id();
     while (len > 1) {
       const int step = (len + 63) / 64;
       const long at = (long)lane * step;
-      const bool below = at < len && cu[lo + at] <= t;
+      const bool below = at < len && cu.lane_value(lo + (int)at) <= t;
       const int count = __popcll(__ballot(below));
       const int skip = count > 1 ? (count - 1) * step : 0;
       lo += skip;
       len = min(step, len - skip);
     }
     seq = uniform(lo);
-    start = uniform(cu[seq]);
-    end = uniform(cu[seq + 1]);
+    start = cu[seq];
+    end = cu[seq + 1];
   }
   // To the sequence of the token after this one's last (which must exist).
   __device__ void next() {
     start = end;
     do {
       ++seq;
-      end = uniform(cu[seq + 1]);
+      end = cu[seq + 1];
     } while (end == start);
   }
   // To the sequence of the token before this one's first (which must exist).
@@ -96,7 +118,7 @@ struct Cursor {
     end = start;
     do {
       --seq;
-      start = uniform(cu[seq]);
+      start = cu[seq];
     } while (end == start);
   }
 };

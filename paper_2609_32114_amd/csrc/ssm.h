@@ -17,7 +17,6 @@
 // independent of what enters, whatever that is.
 #pragma once
 
-#include "glr.h"  // row access
 #include "mixer_dev.h"
 
 namespace hagdn {
@@ -185,15 +184,6 @@ __device__ __forceinline__ void step_sizes(const SsmArgs &a, const S (&given)[N]
   if (!a.raw) return;
 #pragma unroll
   for (int i = 0; i < N; ++i) step[i] = softplus(v[i]);
-}
-
-// Whether the offsets are right: asked here, or told by the kernel before.  The whole
-// workgroup calls; the call's first one tells the host.
-__device__ __forceinline__ bool ssm_offsets_ok(const SsmArgs &a) {
-  if (a.N > kCheckInPlace) return *a.status == 0;
-  const bool ok = offsets_ok(a.cu, a.N, a.T);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = ok ? 0 : kDevBadSeqlens;
-  return ok;
 }
 
 // The instance of a launcher for a call's types and padded states:
