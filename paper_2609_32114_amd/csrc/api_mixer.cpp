@@ -149,7 +149,7 @@ SsmPlan ssm_plan(int T, int D, int S, int G, bool backward) {
   p.sums = take(between * D * 4);
   p.resets = take(between * 4);
   if (backward) {
-    p.dbc = take((size_t)hagdn::ssm_quads(D, G, S) * T * G * 2 * np * 4);
+    p.dbc = take((size_t)hagdn::ssm_teams(D, G) * T * G * 2 * np * 4);
     p.dweights = take((size_t)p.chunks * (np + 2) * D * 4);
   }
   p.bytes = at;

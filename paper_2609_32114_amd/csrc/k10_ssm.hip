@@ -6,18 +6,18 @@ namespace hagdn {
 
 constexpr int kSsmRows = 8;  // tokens whose rows are on their way at once; divides every chunk and group
 
-// A chunk's tokens: what it leaves of a zero state (OUT false), or its outputs.  The four
-// waves of a workgroup have four columns of a group and the same chunk.
-template <typename T, typename S, int NP, bool OUT>
-__global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan_kernel(SsmArgs a, uint32_t quads) {
-  using Stage = Maps<T, NP, OUT ? 3 : 1, kSsmRows, 256>;
+// A chunk's tokens: what it leaves of a zero state (OUT false), or its outputs.  The W waves
+// of a workgroup have columns of one group and the same chunk.
+template <typename T, typename S, int NP, int W, bool OUT>
+__global__ __launch_bounds__(W * 64, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan_kernel(SsmArgs a, uint32_t teams) {
+  using Stage = Maps<T, NP, OUT ? 3 : 1, kSsmRows, W * 64>;
   __shared__ __align__(16) float sMaps[2][Stage::kAll];
   __shared__ int32_t sCu[kCheckInPlace + 1];
   Offsets32 cu;
   const bool ok = stage_offsets(a.cu, a.N, a.T, a.status, sCu, cu);
-  const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads;
-  const int chunk = (int)(blockIdx.x / (quads * a.G));
-  const Column col(group, (quad - group * quads) * 4 + uniform(threadIdx.x >> 6), a);
+  const uint32_t team = blockIdx.x % (teams * a.G), group = team / teams;
+  const int chunk = (int)(blockIdx.x / (teams * a.G));
+  const Column col(group, (team - group * teams) * W + uniform(threadIdx.x >> 6), a);
   const uint32_t c = col.c;
   if (OUT && chunk == 0) pass_states(a, ok, a.s0, a.s_final, col);
   const int t0 = chunk * a.chunk, t1 = (int)min((long)t0 + a.chunk, (long)a.T);
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_scan
   if (OUT) return;
   store_states(a.maps + (size_t)chunk * NP * a.D, a, col, h);
   if (col.mine) a.sums[(size_t)chunk * a.D + c] = sum;
-  if (quad == 0 && threadIdx.x == 0) a.resets[chunk] = reset;
+  if (team == 0 && threadIdx.x == 0) a.resets[chunk] = reset;
 }
 
 // What enters each chunk, in place of what it leaves of nothing.  A workgroup has one state
@@ -180,22 +180,22 @@ hipError_t launch_ssm_carry(const SsmArgs &a, bool backward, hipStream_t s) {
 }
 
 hipError_t launch_ssm_forward(const SsmArgs &a, bool bf16, bool dt_bf16, hipStream_t s) {
-  return ssm_dispatch(a.S, bf16, dt_bf16, [&](auto t, auto st, auto np) {
+  return ssm_dispatch(a, bf16, dt_bf16, [&](auto t, auto st, auto np, auto w) {
     using T = decltype(t);
     using S = decltype(st);
-    constexpr int NP = decltype(np)::value;
-    const uint32_t quads = (uint32_t)((ssm_columns(a.D, a.G) + 3) / 4);
-    const long each = (long)quads * a.G, all = a.chunks * each;
+    constexpr int NP = decltype(np)::value, W = decltype(w)::value;
+    const uint32_t teams = (uint32_t)ssm_teams(a.D, a.G);
+    const long each = (long)teams * a.G, all = a.chunks * each;
     if (all > 0x7fffffffl) return hipErrorInvalidValue;
     hipError_t e = a.N > kCheckInPlace ? launch_check_offsets(a.cu, a.N, a.T, a.status, s) : hipSuccess;
     if (e != hipSuccess) return e;
     if (a.chunks > 1) {
-      hipLaunchKernelGGL((ssm_scan_kernel<T, S, NP, false>), dim3((unsigned)(all - each)), dim3(256), 0, s, a, quads);
+      hipLaunchKernelGGL((ssm_scan_kernel<T, S, NP, W, false>), dim3((unsigned)(all - each)), dim3(W * 64), 0, s, a, teams);
       e = hipGetLastError();
       if (e == hipSuccess) e = launch_ssm_carry(a, false, s);
       if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((ssm_scan_kernel<T, S, NP, true>), dim3((unsigned)all), dim3(256), 0, s, a, quads);
+    hipLaunchKernelGGL((ssm_scan_kernel<T, S, NP, W, true>), dim3((unsigned)all), dim3(W * 64), 0, s, a, teams);
     return hipGetLastError();
   });
 }

@@ -12,16 +12,16 @@ namespace hagdn {
 constexpr int kBackRows = 8;
 
 // What a chunk passes back of a zero gradient.
-template <typename T, typename S, int NP>
-__global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back_local_kernel(SsmArgs a, uint32_t quads) {
-  using Stage = Maps<T, NP, 2, kBackRows, 256>;
+template <typename T, typename S, int NP, int W>
+__global__ __launch_bounds__(W * 64, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back_local_kernel(SsmArgs a, uint32_t teams) {
+  using Stage = Maps<T, NP, 2, kBackRows, W * 64>;
   __shared__ __align__(16) float sMaps[2][Stage::kAll];
   __shared__ int32_t sCu[kCheckInPlace + 1];
   Offsets32 cu;
   const bool ok = stage_offsets(a.cu, a.N, a.T, a.status, sCu, cu);
-  const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads;
-  const int chunk = 1 + (int)(blockIdx.x / (quads * a.G));  // the first chunk passes nothing on
-  const Column col(group, (quad - group * quads) * 4 + uniform(threadIdx.x >> 6), a);
+  const uint32_t team = blockIdx.x % (teams * a.G), group = team / teams;
+  const int chunk = 1 + (int)(blockIdx.x / (teams * a.G));  // the first chunk passes nothing on
+  const Column col(group, (team - group * teams) * W + uniform(threadIdx.x >> 6), a);
   const uint32_t c = col.c;
   if (!ok) return;
   const int t0 = chunk * a.chunk, t1 = (int)min((long)t0 + a.chunk, (long)a.T);
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_back
   }
   store_states(a.maps + (size_t)chunk * NP * a.D, a, col, e);
   if (col.mine) a.sums[(size_t)chunk * a.D + c] = sum;
-  if (quad == 0 && threadIdx.x == 0) a.resets[chunk] = reset;
+  if (team == 0 && threadIdx.x == 0) a.resets[chunk] = reset;
 }
 
 // Sums of N = 8 or 16 values over the wave's 64 lanes: value n to lanes 64 / N n and up.  Each
@@ -113,25 +113,23 @@ template <int N> __device__ __forceinline__ float sum_lanes(float (&v)[N]) {
   return s + dpp<0x4e>(s);   // lane ^ 2
 }
 
-// The forms for NP padded states: kWaves columns to a workgroup.  In LDS: the states at the
-// starts of a group's four runs of 8 tokens, the group's B and C, and a run's sums of dB
-// and dC for each wave.
-template <int NP> struct BackForm {
-  static constexpr int kWaves = NP == 64 ? 2 : 4;  // ssm_waves()
+// The LDS of NP padded states and W waves: the states at the starts of a group's runs of 8
+// tokens, the group's B and C, and a run's sums of dB and dC for each wave.
+template <int NP, int W> struct BackForm {
   static constexpr int kRuns = kSsmGroup / kBackRows;
-  static constexpr size_t kStates = (size_t)kWaves * kRuns * NP * 64, kSums = (size_t)kWaves * kBackRows * 2 * NP;
+  static constexpr size_t kStates = (size_t)W * kRuns * NP * 64, kSums = (size_t)W * kBackRows * 2 * NP;
   static constexpr size_t kMaps = (size_t)kSsmGroup * 2 * NP;
   static constexpr size_t kLds = (kStates + kSums + kMaps) * sizeof(float);
 };
 constexpr int kSlice = 8;  // states whose run of 8 tokens is held in registers at once
 
-// A group of 32 tokens at a time, the last first: its states at every eighth token are formed
+// A group of 16 tokens at a time, the last first: its states at every eighth token are formed
 // from the saved ones; then a run of 8 tokens at a time, the last first, and of 8 states of
 // it, goes forward again, its a_t h_{t-1} kept in registers, and back.
-template <typename T, typename S, int NP>
-__global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void ssm_backward_kernel(SsmArgs a, uint32_t quads) {
-  using F = BackForm<NP>;
-  using Stage = Maps<T, NP, 3, kSsmGroup, F::kWaves * 64>;
+template <typename T, typename S, int NP, int W>
+__global__ __launch_bounds__(W * 64, NP <= 32 ? 2 : 1) void ssm_backward_kernel(SsmArgs a, uint32_t teams) {
+  using F = BackForm<NP, W>;
+  using Stage = Maps<T, NP, 3, kSsmGroup, W * 64>;
   extern __shared__ __align__(16) float lds[];
   const int wave = uniform(threadIdx.x >> 6), lane = lane_id();
   float *starts = lds + (size_t)wave * F::kRuns * NP * 64 + lane;  // [runs][NP][64]
@@ -142,9 +140,9 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
   __shared__ int32_t sCu[kCheckInPlace + 1];
   Offsets32 cu;
   const bool ok = stage_offsets(a.cu, a.N, a.T, a.status, sCu, cu);
-  const uint32_t quad = blockIdx.x % (quads * a.G), group = quad / quads, in_group = quad - group * quads;
-  const int chunk = (int)(blockIdx.x / (quads * a.G));
-  const Column col(group, in_group * F::kWaves + wave, a);
+  const uint32_t team = blockIdx.x % (teams * a.G), group = team / teams, in_group = team - group * teams;
+  const int chunk = (int)(blockIdx.x / (teams * a.G));
+  const Column col(group, in_group * W + wave, a);
   const uint32_t c = col.c;
   if (chunk == 0) pass_states(a, ok, a.dfinal, a.ds0, col);
   const int t0 = chunk * a.chunk, t1 = ok ? (int)min((long)t0 + a.chunk, (long)a.T) : t0;
@@ -157,7 +155,7 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
   const float bias = a.raw && a.bias ? a.bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
 
   // waves of the workgroup that have channels
-  const int working = min(F::kWaves, (int)(((uint32_t)a.D / a.G + 63) / 64 - in_group * F::kWaves));
+  const int working = min(W, (int)(((uint32_t)a.D / a.G + 63) / 64 - in_group * W));
   Stage stage;
   for (int g0 = t0 + (t1 - 1 - t0) / kSsmGroup * kSsmGroup; t1 > t0 && g0 >= t0; g0 -= kSsmGroup) {
     const int g1 = min(g0 + kSsmGroup, t1), runs = (g1 - g0 + kBackRows - 1) / kBackRows;
@@ -330,7 +328,7 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
         if (a.z) store_tokens<T>(a.dz, a, col, base, count, dgate);
       }
       __syncthreads();
-      for (int i = threadIdx.x; i < count * 2 * NP; i += F::kWaves * 64) {
+      for (int i = threadIdx.x; i < count * 2 * NP; i += W * 64) {
         float s = 0.f;
         for (int v = 0; v < working; ++v) s += sums[v * kBackRows * 2 * NP + i];
         const size_t t = base + i / (2 * NP);
@@ -348,8 +346,8 @@ __global__ __launch_bounds__(BackForm<NP>::kWaves * 64, NP == 16 ? 2 : 1) void s
   out[(size_t)(NP + 1) * a.D] = dbias;
 }
 
-// dB and dC from the column groups' sums, in their order.
-template <typename T> __global__ __launch_bounds__(256) void ssm_sum_bc_kernel(SsmArgs a, int padded, uint32_t quads) {
+// dB and dC from the teams' sums, in their order.
+template <typename T> __global__ __launch_bounds__(256) void ssm_sum_bc_kernel(SsmArgs a, int padded, uint32_t teams) {
   if (*a.status != 0) return;
   const size_t rows = (size_t)a.T * a.G, total = rows * 2 * padded;
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (size_t)gridDim.x * 256) {
@@ -357,7 +355,7 @@ template <typename T> __global__ __launch_bounds__(256) void ssm_sum_bc_kernel(S
     const int e = (int)(i & (2 * padded - 1)), n = e & (padded - 1);
     if (n >= a.S) continue;
     float s = 0.f;
-    for (uint32_t q = 0; q < quads; ++q) s += a.dbc[q * total + i];
+    for (uint32_t q = 0; q < teams; ++q) s += a.dbc[q * total + i];
     static_cast<T *>(e < padded ? a.dB : a.dC)[row * a.S + n] = Elt<T>::from_f32(s);
   }
 }
@@ -385,33 +383,33 @@ __global__ __launch_bounds__(1024) void ssm_sum_weights_kernel(SsmArgs a, int pa
 }
 
 hipError_t launch_ssm_backward(const SsmArgs &a, bool bf16, bool dt_bf16, hipStream_t s) {
-  return ssm_dispatch(a.S, bf16, dt_bf16, [&](auto t, auto st, auto np) {
+  return ssm_dispatch(a, bf16, dt_bf16, [&](auto t, auto st, auto np, auto w) {
     using T = decltype(t);
     using S = decltype(st);
-    constexpr int NP = decltype(np)::value;
-    using F = BackForm<NP>;
-    const uint32_t fours = (uint32_t)((ssm_columns(a.D, a.G) + 3) / 4), quads = (uint32_t)ssm_quads(a.D, a.G, a.S);
-    const long all = (long)a.chunks * quads * a.G;
+    constexpr int NP = decltype(np)::value, W = decltype(w)::value;
+    using F = BackForm<NP, W>;
+    const uint32_t teams = (uint32_t)ssm_teams(a.D, a.G);
+    const long each = (long)teams * a.G, all = a.chunks * each;
     if (all > 0x7fffffffl) return hipErrorInvalidValue;
     hipError_t e = a.N > kCheckInPlace ? launch_check_offsets(a.cu, a.N, a.T, a.status, s) : hipSuccess;
     if (e != hipSuccess) return e;
     if (a.chunks > 1) {
-      hipLaunchKernelGGL((ssm_back_local_kernel<T, S, NP>), dim3((unsigned)((a.chunks - 1l) * fours * a.G)), dim3(256), 0, s, a,
-                         fours);
+      hipLaunchKernelGGL((ssm_back_local_kernel<T, S, NP, W>), dim3((unsigned)(all - each)), dim3(W * 64), 0, s, a, teams);
       e = hipGetLastError();
       if (e == hipSuccess) e = launch_ssm_carry(a, true, s);
       if (e != hipSuccess) return e;
     }
-    const void *kernel = reinterpret_cast<const void *>(&ssm_backward_kernel<T, S, NP>);
-    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)F::kLds);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((ssm_backward_kernel<T, S, NP>), dim3((unsigned)all), dim3(F::kWaves * 64),
-                       F::kLds, s, a, quads);
+    if (F::kLds > 48 * 1024) {
+      const void *kernel = reinterpret_cast<const void *>(&ssm_backward_kernel<T, S, NP, W>);
+      e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)F::kLds);
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((ssm_backward_kernel<T, S, NP, W>), dim3((unsigned)all), dim3(W * 64), F::kLds, s, a, teams);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     const size_t blocks = ((size_t)a.T * a.G * 2 * NP + 255) / 256;
     hipLaunchKernelGGL((ssm_sum_bc_kernel<T>), dim3((unsigned)(blocks < 1 ? 1 : blocks < 16384 ? blocks : 16384)), dim3(256), 0, s,
-                       a, NP, quads);
+                       a, NP, teams);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(ssm_sum_weights_kernel, dim3(((unsigned)a.D + 63) / 64, (unsigned)a.S + 2), dim3(1024), 0, s, a, NP);

@@ -13,8 +13,8 @@ namespace hagdn {
 
 constexpr size_t kMixerHeader = 256;  // workspace bytes before anything else: the status word
 // Offsets of up to this many sequences are checked by every workgroup that needs to know;
-// more are checked once, by a kernel of their own (check_kernel, 30000 offsets 8 us).
-constexpr int kCheckInPlace = 1024;
+// more are checked once, by a kernel of their own.
+constexpr int kCheckInPlace = 512;
 
 // ------------------------------------------------------- short causal convolution
 constexpr int kMinTaps = 2, kMaxTaps = 8;
@@ -100,7 +100,7 @@ struct SsmArgs {
   float *maps;                          // [chunks][padded S][D]: what a chunk leaves of nothing, then what enters it
   float *sums;                          // [chunks][D]: its step sizes' sum
   int *resets;                          // [chunks]: whether a sequence starts (backward: ends) in it
-  float *dbc;                           // [column groups of a group][T][G][2][padded S]: sums of dB and dC over channels
+  float *dbc;                           // [teams of a group][T][G][2][padded S]: sums of dB and dC over channels
   float *dweights;                      // [chunks][padded S + 2][D]: sums of dA, dskip and dbias over a chunk
   int chunk, chunks;                    // tokens of a chunk
 };
@@ -116,25 +116,27 @@ struct SsmStepArgs {
   void *y;
 };
 
-// Columns of 64 channels of a group of channels, and groups of four of them (two for the
-// most states), which a workgroup of the backward pass goes over together.
+// Columns of 64 channels of a group of channels, the waves of a workgroup, which have a column
+// each and share B and C (one where a group has fewer than four columns: the others would
+// only wait), and workgroups that a group's columns take.
 inline long ssm_columns(int D, int G) { return ((long)D / G + 63) / 64; }
-inline int ssm_waves(int S) { return S <= 32 ? 4 : 2; }
-inline long ssm_quads(int D, int G, int S) { return (ssm_columns(D, G) + ssm_waves(S) - 1) / ssm_waves(S); }
+inline int ssm_waves(int D, int G) { return ssm_columns(D, G) < 4 ? 1 : 4; }
+inline long ssm_teams(int D, int G) { return (ssm_columns(D, G) + ssm_waves(D, G) - 1) / ssm_waves(D, G); }
 
 // Tokens of a chunk: a workgroup goes over a chunk of its four columns.  The scan is bound by
 // its arithmetic, so that every CU should get as many workgroups as the others: one round of
-// what can be resident (four a CU; backward two, of most states one), or in calls where a
-// chunk would pass 512 tokens as few rounds as keep it below.  (17401 x 2048 tokens in 68 chunks
+// what can be resident (by registers and LDS), or in calls where a chunk would pass 512 tokens as few rounds as keep it below.  (17401 x 2048 tokens in 68 chunks
 // of 256, 2.1 workgroups a CU: outputs 230 us, backward 1022; in chunks of 136 and 288, 160 and
 // 730.)
 // Calls of up to 64 tokens of 16 states are one chunk, which needs one launch instead of three.
 inline int ssm_chunk(int T, int D, int S, int G, int cus, bool backward) {
-  const long each = backward ? ssm_quads(D, G, S) * G : (ssm_columns(D, G) + 3) / 4 * G;
-  const long slots = (cus > 0 ? cus : 256) * (backward ? (S <= 16 ? 2l : 1l) : 4l);
   const auto over = [](long a, long b) { return (a + b - 1) / b; };
-  const long total = (long)T * each, rounds = over(total + 1, slots * 512);
-  const int unit = backward ? kSsmGroup : 8, least = (long)T * ssm_padded(S) <= 1024 ? 64 : 16;
+  const int padded = ssm_padded(S);
+  const bool one = ssm_waves(D, G) == 1;
+  const int resident = !backward ? (one ? 16 : 4) : padded == 16 ? (one ? 8 : 2) : padded == 32 ? (one ? 6 : 2) : one ? 3 : 1;
+  const long slots = (cus > 0 ? cus : 256) * (long)resident;
+  const long total = (long)T * ssm_teams(D, G) * G, rounds = over(total + 1, slots * 512);
+  const int unit = backward ? kSsmGroup : 8, least = (long)T * padded <= 1024 ? 64 : 16;
   const long chunk = over(over(total, slots * rounds), unit) * unit;
   return (int)(chunk < least ? least : chunk);
 }

@@ -186,14 +186,18 @@ __device__ __forceinline__ void step_sizes(const SsmArgs &a, const S (&given)[N]
   for (int i = 0; i < N; ++i) step[i] = softplus(v[i]);
 }
 
-// The instance of a launcher for a call's types and padded states:
-// f(T(), S(), integral_constant<NP>).
-template <typename F> hipError_t ssm_dispatch(int states, bool bf16, bool dt_bf16, F f) {
+// The instance of a launcher for a call's types, padded states and waves of a workgroup:
+// f(T(), S(), integral_constant<NP>, integral_constant<W>).
+template <typename F> hipError_t ssm_dispatch(const SsmArgs &a, bool bf16, bool dt_bf16, F f) {
   const auto sized = [&](auto t, auto s) {
-    switch (ssm_padded(states)) {
-      case 16: return f(t, s, std::integral_constant<int, 16>());
-      case 32: return f(t, s, std::integral_constant<int, 32>());
-      default: return f(t, s, std::integral_constant<int, 64>());
+    const auto wide = [&](auto np) {
+      if (ssm_waves(a.D, a.G) == 1) return f(t, s, np, std::integral_constant<int, 1>());
+      return f(t, s, np, std::integral_constant<int, 4>());
+    };
+    switch (ssm_padded(a.S)) {
+      case 16: return wide(std::integral_constant<int, 16>());
+      case 32: return wide(std::integral_constant<int, 32>());
+      default: return wide(std::integral_constant<int, 64>());
     }
   };
   if (!bf16) return sized(float(), float());
