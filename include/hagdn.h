@@ -332,7 +332,8 @@ int hagdn_gate_norm_backward(const void *dy, int64_t dy_stride, const void *o,
  * sequence are the window that continues it.
  * The conventions of the gated linear recurrence hold (row strides, element alignment,
  * contiguous outputs, cu_seqlens NULL for N = 1, malformed ones), with
- *   weight [D, W] and bias [D] (or NULL) fp32, W = 2 .. 8, D = 1 .. 2^28;
+ *   weight [D, W] and bias [D] (or NULL) fp32, W = 2 .. 8, D = 1 .. 2^28, T_total up to
+ *   2^31 - 2^16;
  *   windows [N, W - 1, D] dtype, oldest input first; w0 NULL: zeros;
  *   activation HAGDN_ACT_SILU or HAGDN_ACT_NONE.
  * Sums are fp32.  Outputs must not overlap inputs (w_final not even w0 exactly: other
@@ -378,7 +379,7 @@ int hagdn_conv_decode(const void *x, int64_t x_stride, const float *weight, cons
  *   A [D, S], skip [D] (or NULL) fp32;  S = 1 .. 64;  D % G == 0;
  *   states [N, D, S] fp32; s0 NULL: zero.
  * dt A <= 0 is expected: where some 500 tokens together let a state grow by e^88
- * results are unspecified.  N x D x S below 2^31.  Sums and states are fp32.  Outputs must
+ * results are unspecified.  N x D x S below 2^31, T_total up to 2^31 - 2^16.  Sums and states are fp32.  Outputs must
  * not overlap inputs (s_final not even s0 exactly, nor ds0 dfinal).  Results repeat bit
  * for bit on one device.  No value of one sequence reaches another. */
 

@@ -82,9 +82,17 @@ int query_cus() {
 
 size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
 
+// Token numbers, and those of the rows that kernels look ahead for, fit 31 bits.
+constexpr int kMaxTokens = 0x7fff0000;
+int check_tokens(int T) {
+  if (T < 0) return fail(HAGDN_EINVAL, "T_total must be >= 0 (got %d)", T);
+  if (T > kMaxTokens) return fail(HAGDN_EUNSUPPORTED, "T_total > %d unsupported (got %d)", kMaxTokens, T);
+  return HAGDN_OK;
+}
+
 // --------------------------------------------------------------- convolution
 int check_conv(int T, int D, int W, int dtype, int activation) {
-  if (T < 0) return fail(HAGDN_EINVAL, "T_total must be >= 0 (got %d)", T);
+  if (int rc = check_tokens(T)) return rc;
   if (D < 1) return fail(HAGDN_EINVAL, "D must be >= 1 (got %d)", D);
   if (D > (1 << 28)) return fail(HAGDN_EUNSUPPORTED, "D > 2^28 unsupported");
   if (W < hagdn::kMinTaps || W > hagdn::kMaxTaps)
@@ -115,7 +123,7 @@ int check_workspace(const void *ws, size_t bytes, size_t need) {
 
 // ---------------------------------------------------------------------- scan
 int check_ssm(int T, int D, int S, int G, int dtype, int dt_dtype, int pre) {
-  if (T < 0) return fail(HAGDN_EINVAL, "T_total must be >= 0 (got %d)", T);
+  if (int rc = check_tokens(T)) return rc;
   if (D < 1) return fail(HAGDN_EINVAL, "D must be >= 1 (got %d)", D);
   if (D > (1 << 28)) return fail(HAGDN_EUNSUPPORTED, "D > 2^28 unsupported");
   if (S < 1) return fail(HAGDN_EINVAL, "S must be >= 1 (got %d)", S);

@@ -204,11 +204,9 @@ hipError_t launch_ssm_forward(const SsmArgs &a, bool bf16, bool dt_bf16, hipStre
 // P states of a channel to a lane, S / P lanes (a power of two up to 16) to a channel; P = 0: a
 // lane goes over all of a channel's states.
 template <typename T, typename S, int P>
-__global__ __launch_bounds__(256) void ssm_step_kernel(SsmStepArgs a, uint32_t lanes, uint64_t items) {
-  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (uint64_t)gridDim.x * 256) {
-    const uint32_t part = (uint32_t)i & (lanes - 1);
-    const uint64_t row = i / lanes;
-    const uint32_t n = (uint32_t)(row / (uint32_t)a.D), c = (uint32_t)(row - (uint64_t)n * a.D);
+__global__ __launch_bounds__(256) void ssm_step_kernel(SsmStepArgs a, uint32_t lanes, uint32_t items) {
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < items; i += gridDim.x * 256) {  // N x D x S < 2^31
+    const uint32_t part = i & (lanes - 1), row = i / lanes, n = row / (uint32_t)a.D, c = row - n * (uint32_t)a.D;
     const int slot = a.slots ? a.slots[n] : (int)n;
     const bool live = slot >= 0 && slot < a.num_slots;
     float y = 0.f, x = 0.f;
@@ -254,8 +252,8 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmStepArgs a, uint32_t l
 template <typename T, typename S> hipError_t ssm_step(const SsmStepArgs &a, hipStream_t s) {
   const bool four = a.S % 4 == 0 && (a.S & (a.S - 1)) == 0;
   const uint32_t lanes = four ? (uint32_t)a.S / 4 : 1;
-  const uint64_t items = (uint64_t)a.N * a.D * lanes, blocks = (items + 255) / 256;
-  const dim3 grid((unsigned)(blocks < 1u << 20 ? blocks : 1u << 20));
+  const uint32_t items = (uint32_t)a.N * a.D * lanes, blocks = (items + 255) / 256;
+  const dim3 grid(blocks < 1u << 20 ? blocks : 1u << 20);
   if (four) hipLaunchKernelGGL((ssm_step_kernel<T, S, 4>), grid, dim3(256), 0, s, a, lanes, items);
   else hipLaunchKernelGGL((ssm_step_kernel<T, S, 0>), grid, dim3(256), 0, s, a, lanes, items);
   return hipGetLastError();

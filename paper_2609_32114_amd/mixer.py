@@ -40,6 +40,15 @@ def _size(n):
     return n
 
 
+def _call(di, fn, *args):
+    """fn(*args) with the operands' GPU current, whose streams it launches on."""
+    if torch._C._cuda_getDevice() == di:
+        _check(fn(*args))
+    else:
+        with torch.cuda.device(di):
+            _check(fn(*args))
+
+
 def _slots(slots, S, N, x):
     if slots is None:
         if S < N:
@@ -87,9 +96,8 @@ def conv_prefill(x, weight, bias=None, initial_window=None, cu_seqlens=None, act
     ws, ws_bytes = _workspace(workspace, lambda: conv_workspace_size(T, D, W), x)
     y = _like("out", out, x)
     final = _output("final_out", final_out, windows, x.dtype, x) if output_final_window else None
-    _check(lib.hagdn_conv_prefill(
-        x.data_ptr(), xs, weight.data_ptr(), pb, _ptr(initial_window), cu, N, T, D, W, dt, act, y.data_ptr(),
-        _ptr(final), ws.data_ptr(), ws_bytes, _stream(di)))
+    _call(di, lib.hagdn_conv_prefill, x.data_ptr(), xs, weight.data_ptr(), pb, _ptr(initial_window), cu, N, T, D, W,
+          dt, act, y.data_ptr(), _ptr(final), ws.data_ptr(), ws_bytes, _stream(di))
     return y, final
 
 
@@ -114,9 +122,9 @@ def conv_backward(dy, x, weight, bias=None, initial_window=None, dfinal=None, cu
     ws, ws_bytes = _workspace(workspace, lambda: conv_workspace_size(T, D, W, True), x)
     dx, dw = _like("dx", None, x), torch.empty_like(weight)
     db = torch.empty_like(bias) if bias is not None else None
-    _check(lib.hagdn_conv_backward(
-        dy.data_ptr(), dys, x.data_ptr(), xs, weight.data_ptr(), pb, _ptr(initial_window), _ptr(dfinal), cu, N, T,
-        D, W, dt, act, dx.data_ptr(), dw.data_ptr(), _ptr(db), _ptr(dw0), ws.data_ptr(), ws_bytes, _stream(di)))
+    _call(di, lib.hagdn_conv_backward, dy.data_ptr(), dys, x.data_ptr(), xs, weight.data_ptr(), pb,
+          _ptr(initial_window), _ptr(dfinal), cu, N, T, D, W, dt, act, dx.data_ptr(), dw.data_ptr(), _ptr(db),
+          _ptr(dw0), ws.data_ptr(), ws_bytes, _stream(di))
     return dx, dw, db, dw0
 
 
@@ -132,9 +140,8 @@ def conv_decode(x, weight, state, bias=None, slots=None, activation="silu", out=
     _check_buffer("state", state, x.device, x.dtype, (S, W - 1, D))
     _slots(slots, S, N, x)
     y = _like("out", out, x)
-    _check(lib.hagdn_conv_decode(
-        x.data_ptr(), xs, weight.data_ptr(), pb, state.data_ptr(), _ptr(slots), S, N, D, W, dt, act, y.data_ptr(),
-        _stream(di)))
+    _call(di, lib.hagdn_conv_decode, x.data_ptr(), xs, weight.data_ptr(), pb, state.data_ptr(), _ptr(slots), S, N, D,
+          W, dt, act, y.data_ptr(), _stream(di))
     return y
 
 
@@ -220,9 +227,8 @@ def ssm_prefill(x, dt, A, B, C, skip=None, z=None, dt_bias=None, initial_state=N
     y = _like("out", out, x)
     final = _output("final_out", final_out, (N, D, S), _F32, x) if output_final_state else None
     saved = x.new_empty(ssm_checkpoints_size(T, D, S), dtype=_F32) if output_checkpoints else None
-    _check(lib.ssm_prefill(
-        *args, _ptr(initial_state), cu, N, T, D, S, G, *types, int(preprocess), y.data_ptr(), _ptr(final), _ptr(saved),
-        ws.data_ptr(), ws_bytes, _stream(di)))
+    _call(di, lib.ssm_prefill, *args, _ptr(initial_state), cu, N, T, D, S, G, *types, int(preprocess), y.data_ptr(),
+          _ptr(final), _ptr(saved), ws.data_ptr(), ws_bytes, _stream(di))
     return (y, final, saved) if output_checkpoints else (y, final)
 
 
@@ -250,10 +256,9 @@ def ssm_backward(dy, x, dt, A, B, C, checkpoints, skip=None, z=None, dt_bias=Non
     dskip = torch.empty_like(skip) if skip is not None else None
     dz = _like("dz", None, z) if z is not None else None
     dbias = torch.empty_like(dt_bias) if dt_bias is not None else None
-    _check(lib.ssm_backward(
-        dy.data_ptr(), dys, *args, checkpoints.data_ptr(), _ptr(initial_state), _ptr(dfinal), cu, N, T, D, S, G, *types,
-        int(preprocess), dx.data_ptr(), ddt.data_ptr(), dA.data_ptr(), dB.data_ptr(), dC.data_ptr(), _ptr(dskip), _ptr(dz),
-        _ptr(dbias), _ptr(ds0), ws.data_ptr(), ws_bytes, _stream(di)))
+    _call(di, lib.ssm_backward, dy.data_ptr(), dys, *args, checkpoints.data_ptr(), _ptr(initial_state), _ptr(dfinal),
+          cu, N, T, D, S, G, *types, int(preprocess), dx.data_ptr(), ddt.data_ptr(), dA.data_ptr(), dB.data_ptr(),
+          dC.data_ptr(), _ptr(dskip), _ptr(dz), _ptr(dbias), _ptr(ds0), ws.data_ptr(), ws_bytes, _stream(di))
     return dx, ddt, dA, dB, dC, dskip, dz, dbias, ds0
 
 
@@ -267,7 +272,6 @@ def ssm_decode(x, dt, A, B, C, state, slots=None, skip=None, z=None, dt_bias=Non
     _fp32("state", state, (pool, D, S), x)
     _slots(slots, pool, N, x)
     y = _like("out", out, x)
-    _check(lib.ssm_decode(
-        *args, state.data_ptr(), _ptr(slots), pool, N, D, S, G, *types, int(preprocess), y.data_ptr(),
-        _stream(di)))
+    _call(di, lib.ssm_decode, *args, state.data_ptr(), _ptr(slots), pool, N, D, S, G, *types, int(preprocess),
+          y.data_ptr(), _stream(di))
     return y

@@ -16,7 +16,8 @@ import ctypes
 import torch
 
 from . import HagdnError, _check_buffer, _err, _ptr, load_library
-from .layer import _check, _stream, _workspace
+from .layer import _stream, _workspace
+from .mixer import _call
 
 
 def pool_workspace_size(slots: int) -> int:
@@ -29,7 +30,7 @@ def pool_workspace_size(slots: int) -> int:
 
 
 def _pools(pools, name="pools"):
-    """(first tensor, rows, pointers, row sizes, count) of a list of pools."""
+    """(first tensor, its device index, rows, pointers, row sizes, count) of a list of pools."""
     pools = [pools] if isinstance(pools, torch.Tensor) else list(pools)
     if not pools:
         raise ValueError(f"{name} must not be empty")
@@ -42,7 +43,7 @@ def _pools(pools, name="pools"):
             raise ValueError(f"{name} must have one number of rows (got {[tuple(q.shape) for q in pools]})")
     sizes = [p.numel() // rows * p.element_size() if rows else 0 for p in pools]
     n = len(pools)
-    return first, rows, (ctypes.c_void_p * n)(*[p.data_ptr() for p in pools]), (ctypes.c_size_t * n)(*sizes), n
+    return first, di, rows, (ctypes.c_void_p * n)(*[p.data_ptr() for p in pools]), (ctypes.c_size_t * n)(*sizes), n
 
 
 def _table(name, t, pool):
@@ -61,11 +62,11 @@ def pool_copy(pools, dst=None, src=None, sources=None):
     them.  dst outside the pool: padding; src outside: a row of zeros, a new sequence's state.
     No two entries may name one destination."""
     lib = load_library()
-    first, rows, pointers, sizes, n = _pools(pools)
+    first, di, rows, pointers, sizes, n = _pools(pools)
     from_rows, from_pointers = rows, None
     if sources is not None:
-        other, from_rows, from_pointers, from_sizes, m = _pools(sources, "sources")
-        if m != n or other.get_device() != first.get_device():
+        _, other, from_rows, from_pointers, from_sizes, m = _pools(sources, "sources")
+        if m != n or other != di:
             raise ValueError("sources must be as many tensors as pools, on the same GPU")
         if rows and from_rows and list(sizes) != list(from_sizes):
             raise ValueError("rows of sources must have the pools' sizes")
@@ -80,14 +81,14 @@ def pool_copy(pools, dst=None, src=None, sources=None):
         return
     if sources is not None and from_rows == 0:
         raise ValueError("sources have no rows")
-    _check(lib.hagdn_pool_copy(pointers, from_pointers, sizes, n, _ptr(dst), _ptr(src), count, rows, from_rows,
-                               _stream(first.get_device())))
+    _call(di, lib.hagdn_pool_copy, pointers, from_pointers, sizes, n, _ptr(dst), _ptr(src), count, rows, from_rows,
+          _stream(di))
 
 
 def _plan(pools, workspace):
-    first, rows, pointers, sizes, n = _pools(pools)
+    first, di, rows, pointers, sizes, n = _pools(pools)
     ws, ws_bytes = _workspace(workspace, lambda: pool_workspace_size(rows), first)
-    return first, rows, pointers, sizes, n, ws, ws_bytes
+    return first, di, rows, pointers, sizes, n, ws, ws_bytes
 
 
 def _new_slots(out, count, pool):
@@ -105,11 +106,11 @@ def pool_fork(pools, slots, parents, workspace=None, out=None):
     children's slots; -1 where the parent has none, or the free slots did not suffice
     (device_status of the caller's own workspace is then DEV_POOL_FULL)."""
     lib = load_library()
-    first, rows, pointers, sizes, n, ws, ws_bytes = _plan(pools, workspace)
+    first, di, rows, pointers, sizes, n, ws, ws_bytes = _plan(pools, workspace)
     N, M = _table("slots", slots, first), _table("parents", parents, first)
     new = _new_slots(out, M, first)
-    _check(lib.hagdn_pool_fork(pointers, sizes, n, slots.data_ptr(), N, parents.data_ptr(), M, rows, new.data_ptr(),
-                               ws.data_ptr(), ws_bytes, _stream(first.get_device())))
+    _call(di, lib.hagdn_pool_fork, pointers, sizes, n, slots.data_ptr(), N, parents.data_ptr(), M, rows,
+          new.data_ptr(), ws.data_ptr(), ws_bytes, _stream(di))
     return new
 
 
@@ -118,9 +119,9 @@ def pool_compact(pools, slots, workspace=None, out=None):
     live slots those from L on go, in order, to the free ones below L.  Returns the table
     after it (``out`` may be the table itself); entries outside the pools stay as they are."""
     lib = load_library()
-    first, rows, pointers, sizes, n, ws, ws_bytes = _plan(pools, workspace)
+    first, di, rows, pointers, sizes, n, ws, ws_bytes = _plan(pools, workspace)
     N = _table("slots", slots, first)
     new = _new_slots(out, N, first)
-    _check(lib.hagdn_pool_compact(pointers, sizes, n, slots.data_ptr(), N, rows, new.data_ptr(), ws.data_ptr(), ws_bytes,
-                                  _stream(first.get_device())))
+    _call(di, lib.hagdn_pool_compact, pointers, sizes, n, slots.data_ptr(), N, rows, new.data_ptr(), ws.data_ptr(),
+          ws_bytes, _stream(di))
     return new

@@ -53,7 +53,7 @@ def test_conv_refusals(fn, d):
                  dict(ws=F[7] + 8), dict(cu=None), dict(cu=F[4] + 2), dict(xs=-1), dict(xs=1 << 31), dict(x=F[0] + 1),
                  dict(w=F[1] + 2), dict(w0=F[3] + 1)):
         assert call(fn, d, **{"wsb": BIG, **over})[0] == EINVAL, over
-    for over in (dict(dtype=2), dict(W=1), dict(W=9), dict(W=-3), dict(D=(1 << 28) + 1)):
+    for over in (dict(dtype=2), dict(W=1), dict(W=9), dict(W=-3), dict(D=(1 << 28) + 1), dict(T=0x7fff0001)):
         assert call(fn, d, **{"wsb": BIG, **over})[0] == EUNSUP, over
     out = dict(y=None) if fn == "hagdn_conv_prefill" else dict(dx=None)
     assert call(fn, d, **{"wsb": BIG, **out})[0] == EINVAL
@@ -83,7 +83,8 @@ def test_ssm_refusals(fn, d):
                  dict(ws=F[13] + 8), dict(cu=None), dict(xs=-1), dict(Bs=1 << 31), dict(zs=-4), dict(x=F[0] + 1),
                  dict(dt=F[1] + 2), dict(B=F[3] + 1), dict(N=1 << 20, D=1 << 12)):
         assert call(fn, d, **{"wsb": BIG, **over})[0] == EINVAL, over
-    for over in (dict(dtype=2), dict(st=3), dict(dtype=0, st=1), dict(S=65), dict(N=1, D=(1 << 28) + 1, S=1)):
+    for over in (dict(dtype=2), dict(st=3), dict(dtype=0, st=1), dict(S=65), dict(N=1, D=(1 << 28) + 1, S=1),
+                 dict(T=0x7fff0001)):
         assert call(fn, d, **{"wsb": BIG, **over})[0] == EUNSUP, over
     outs = ("y",) if fn == "ssm_prefill" else ("dx", "ddt", "dA", "dB", "dC", "dskip", "dz", "dbias", "ck")
     for name in outs:

@@ -190,10 +190,11 @@ def test_block_together():
 
 
 @gpu
-def test_graph_replays():
+@pytest.mark.parametrize("S", [16, 40])
+def test_graph_replays(S):
     """Prefill, backward, step and pools captured together, replayed on new inputs, with eager work
     and synchronisations between the replays."""
-    lens, D, S = (70, 40), 130, 16
+    lens, D = (70, 40), 130
     o = {k: v.detach() for k, v in operands(lens, D, S, torch.bfloat16).items()}
     off, w = cu(lens), torch.randn(D, 4, device="cuda")
     pools = [torch.zeros(6, 3, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(6, D, S, device="cuda")]
@@ -300,8 +301,8 @@ def test_binding_refuses_tensors_off_the_gpu():
     with pytest.raises(ValueError, match="empty"):
         P.pool_copy([])
     with pytest.raises(ValueError, match="activation"):
-        P.mixer._activation("gelu") if hasattr(P, "mixer") else __import__(
-            "paper_2609_32114_amd.mixer", fromlist=["x"])._activation("gelu")
+        from paper_2609_32114_amd import mixer
+        mixer._activation("gelu")
 
 
 @gpu
