@@ -83,7 +83,9 @@ __global__ __launch_bounds__(W * 64, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_s
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               float &s = h[n + k];
-              s = __builtin_fmaf(__builtin_amdgcn_exp2f(step[i] * A[n + k]), s, in * B[k]);
+              // (in place: a product and a fused sum into the state's own register)
+              s *= __builtin_amdgcn_exp2f(step[i] * A[n + k]);
+              s = __builtin_fmaf(in, B[k], s);
               if (OUT) y[i] = __builtin_fmaf(C[k], s, y[i]);
             }
           }

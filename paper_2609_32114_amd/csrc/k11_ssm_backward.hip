@@ -197,7 +197,7 @@ __global__ __launch_bounds__(W * 64, NP <= 32 ? 2 : 1) void ssm_backward_kernel(
                 const f32x4 B = rows.four(i * 2 * NP + n);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                  h[n + k] = __builtin_fmaf(__builtin_amdgcn_exp2f(step[i] * A[n + k]), h[n + k], in * B[k]);
+                  h[n + k] = __builtin_fmaf(in, B[k], __builtin_amdgcn_exp2f(step[i] * A[n + k]) * h[n + k]);
               }
             }
           lo = hi;
