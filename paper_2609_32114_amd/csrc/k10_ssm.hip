@@ -1,5 +1,15 @@
 // k10_ssm.hip -- the selective state space scan, forward (ssm.h has the scheme), and its
 // step for single tokens.
+//
+// Bound by its arithmetic: per token, channel and state a product, an exponential (8 cycles
+// of a wave, the others 4) and three or, for outputs, four more operations, and both passes over
+// the chunks take them.  32768 tokens x 2048 channels x 16 states, x, z, y and dt in bf16: what
+// chunks leave 211 to 230 us, what enters them 10, outputs 279 to 300 (the clock falls under
+// this load from 2.4 to 2.2 GHz), where 539 MB would take 104 us of HBM.  The vector units are
+// busy 85 % of the time; 22 of 86 instructions a token and lane are the step size's softplus
+// and conversions, in outputs 30 of 110.  On the way (both passes): B and C through scalar loads
+// and each sequence's end inside an unrolled loop 697 us; B and C through LDS, ends apart 573;
+// the next rows on their way, no copies around the states 510.
 #include "ssm.h"
 
 namespace hagdn {

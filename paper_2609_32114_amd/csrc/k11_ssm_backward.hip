@@ -5,6 +5,17 @@
 //   dC_t = sum_d dy_t h_t,  dB_t = sum_d dh_t dt_t x_t,  w_t = sum_n dh_t B_t,
 //   dx_t = dt_t w_t + skip dy_t,  d(dt_t) = x_t w_t + sum_n A dh_t a_t h_{t-1},
 //   dA = sum_t dt_t dh_t a_t h_{t-1}.
+//
+// Bound by its arithmetic, as the forward pass: some 29 instructions per token, channel and
+// state in the main kernel, of which 4.4 are the sums of dB and dC over lanes and 8 form the
+// states again.  17401 x 2048 x 16 in bf16, packed from eight sequences: what chunks pass back
+// 149 us, what reaches them 8, the main kernel 676, sums 16.  The vector units are busy 3/4 of
+// the time: two waves a SIMD, 232 registers each.  On the way: states formed again over 64
+// tokens from scalar rows 1665 us; through LDS, 8 states at a time 1020; chunks that fill every
+// CU alike 760; states saved every 16 tokens instead of 32 720 (every 8: 660, for twice the
+// memory); sums written by all lanes that have them 690.  Three waves a SIMD with 4 states at a
+// time spill (808); a branch-free copy for whole runs spills too (871); sums over lanes
+// through LDS 680 to 720; decays kept instead of formed again 685.
 #include "ssm.h"
 
 namespace hagdn {
@@ -87,30 +98,28 @@ __global__ __launch_bounds__(W * 64, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_b
   if (team == 0 && threadIdx.x == 0) a.resets[chunk] = reset;
 }
 
-// Sums of N = 8 or 16 values over the wave's 64 lanes: value n to lanes 64 / N n and up.  Each
-// exchange halves the values that a lane still holds: 35 instructions for 16 values instead of
-// the 96 of separate sums.
+// Sums of 16 values over the wave's 64 lanes: value n to lanes 4 n to 4 n + 3.  Each exchange
+// halves the values that a lane still holds: 35 instructions instead of the 96 of separate sums.
 template <int CTRL> __device__ __forceinline__ float dpp(float v) {
   return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true));
 }
-template <int N> __device__ __forceinline__ float sum_lanes(float (&v)[N]) {
+__device__ __forceinline__ float sum_lanes(float (&v)[16]) {
 #pragma unroll
-  for (int i = 0; i < N / 2; ++i) {  // halves of 32 lanes
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 2]), false, false);
+  for (int i = 0; i < 8; ++i) {  // halves of 32 lanes
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 8]), false, false);
     v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
 #pragma unroll
-  for (int i = 0; i < N / 4; ++i) {  // rows of 16
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 4]), false, false);
+  for (int i = 0; i < 4; ++i) {  // rows of 16
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 4]), false, false);
     v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
   }
   const bool high8 = lane_id() & 8, high4 = lane_id() & 4;
 #pragma unroll
-  for (int i = 0; i < N / 8; ++i)  // lane + 8 of 16
-    v[i] = (high8 ? v[i + N / 8] : v[i]) + dpp<0x128>(high8 ? v[i] : v[i + N / 8]);
-  float s = N == 16 ? (high4 ? v[1] : v[0]) + dpp<0x141>(high4 ? v[0] : v[1]) : v[0] + dpp<0x141>(v[0]);  // lane 7 - i of 8
-  s += dpp<0xb1>(s);         // lane ^ 1
-  return s + dpp<0x4e>(s);   // lane ^ 2
+  for (int i = 0; i < 2; ++i) v[i] = (high8 ? v[i + 2] : v[i]) + dpp<0x128>(high8 ? v[i] : v[i + 2]);  // lane + 8 of 16
+  float s = (high4 ? v[1] : v[0]) + dpp<0x141>(high4 ? v[0] : v[1]);                                   // lane 7 - i of 8
+  s += dpp<0xb1>(s);        // lane ^ 1
+  return s + dpp<0x4e>(s);  // lane ^ 2
 }
 
 // The LDS of NP padded states and W waves: the states at the starts of a group's runs of 8

@@ -123,12 +123,12 @@ inline long ssm_columns(int D, int G) { return ((long)D / G + 63) / 64; }
 inline int ssm_waves(int D, int G) { return ssm_columns(D, G) < 4 ? 1 : 4; }
 inline long ssm_teams(int D, int G) { return (ssm_columns(D, G) + ssm_waves(D, G) - 1) / ssm_waves(D, G); }
 
-// Tokens of a chunk: a workgroup goes over a chunk of its four columns.  The scan is bound by
-// its arithmetic, so that every CU should get as many workgroups as the others: one round of
-// what can be resident (by registers and LDS), or in calls where a chunk would pass 512 tokens as few rounds as keep it below.  (17401 x 2048 tokens in 68 chunks
-// of 256, 2.1 workgroups a CU: outputs 230 us, backward 1022; in chunks of 136 and 288, 160 and
-// 730.)
-// Calls of up to 64 tokens of 16 states are one chunk, which needs one launch instead of three.
+// Tokens of a chunk, which a workgroup goes over.  The scan is bound by its arithmetic, so that
+// every CU should get as many workgroups as the others: one round of what can be resident (by
+// registers and LDS), or in calls where a chunk would pass 512 tokens as few rounds as keep it
+// below.  (17401 x 2048 tokens in 68 chunks of 256, 2.1 workgroups a CU: outputs 230 us, backward
+// 1022; in chunks of 136 and 288 160 and 760.)  Calls of up to 64 tokens of 16 states are one
+// chunk, which needs one launch instead of three.
 inline int ssm_chunk(int T, int D, int S, int G, int cus, bool backward) {
   const auto over = [](long a, long b) { return (a + b - 1) / b; };
   const int padded = ssm_padded(S);
