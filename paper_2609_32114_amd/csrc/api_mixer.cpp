@@ -178,7 +178,6 @@ void set_plan(hagdn::SsmArgs *a, const SsmPlan &p, void *ws) {
   char *w = static_cast<char *>(ws);
   a->chunk = p.chunk;
   a->chunks = p.chunks;
-  a->cus = query_cus();
   a->status = reinterpret_cast<int *>(w);
   a->maps = reinterpret_cast<float *>(w + p.maps);
   a->sums = reinterpret_cast<float *>(w + p.sums);
@@ -314,8 +313,7 @@ int hagdn_conv_prefill(const void *x, int64_t x_stride, const float *weight, con
   hagdn::ConvArgs a = {};
   a.x = x; a.xs = x_stride; a.w = weight; a.b = bias; a.w0 = w0; a.cu = cu_seqlens; a.N = N; a.T = T_total; a.D = D; a.W = W;
   a.silu = activation == HAGDN_ACT_SILU; a.y = y; a.w_final = w_final; a.status = static_cast<int *>(workspace);
-  a.cus = query_cus();
-  a.run = hagdn::conv_forward_run(T_total, D, a.cus);
+  a.run = hagdn::conv_forward_run(T_total, D, query_cus());
   return done(hagdn::launch_conv_forward(a, dtype == HAGDN_BF16, static_cast<hipStream_t>(stream)));
 }
 
@@ -344,9 +342,8 @@ int hagdn_conv_backward(const void *dy, int64_t dy_stride, const void *x, int64_
   a.cu = cu_seqlens; a.N = N; a.T = T_total; a.D = D; a.W = W; a.silu = activation == HAGDN_ACT_SILU;
   a.dx = dx; a.dw = dweight; a.db = bias ? dbias : nullptr; a.dw0 = dw0; a.status = static_cast<int *>(workspace);
   a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + hagdn::kMixerHeader);
-  a.cus = query_cus();
-  a.run = hagdn::conv_run(T_total, D, a.cus);
-  a.parts = hagdn::conv_parts(T_total, D, a.cus);
+  a.run = hagdn::conv_run(T_total, D, query_cus());
+  a.parts = hagdn::conv_parts(T_total, D, query_cus());
   return done(hagdn::launch_conv_backward(a, dtype == HAGDN_BF16, static_cast<hipStream_t>(stream)));
 }
 

@@ -35,7 +35,6 @@ struct ConvArgs {
   float *partial;         // [parts][W + 1][D]
   int parts;              // runs of tokens whose sums of the weights' gradients stand apart
   int run;                // tokens of a run
-  int cus;
 };
 
 struct ConvStepArgs {
@@ -94,7 +93,6 @@ struct SsmArgs {
   float *ckpt;                          // [ceil(T / group), padded S, D] or null
   void *dx, *ddt, *dz, *dB, *dC;        // [T, D], .., [T, G, S]
   float *dA, *dskip, *dbias, *ds0;
-  int cus;
   // workspace
   int *status;
   float *maps;                          // [chunks][padded S][D]: what a chunk leaves of nothing, then what enters it
