@@ -121,8 +121,7 @@ def serve(model, lens, ahead):
     # the states live in a larger pool, in any order
     slots = torch.randperm(2 * len(lens), generator=gen, device="cuda")[:len(lens)].to(torch.int32)
     pools = [torch.zeros(2 * len(lens), model.width, device="cuda") for _ in finals]
-    for pool, final in zip(pools, finals):
-        pool[slots.long()] = final
+    hagdn.pool_copy(pools, dst=slots, sources=finals)
     stepped = [model.step(torch.stack([d[n + t] for d, n in zip(docs, lens)]), pools, slots) for t in range(ahead)]
     whole = model.logits(tokens, whole_cu).split([n + ahead for n in lens])
     return torch.stack(stepped, 1), torch.stack([w[n:] for w, n in zip(whole, lens)])

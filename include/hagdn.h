@@ -342,7 +342,8 @@ int hagdn_gate_norm_backward(const void *dy, int64_t dy_stride, const void *o,
 /* Bytes of workspace (0 on invalid sizes); backward 1: of hagdn_conv_backward. */
 size_t hagdn_conv_workspace_size(int T_total, int D, int W, int backward);
 
-/* y [T, D] and, unless NULL, w_final [N, W - 1, D]. */
+/* y [T, D] and, unless NULL, w_final [N, W - 1, D].  workspace may be NULL for up to 512
+ * sequences: malformed offsets are then found all the same, but not reported. */
 int hagdn_conv_prefill(const void *x, int64_t x_stride, const float *weight, const float *bias,
                        const void *w0, const int32_t *cu_seqlens, int N, int T_total, int D, int W,
                        int dtype, int activation, void *y, void *w_final, void *workspace,

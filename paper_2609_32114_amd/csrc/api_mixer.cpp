@@ -298,7 +298,8 @@ int hagdn_conv_prefill(const void *x, int64_t x_stride, const float *weight, con
                        void *w_final, void *workspace, size_t workspace_bytes, void *stream) {
   if (int rc = check_sequences(cu_seqlens, N)) return rc;
   if (int rc = check_conv(T_total, D, W, dtype, activation)) return rc;
-  if (int rc = check_workspace(workspace, workspace_bytes, conv_bytes(T_total, D, W, false))) return rc;
+  if (workspace || N > hagdn::kCheckInPlace)
+    if (int rc = check_workspace(workspace, workspace_bytes, conv_bytes(T_total, D, W, false))) return rc;
   const Stride ss[] = {{x_stride, "x_stride"}};
   if (int rc = check_strides(ss)) return rc;
   const bool tok = T_total > 0;

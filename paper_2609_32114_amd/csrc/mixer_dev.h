@@ -63,8 +63,8 @@ struct Offsets32 {
   }
 };
 // Fills the LDS copy and says whether cu[0 .. N] are the offsets of N sequences over T tokens:
-// asked here, where the call's first workgroup tells the host, or by the kernel before.  The
-// whole workgroup calls.
+// asked here, where the call's first workgroup tells the host (unless status is null), or by the
+// kernel before.  The whole workgroup calls.
 __device__ __forceinline__ bool stage_offsets(const int32_t *cu, int N, int T, int *status, int32_t (&lds)[kCheckInPlace + 1],
                                               Offsets32 &o) {
   o = {cu, N, T, (const HAGDN_LDS int32_t *)lds};
@@ -78,7 +78,7 @@ __device__ __forceinline__ bool stage_offsets(const int32_t *cu, int N, int T, i
     if (threadIdx.x == 0) bad |= lds[0] != 0 || lds[N] != T;
     ok = !__syncthreads_or(bad);
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) *status = ok ? 0 : kDevBadSeqlens;
+  if (status && blockIdx.x == 0 && threadIdx.x == 0) *status = ok ? 0 : kDevBadSeqlens;
   return ok;
 }
 

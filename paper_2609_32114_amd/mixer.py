@@ -93,11 +93,13 @@ def conv_prefill(x, weight, bias=None, initial_window=None, cu_seqlens=None, act
     windows = (N, W - 1, D)
     if initial_window is not None:
         _check_buffer("initial_window", initial_window, x.device, x.dtype, windows)
-    ws, ws_bytes = _workspace(workspace, lambda: conv_workspace_size(T, D, W), x)
+    ws, ws_bytes = None, 0  # only a caller's own tells of malformed offsets
+    if workspace is not None or N > 512:
+        ws, ws_bytes = _workspace(workspace, lambda: conv_workspace_size(T, D, W), x)
     y = _like("out", out, x)
     final = _output("final_out", final_out, windows, x.dtype, x) if output_final_window else None
     _call(di, lib.hagdn_conv_prefill, x.data_ptr(), xs, weight.data_ptr(), pb, _ptr(initial_window), cu, N, T, D, W,
-          dt, act, y.data_ptr(), _ptr(final), ws.data_ptr(), ws_bytes, _stream(di))
+          dt, act, y.data_ptr(), _ptr(final), _ptr(ws), ws_bytes, _stream(di))
     return y, final
 
 

@@ -49,7 +49,7 @@ def test_valid_calls_reach_the_workspace_check():
 
 @pytest.mark.parametrize("fn,d", [("hagdn_conv_prefill", CONV), ("hagdn_conv_backward", CONV_BACK)], ids=["prefill", "backward"])
 def test_conv_refusals(fn, d):
-    for over in (dict(N=0), dict(T=-1), dict(D=0), dict(act=1), dict(act=3), dict(x=None), dict(w=None), dict(ws=None),
+    for over in (dict(N=0), dict(T=-1), dict(D=0), dict(act=1), dict(act=3), dict(x=None), dict(w=None), dict(ws=None, N=513),
                  dict(ws=F[7] + 8), dict(cu=None), dict(cu=F[4] + 2), dict(xs=-1), dict(xs=1 << 31), dict(x=F[0] + 1),
                  dict(w=F[1] + 2), dict(w0=F[3] + 1)):
         assert call(fn, d, **{"wsb": BIG, **over})[0] == EINVAL, over

@@ -146,6 +146,25 @@ def test_widths_and_groups(D, G):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("D,G", [(256, 1), (300, 1), (520, 2)])
+@pytest.mark.parametrize("S", [17, 32, 33, 64])
+def test_many_states_in_wide_calls(S, D, G):
+    """Workgroups of four waves with more than 16 states, some of whose columns are missing."""
+    lens = (20, 0, 37, 1)
+    d = make(lens, D, S, G, "bf16", "f32", seed=D + S)
+    check(run(d, lens, True), expected(d, lens, True), "bf16", "f32", f"D={D} G={G} S={S}")
+
+
+@pytest.mark.gpu
+def test_many_sequences():
+    """More sequences than a workgroup checks alone, of no, one, two and five tokens."""
+    lens = tuple([1, 2, 0, 5] * 200)
+    for dtype, S in (("bf16", 16), ("f32", 20)):
+        d = make(lens, 40, S, 1, dtype, "f32", seed=S)
+        check(run(d, lens, True), expected(d, lens, True), dtype, "f32", f"{len(lens)} sequences S={S}")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("S,G", [(16, 1), (40, 2)])
 def test_long_sequences(S, G):
     """Many chunks to a run of the carry, channels that remember most of them."""
