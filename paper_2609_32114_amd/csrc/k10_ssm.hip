@@ -30,8 +30,13 @@ __global__ __launch_bounds__(W * 64, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_s
   const Column col(group, (team - group * teams) * W + uniform(threadIdx.x >> 6), a);
   const uint32_t c = col.c;
   if (OUT && chunk == 0) pass_states(a, ok, a.s0, a.s_final, col);
-  const int t0 = chunk * a.chunk, t1 = (int)min((long)t0 + a.chunk, (long)a.T);
+  int t0 = chunk * a.chunk;
+  const int t1 = (int)min((long)t0 + a.chunk, (long)a.T);
   if (!ok || t0 >= t1) return;
+  if (!OUT) {  // what a chunk leaves is its last sequence's
+    const Cursor last(cu, t1 - 1);
+    if (last.start > t0) t0 += (last.start - t0) / kSsmRows * kSsmRows;
+  }
 
   // x, dt, B and C of the first tokens are on their way before anything waits; z, which only
   // the outputs need, is read in its turn

@@ -35,7 +35,12 @@ __global__ __launch_bounds__(W * 64, NP == 16 ? 4 : NP == 32 ? 2 : 1) void ssm_b
   const Column col(group, (team - group * teams) * W + uniform(threadIdx.x >> 6), a);
   const uint32_t c = col.c;
   if (!ok) return;
-  const int t0 = chunk * a.chunk, t1 = (int)min((long)t0 + a.chunk, (long)a.T);
+  const int t0 = chunk * a.chunk;
+  int t1 = (int)min((long)t0 + a.chunk, (long)a.T);
+  {  // what a chunk passes back is its first sequence's
+    const Cursor first(cu, t0);
+    if (first.end < t1) t1 = min(t1, t0 + (first.end - t0 + kBackRows - 1) / kBackRows * kBackRows);
+  }
   float A[NP], e[NP];
   load_rates(a, c, A);
 #pragma unroll

@@ -21,20 +21,13 @@ __device__ __forceinline__ float silu(float v) { return v * logistic(v); }
 // one is |v| 2^-24 of the result.
 __device__ __forceinline__ float silu_slope(float v, float s) { return s * __builtin_fmaf(v, 1.f - s, 1.f); }
 
-// log(1 + e^v) = max(v, 0) + log1p(t), t = e^-|v|, with log1p(t) = 2 artanh(r), r = t / (2 + t)
-// in [0, 1/3]: r times a polynomial in r^2 through the degree 5 Chebyshev nodes of
-// [0, 1/9] (relative error 2^-33).  Every term is positive, so that small results, steps of
-// 1e-3 and less, keep their digits.
+// log(1 + e^v) = max(v, 0) + log1p(t), t = e^-|v|.  With w = 1 + t rounded, log1p(t) is log w and
+// what w lost of t (over w, which is one wherever that counts).  The hardware's logarithm keeps
+// its digits near one: at most 1.8 ulp, measured over every seventh t from 2^-30 to 1, so that
+// small results, steps of 1e-3 and less, keep theirs.
 __device__ __forceinline__ float softplus(float v) {
-  const float t = __builtin_amdgcn_exp2f(-__builtin_fabsf(v) * kLog2e);
-  const float r = t * __builtin_amdgcn_rcpf(2.f + t), q = r * r;
-  float p = 0.24393908f;
-  p = __builtin_fmaf(p, q, 0.21398561f);
-  p = __builtin_fmaf(p, q, 0.28620207f);
-  p = __builtin_fmaf(p, q, 0.39998711f);
-  p = __builtin_fmaf(p, q, 0.66666679f);
-  p = __builtin_fmaf(p, q, 2.f);
-  return __builtin_fmaf(r, p, __builtin_fmaxf(v, 0.f));  // (a NaN comes through r)
+  const float t = __builtin_amdgcn_exp2f(-__builtin_fabsf(v) * kLog2e), w = 1.f + t;
+  return __builtin_fmaf(__builtin_amdgcn_logf(w), 0.693147182f, t - (w - 1.f)) + __builtin_fmaxf(v, 0.f);  // (a NaN comes through t)
 }
 
 // V consecutive elements, aligned as one of them is.
