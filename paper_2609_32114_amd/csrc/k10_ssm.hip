@@ -218,9 +218,10 @@ hipError_t launch_ssm_forward(const SsmArgs &a, bool bf16, bool dt_bf16, hipStre
 }
 
 // ------------------------------------------------------------- single tokens
-// P states of a channel to a lane, S / P lanes (a power of two up to 16) to a channel; P = 0: a
-// lane goes over all of a channel's states.
-template <typename T, typename S, int P>
+// Four states of a channel to a lane, the power of two of lanes (up to 16) that covers S to a
+// channel, so that a wave's loads lie side by side. QUADS, where 4 divides S: a lane's four are
+// neighbours, in one load. Otherwise they stand a channel's lanes apart.
+template <typename T, typename S, bool QUADS>
 __global__ __launch_bounds__(256) void ssm_step_kernel(SsmStepArgs a, uint32_t lanes, uint32_t items) {
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < items; i += gridDim.x * 256) {  // N x D x S < 2^31
     const uint32_t part = i & (lanes - 1), row = i / lanes, n = row / (uint32_t)a.D, c = row - n * (uint32_t)a.D;
@@ -236,22 +237,37 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmStepArgs a, uint32_t l
       const T *B = static_cast<const T *>(a.B) + (size_t)n * a.Bs + g * a.S, *C = static_cast<const T *>(a.C) + (size_t)n * a.Cs + g * a.S;
       float *state = a.state + ((size_t)slot * a.D + c) * a.S;
       const float *A = a.A + (size_t)c * a.S;
-      if constexpr (P > 0) {
-        const uint32_t at = part * P;
-        auto s = load_pack<float, P>(state, at);
-        const auto r = load_pack<float, P>(A, at);
-        const auto b = load_pack<T, P>(B, at), w = load_pack<T, P>(C, at);
+      if (QUADS) {
+        const uint32_t at = part * 4;
+        if (at < (uint32_t)a.S) {
+          auto s = load_pack<float, 4>(state, at);
+          const auto r = load_pack<float, 4>(A, at);
+          const auto b = load_pack<T, 4>(B, at), w = load_pack<T, 4>(C, at);
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-          s.v[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(step * (r.v[k] * kLog2e)), s.v[k], in * Elt<T>::to_f32(b.v[k]));
-          y = __builtin_fmaf(Elt<T>::to_f32(w.v[k]), s.v[k], y);
+          for (int k = 0; k < 4; ++k) {
+            s.v[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(step * (r.v[k] * kLog2e)), s.v[k], in * Elt<T>::to_f32(b.v[k]));
+            y = __builtin_fmaf(Elt<T>::to_f32(w.v[k]), s.v[k], y);
+          }
+          store_pack<float, 4>(state, at, s);
         }
-        store_pack<float, P>(state, at, s);
       } else {
-        for (int k = 0; k < a.S; ++k) {
-          const float s = __builtin_fmaf(__builtin_amdgcn_exp2f(step * (A[k] * kLog2e)), state[k], in * Elt<T>::to_f32(B[k]));
-          y = __builtin_fmaf(Elt<T>::to_f32(C[k]), s, y);
-          state[k] = s;
+        float s[4], r[4], b[4], w[4];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {
+          const uint32_t at = part + k * lanes;
+          const bool in_range = at < (uint32_t)a.S;
+          s[k] = in_range ? state[at] : 0.f;
+          r[k] = in_range ? A[at] : 0.f;
+          b[k] = in_range ? Elt<T>::to_f32(B[at]) : 0.f;
+          w[k] = in_range ? Elt<T>::to_f32(C[at]) : 0.f;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {
+          const uint32_t at = part + k * lanes;
+          if (at >= (uint32_t)a.S) break;
+          s[k] = __builtin_fmaf(__builtin_amdgcn_exp2f(step * (r[k] * kLog2e)), s[k], in * b[k]);
+          y = __builtin_fmaf(w[k], s[k], y);
+          state[at] = s[k];
         }
       }
     }
@@ -267,12 +283,12 @@ __global__ __launch_bounds__(256) void ssm_step_kernel(SsmStepArgs a, uint32_t l
 }
 
 template <typename T, typename S> hipError_t ssm_step(const SsmStepArgs &a, hipStream_t s) {
-  const bool four = a.S % 4 == 0 && (a.S & (a.S - 1)) == 0;
-  const uint32_t lanes = four ? (uint32_t)a.S / 4 : 1;
+  uint32_t lanes = 1;
+  while (lanes * 4 < (uint32_t)a.S) lanes *= 2;
   const uint32_t items = (uint32_t)a.N * a.D * lanes, blocks = (items + 255) / 256;
   const dim3 grid(blocks < 1u << 20 ? blocks : 1u << 20);
-  if (four) hipLaunchKernelGGL((ssm_step_kernel<T, S, 4>), grid, dim3(256), 0, s, a, lanes, items);
-  else hipLaunchKernelGGL((ssm_step_kernel<T, S, 0>), grid, dim3(256), 0, s, a, lanes, items);
+  if (a.S % 4 == 0) hipLaunchKernelGGL((ssm_step_kernel<T, S, true>), grid, dim3(256), 0, s, a, lanes, items);
+  else hipLaunchKernelGGL((ssm_step_kernel<T, S, false>), grid, dim3(256), 0, s, a, lanes, items);
   return hipGetLastError();
 }
 hipError_t launch_ssm_step(const SsmStepArgs &a, bool bf16, bool dt_bf16, hipStream_t s) {

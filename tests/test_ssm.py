@@ -322,7 +322,9 @@ def test_no_value_of_another_sequence():
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype,step", TYPES, ids=lambda t: t)
 @pytest.mark.parametrize("N,D,S,G", [(1, 1, 16, 1), (1, 2048, 16, 1), (5, 67, 16, 1), (33, 260, 8, 2), (7, 65, 5, 1),
-                                     (3, 64, 64, 4), (2, 100, 32, 1), (64, 1280, 16, 1), (9, 130, 4, 1), (2, 5, 33, 1)])
+                                     (3, 64, 64, 4), (2, 100, 32, 1), (64, 1280, 16, 1), (9, 130, 4, 1), (2, 5, 33, 1),
+                                     (4, 70, 2, 1), (3, 66, 6, 2), (5, 65, 12, 1), (4, 130, 24, 2), (7, 97, 40, 1),
+                                     (6, 260, 61, 4), (1, 3, 1, 1)])
 def test_decode_against_oracle(N, D, S, G, dtype, step):
     """One token of each sequence from a shuffled pool; padding and idle slots are left alone."""
     import torch
