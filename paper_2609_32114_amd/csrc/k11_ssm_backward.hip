@@ -129,8 +129,17 @@ __device__ __forceinline__ float sum_lanes(float (&v)[16]) {
 
 // The LDS of NP padded states and W waves: the states at the starts of a group's runs of 8
 // tokens, the group's B and C, and a run's sums of dB and dC for each wave.
+//
+// Up to 32 states are gone over together, in code of up to 65 KB.  With 64 it would be 86 KB, more
+// than the instruction cache holds, and every run would fetch it anew (17401 x 2048 x 64: 6960 us):
+// there a loop takes blocks of 16, whose rates, gradients and sums are loaded and stored for each
+// run (3440 us).  The gradients that go on to earlier tokens lie in the place of the first run's
+// states, which the saved ones are; the sums of dA in their workspace.  With 32 states blocks of
+// 16 are slower (1470 us against 1330).
 template <int NP, int W> struct BackForm {
   static constexpr int kRuns = kSsmGroup / kBackRows;
+  static constexpr int kBlock = NP < 64 ? NP : 16;
+  static constexpr bool kWhole = kBlock == NP;
   static constexpr size_t kStates = (size_t)W * kRuns * NP * 64, kSums = (size_t)W * kBackRows * 2 * NP;
   static constexpr size_t kMaps = (size_t)kSsmGroup * 2 * NP;
   static constexpr size_t kLds = (kStates + kSums + kMaps) * sizeof(float);
@@ -161,11 +170,22 @@ __global__ __launch_bounds__(W * 64, NP <= 32 ? 2 : 1) void ssm_backward_kernel(
   if (chunk == 0) pass_states(a, ok, a.dfinal, a.ds0, col);
   const int t0 = chunk * a.chunk, t1 = ok ? (int)min((long)t0 + a.chunk, (long)a.T) : t0;
 
-  float A[NP], e[NP], dA[NP], dskip = 0.f, dbias = 0.f;
-  load_rates(a, c, A);
+  constexpr int NB = F::kBlock;
+  const int blocks_end = F::kWhole ? NP : states(a);
+  float A[NB], e[NB], dA[NB], dskip = 0.f, dbias = 0.f;
+  float *passed = starts;
+  const auto weights = [&] { return a.dweights + (size_t)chunk * (NP + 2) * a.D; };
+  bool fresh = true;  // no run has been gone over
+  if (F::kWhole) load_rates(a, c, A);
 #pragma unroll
-  for (int n = 0; n < NP; ++n) e[n] = dA[n] = 0.f;
-  if (ok && chunk + 1 < a.chunks) load_states(a.maps + (size_t)chunk * NP * a.D, a, c, e);
+  for (int n = 0; n < NB; ++n) e[n] = dA[n] = 0.f;
+  const bool later = ok && chunk + 1 < a.chunks;
+  if (F::kWhole && later) load_states(a.maps + (size_t)chunk * NP * a.D, a, c, e);
+  for (int b = 0; b < blocks_end && !F::kWhole; b += NB) {
+    if (later) load_states(a.maps + (size_t)chunk * NP * a.D, a, c, e, b);
+#pragma unroll
+    for (int n = 0; n < NB; ++n) passed[(b + n) * 64] = e[n];
+  }
   const float bias = a.raw && a.bias ? a.bias[c] : 0.f, skip = a.skip ? a.skip[c] : 0.f;
 
   // waves of the workgroup that have channels
@@ -174,47 +194,56 @@ __global__ __launch_bounds__(W * 64, NP <= 32 ? 2 : 1) void ssm_backward_kernel(
   for (int g0 = t0 + (t1 - 1 - t0) / kSsmGroup * kSsmGroup; t1 > t0 && g0 >= t0; g0 -= kSsmGroup) {
     const int g1 = min(g0 + kSsmGroup, t1), runs = (g1 - g0 + kBackRows - 1) / kBackRows;
     stage.fetch(a, group, g0, g1);
+    const auto saved = [&] { return a.ckpt + (size_t)(g0 / kSsmGroup) * NP * a.D; };
     {
-      float h[NP];
-      load_states(a.ckpt + (size_t)(g0 / kSsmGroup) * NP * a.D, a, c, h);
+      float h[NB];
+      load_states(saved(), a, c, h);
+      static_assert(F::kRuns == 2, "the second run's start is formed, the first one's saved");
       stage.put(maps);  // the last group's have been read: its runs end at a barrier
       __syncthreads();
-      Cursor q(cu, g0);
-      int first = q.start == g0 ? g0 : q.end;
-      for (int run = 0; run < runs && !col.idle; ++run) {
+      T x[kBackRows];
+      S dt[kBackRows];
+      float given[kBackRows], step[kBackRows];
+      for (int b = 0; b < blocks_end; b += NB) {
+        if (!F::kWhole) load_rates(a, c, A, b);
+        if (b) load_states(saved(), a, c, h, b);
+        Cursor q(cu, g0);
+        int first = q.start == g0 ? g0 : q.end;
+        for (int run = 0; run < runs && !col.idle; ++run) {
 #pragma unroll
-        for (int n = 0; n < NP; ++n) starts[(run * NP + n) * 64] = h[n];
-        if (run + 1 == runs) break;
-        const int base = g0 + run * kBackRows;
-        T x[kBackRows];
-        S dt[kBackRows];
-        load_tokens(a.x, a.xs, base, t1, c, x);
-        load_tokens(a.dt, a.dts, base, t1, c, dt);
-        float given[kBackRows], step[kBackRows];
-        step_sizes(a, dt, bias, given, step);
-        LdsRows rows(maps, run * kBackRows * 2 * NP);
-        for (int lo = 0; lo < kBackRows;) {
-          if (base + lo == first) {
-            if (first == q.end) q.next();
-            load_sequence<NP>(a.s0, q.seq, a, c, h);
-            first = q.end;
+          for (int n = 0; n < NB; ++n)
+            if (F::kWhole || run) starts[(run * NP + b + n) * 64] = h[n];
+          if (run + 1 == runs) break;
+          const int base = g0 + run * kBackRows;
+          if (F::kWhole || !b) {  // the first run, for all blocks
+            load_tokens(a.x, a.xs, base, t1, c, x);
+            load_tokens(a.dt, a.dts, base, t1, c, dt);
+            step_sizes(a, dt, bias, given, step);
           }
-          const int hi = min(kBackRows, first - base);
-#pragma unroll
-          for (int i = 0; i < kBackRows; ++i)
-            if (i >= lo && i < hi) {
-              rows.hold();
-              HAGDN_OPAQUE_VECTOR(step[i]);
-              const float in = step[i] * Elt<T>::to_f32(x[i]);
-#pragma unroll
-              for (int n = 0; n < NP; n += 4) {
-                const f32x4 B = rows.four(i * 2 * NP + n);
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  h[n + k] = __builtin_fmaf(in, B[k], __builtin_amdgcn_exp2f(step[i] * A[n + k]) * h[n + k]);
-              }
+          LdsRows rows(maps, run * kBackRows * 2 * NP + b);
+          for (int lo = 0; lo < kBackRows;) {
+            if (base + lo == first) {
+              if (first == q.end) q.next();
+              load_sequence<NB>(a.s0, q.seq, a, c, h, b);
+              first = q.end;
             }
-          lo = hi;
+            const int hi = min(kBackRows, first - base);
+#pragma unroll
+            for (int i = 0; i < kBackRows; ++i)
+              if (i >= lo && i < hi) {
+                rows.hold();
+                HAGDN_OPAQUE_VECTOR(step[i]);
+                const float in = step[i] * Elt<T>::to_f32(x[i]);
+#pragma unroll
+                for (int n = 0; n < NB; n += 4) {
+                  const f32x4 B = rows.four(i * 2 * NP + n);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k)
+                    h[n + k] = __builtin_fmaf(in, B[k], __builtin_amdgcn_exp2f(step[i] * A[n + k]) * h[n + k]);
+                }
+              }
+            lo = hi;
+          }
         }
       }
     }
@@ -253,73 +282,93 @@ __global__ __launch_bounds__(W * 64, NP <= 32 ? 2 : 1) void ssm_backward_kernel(
           w[i] = ds[i] = 0.f;
         }
         const Cursor at(cu, base);
+        for (int b = 0; b < blocks_end; b += NB) {
+          if (!F::kWhole) rows = LdsRows(maps, run * kBackRows * 2 * NP + b);
+          float first_run[NB];
+          if (!F::kWhole) {
+            load_rates(a, c, A, b);
+            if (!run) load_states(saved(), a, c, first_run, b);
+            if (!fresh) load_states(weights(), a, c, dA, b);
 #pragma unroll
-        for (int n0 = 0; n0 < NP; n0 += kSlice) {
-          float kept[kBackRows][kSlice], h[kSlice];  // kept: a_t h_{t-1}
-#pragma unroll
-          for (int k = 0; k < kSlice; ++k) h[k] = starts[(run * NP + n0 + k) * 64];
-          Cursor q = at;
-          int first = q.start == base ? base : q.end;
-          for (int lo = 0; lo < count;) {
-            if (base + lo == first) {
-              if (first == q.end) q.next();
-              load_sequence<kSlice>(a.s0, q.seq, a, c, h, n0);
-              first = q.end;
+            for (int n = 0; n < NB; ++n) {
+              e[n] = passed[(b + n) * 64];
+              if (fresh) dA[n] = 0.f;
             }
-            const int hi = min(count, first - base);
+          }
 #pragma unroll
-            for (int i = 0; i < kBackRows; ++i)
-              if (i >= lo && i < hi) {
-                rows.hold();
-                HAGDN_OPAQUE_VECTOR(step[i]);
-                const float in = step[i] * x[i];
+          for (int n0 = 0; n0 < NB; n0 += kSlice) {
+            float kept[kBackRows][kSlice], h[kSlice];  // kept: a_t h_{t-1}
 #pragma unroll
-                for (int n = 0; n < kSlice; n += 4) {
-                  const f32x4 B = rows.four(i * 2 * NP + n0 + n);
+            for (int k = 0; k < kSlice; ++k) h[k] = F::kWhole || run ? starts[(run * NP + b + n0 + k) * 64] : first_run[n0 + k];
+            Cursor q = at;
+            int first = q.start == base ? base : q.end;
+            for (int lo = 0; lo < count;) {
+              if (base + lo == first) {
+                if (first == q.end) q.next();
+                load_sequence<kSlice>(a.s0, q.seq, a, c, h, b + n0);
+                first = q.end;
+              }
+              const int hi = min(count, first - base);
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) {
-                    kept[i][n + k] = __builtin_amdgcn_exp2f(step[i] * A[n0 + n + k]) * h[n + k];
-                    h[n + k] = __builtin_fmaf(in, B[k], kept[i][n + k]);
+              for (int i = 0; i < kBackRows; ++i)
+                if (i >= lo && i < hi) {
+                  rows.hold();
+                  HAGDN_OPAQUE_VECTOR(step[i]);
+                  const float in = step[i] * x[i];
+#pragma unroll
+                  for (int n = 0; n < kSlice; n += 4) {
+                    const f32x4 B = rows.four(i * 2 * NP + n0 + n);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                      kept[i][n + k] = __builtin_amdgcn_exp2f(step[i] * A[n0 + n + k]) * h[n + k];
+                      h[n + k] = __builtin_fmaf(in, B[k], kept[i][n + k]);
+                    }
                   }
                 }
-              }
-            lo = hi;
-          }
-          const auto back = [&](int i) {
-            rows.hold();
-            HAGDN_OPAQUE_VECTOR(step[i]);
-            const float in = step[i] * x[i], fed = col.mine ? in : 0.f;
-            float terms[2 * kSlice];  // of dB and dC
-#pragma unroll
-            for (int m = 0; m < kSlice; m += 4) {
-              const f32x4 B = rows.four(i * 2 * NP + n0 + m), C = rows.four(i * 2 * NP + NP + n0 + m);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const int k = m + j, n = n0 + k;
-                const float hn = __builtin_fmaf(in, B[j], kept[i][k]), dh = __builtin_fmaf(C[j], d[i], e[n]);
-                y[i] = __builtin_fmaf(C[j], hn, y[i]);
-                w[i] = __builtin_fmaf(B[j], dh, w[i]);
-                terms[k] = dh * fed;
-                terms[kSlice + k] = d[i] * hn;
-                const float p = dh * kept[i][k];
-                ds[i] = __builtin_fmaf(A[n], p, ds[i]);
-                dA[n] = __builtin_fmaf(step[i], p, dA[n]);
-                e[n] = __builtin_amdgcn_exp2f(step[i] * A[n]) * dh;
-              }
+              lo = hi;
             }
-            my_sums[i * 2 * NP + n0] = sum_lanes(terms);  // (by all lanes that have the same one)
-          };
-          for (int hi = count; hi > 0;) {
-            if (base + hi == q.start) q.previous();
-            if (base + hi == q.end) load_sequence<kSlice>(a.dfinal, q.seq, a, c, e + n0, n0);
-            const int lo = max(0, q.start - base);
+            const auto back = [&](int i) {
+              rows.hold();
+              HAGDN_OPAQUE_VECTOR(step[i]);
+              const float in = step[i] * x[i], fed = col.mine ? in : 0.f;
+              float terms[2 * kSlice];  // of dB and dC
 #pragma unroll
-            for (int i = kBackRows - 1; i >= 0; --i)
-              if (i >= lo && i < hi) back(i);
-            if (base + lo == q.start) store_sequence<kSlice>(a.ds0, q.seq, a, col, e + n0, n0);
-            hi = lo;
+              for (int m = 0; m < kSlice; m += 4) {
+                const f32x4 B = rows.four(i * 2 * NP + n0 + m), C = rows.four(i * 2 * NP + NP + n0 + m);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const int k = m + j, n = n0 + k;
+                  const float hn = __builtin_fmaf(in, B[j], kept[i][k]), dh = __builtin_fmaf(C[j], d[i], e[n]);
+                  y[i] = __builtin_fmaf(C[j], hn, y[i]);
+                  w[i] = __builtin_fmaf(B[j], dh, w[i]);
+                  terms[k] = dh * fed;
+                  terms[kSlice + k] = d[i] * hn;
+                  const float p = dh * kept[i][k];
+                  ds[i] = __builtin_fmaf(A[n], p, ds[i]);
+                  dA[n] = __builtin_fmaf(step[i], p, dA[n]);
+                  e[n] = __builtin_amdgcn_exp2f(step[i] * A[n]) * dh;
+                }
+              }
+              my_sums[i * 2 * NP + b + n0] = sum_lanes(terms);  // (by all lanes that have the same one)
+            };
+            for (int hi = count; hi > 0;) {
+              if (base + hi == q.start) q.previous();
+              if (base + hi == q.end) load_sequence<kSlice>(a.dfinal, q.seq, a, c, e + n0, b + n0);
+              const int lo = max(0, q.start - base);
+#pragma unroll
+              for (int i = kBackRows - 1; i >= 0; --i)
+                if (i >= lo && i < hi) back(i);
+              if (base + lo == q.start) store_sequence<kSlice>(a.ds0, q.seq, a, col, e + n0, b + n0);
+              hi = lo;
+            }
+          }
+          if (!F::kWhole) {
+            store_states(weights(), a, col, dA, b);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) passed[(b + n) * 64] = e[n];
           }
         }
+        fresh = false;
         float dx[kBackRows], dv[kBackRows];
 #pragma unroll
         for (int i = 0; i < kBackRows; ++i) {
@@ -352,12 +401,9 @@ __global__ __launch_bounds__(W * 64, NP <= 32 ? 2 : 1) void ssm_backward_kernel(
     }
   }
   if (!col.mine) return;
-  float *out = a.dweights + (size_t)chunk * (NP + 2) * a.D + c;
-#pragma unroll
-  for (int n = 0; n < NP; ++n)
-    if (n < a.S) out[(size_t)n * a.D] = dA[n];
-  out[(size_t)NP * a.D] = dskip;
-  out[(size_t)(NP + 1) * a.D] = dbias;
+  for (int b = 0; b < blocks_end && (F::kWhole || fresh); b += NB) store_states(weights(), a, col, dA, b);
+  weights()[(size_t)NP * a.D + c] = dskip;
+  weights()[(size_t)(NP + 1) * a.D + c] = dbias;
 }
 
 // dB and dC from the teams' sums, in their order.

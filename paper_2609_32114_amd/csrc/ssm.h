@@ -104,21 +104,25 @@ template <int NP> __device__ __forceinline__ void load_row(const float *row, int
   for (int n = 0; n < NP; ++n) v[n] = n < count ? row[n] : 0.f;
 }
 
-// log2(e) A of a channel; states past S never decay and are never fed.
-template <int NP> __device__ __forceinline__ void load_rates(const SsmArgs &a, uint32_t c, float (&r)[NP]) {
-  load_row<NP>(a.A + (size_t)c * a.S, states(a), r);
+// log2(e) A of a channel, from the first-th state on; states past S never decay and are never fed.
+template <int NP> __device__ __forceinline__ void load_rates(const SsmArgs &a, uint32_t c, float (&r)[NP], int first = 0) {
+  load_row<NP>(a.A + (size_t)c * a.S + first, states(a) - first, r);
 #pragma unroll
   for (int n = 0; n < NP; ++n) r[n] *= kLog2e;
 }
-// Rows [NP][D] of states, at a channel.
-template <int NP> __device__ __forceinline__ void load_states(const float *rows, const SsmArgs &a, uint32_t c, float (&h)[NP]) {
-  const int count = states(a);
+// Rows of states [padded][D], at a channel, from the first-th on.
+template <int NP>
+__device__ __forceinline__ void load_states(const float *rows, const SsmArgs &a, uint32_t c, float (&h)[NP], int first = 0) {
+  const int count = states(a) - first;
+  rows += (size_t)first * a.D;
 #pragma unroll
   for (int n = 0; n < NP; ++n) h[n] = n < count ? rows[(size_t)n * a.D + c] : 0.f;
 }
-template <int NP> __device__ __forceinline__ void store_states(float *rows, const SsmArgs &a, const Column &col, const float (&h)[NP]) {
-  const int count = states(a);
+template <int NP>
+__device__ __forceinline__ void store_states(float *rows, const SsmArgs &a, const Column &col, const float (&h)[NP], int first = 0) {
+  const int count = states(a) - first;
   if (!col.mine) return;
+  rows += (size_t)first * a.D;
 #pragma unroll
   for (int n = 0; n < NP; ++n)
     if (n < count) rows[(size_t)n * a.D + col.c] = h[n];
