@@ -4,12 +4,12 @@
 // Bound by its arithmetic: per token, channel and state a product, an exponential (8 cycles
 // of a wave, the others 4) and three or, for outputs, four more operations, and both passes over
 // the chunks take them.  32768 tokens x 2048 channels x 16 states, x, z, y and dt in bf16: what
-// chunks leave 211 to 230 us, what enters them 10, outputs 279 to 300 (the clock falls under
+// chunks leave 204 to 224 us, what enters them 10, outputs 266 to 289 (the clock falls under
 // this load from 2.4 to 2.2 GHz), where 539 MB would take 104 us of HBM.  The vector units are
-// busy 85 % of the time; 22 of 86 instructions a token and lane are the step size's softplus
-// and conversions, in outputs 30 of 110.  On the way (both passes): B and C through scalar loads
+// busy 90 % of the time; 18 of 82 instructions a token and lane are the step size's softplus
+// and conversions, in outputs 29 of 109.  On the way (both passes): B and C through scalar loads
 // and each sequence's end inside an unrolled loop 697 us; B and C through LDS, ends apart 573;
-// the next rows on their way, no copies around the states 510.
+// the next rows on their way, no copies around the states 535; the hardware's logarithm 520.
 #include "ssm.h"
 
 namespace hagdn {
@@ -220,7 +220,9 @@ hipError_t launch_ssm_forward(const SsmArgs &a, bool bf16, bool dt_bf16, hipStre
 // ------------------------------------------------------------- single tokens
 // Four states of a channel to a lane, the power of two of lanes (up to 16) that covers S to a
 // channel, so that a wave's loads lie side by side. QUADS, where 4 divides S: a lane's four are
-// neighbours, in one load. Otherwise they stand a channel's lanes apart.
+// neighbours, in one load. Otherwise they stand a channel's lanes apart (168 x 1280 channels x 61
+// states 37 us, 2.9 TB/s of states; with a channel's states in one lane, apart in memory, 197).
+// 256 x 4096 x 16 in bf16: 31 us, 4.3 TB/s of states.
 template <typename T, typename S, bool QUADS>
 __global__ __launch_bounds__(256) void ssm_step_kernel(SsmStepArgs a, uint32_t lanes, uint32_t items) {
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < items; i += gridDim.x * 256) {  // N x D x S < 2^31

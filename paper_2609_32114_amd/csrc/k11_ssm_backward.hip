@@ -6,10 +6,10 @@
 //   dx_t = dt_t w_t + skip dy_t,  d(dt_t) = x_t w_t + sum_n A dh_t a_t h_{t-1},
 //   dA = sum_t dt_t dh_t a_t h_{t-1}.
 //
-// Bound by its arithmetic, as the forward pass: some 29 instructions per token, channel and
+// Bound by its arithmetic, as the forward pass: some 28 instructions per token, channel and
 // state in the main kernel, of which 4.4 are the sums of dB and dC over lanes and 8 form the
 // states again.  17401 x 2048 x 16 in bf16, packed from eight sequences: what chunks pass back
-// 149 us, what reaches them 8, the main kernel 676, sums 16.  The vector units are busy 3/4 of
+// 144 us, what reaches them 8, the main kernel 645 to 666, sums 16.  The vector units are busy 3/4 of
 // the time: two waves a SIMD, 232 registers each.  On the way: states formed again over 64
 // tokens from scalar rows 1665 us; through LDS, 8 states at a time 1020; chunks that fill every
 // CU alike 760; states saved every 16 tokens instead of 32 720 (every 8: 660, for twice the

@@ -5,8 +5,8 @@ layer_ref.py.
 The reckoning, made before the kernels ran.  One fp32 rounding costs half of EPS = 2^-23
 relative.  A logistic function is off by (|v| + 5) EPS relative (the exponent's product,
 an ulp each of exponential and reciprocal), its product or slope by 3 EPS more.  A step
-size log(1 + e^v) is off by (2 |v| + 8) EPS relative: v's own sum, the exponential, a quotient
-and a polynomial of six terms.  A decay e^(dt A) takes |dt A| times its exponent's error; where
+size log(1 + e^v) is off by (2 |v| + 8) EPS relative: v's own sum, the exponential, the
+logarithm (an ulp) with its product, what rounding 1 + e^v loses, added back, and the sum.  A decay e^(dt A) takes |dt A| times its exponent's error; where
 chunks of at most 520 tokens are folded, the exponent is a sum of so many step sizes, 260
 EPS more.  An error travels the way its value does, so its bound obeys the value's own
 recurrence over magnitudes; regrouping a recurrence into chunks at most doubles it.  A sum of n
