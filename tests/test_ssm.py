@@ -259,10 +259,11 @@ def test_extreme_steps():
 
 
 @pytest.mark.gpu
-def test_no_tokens():
+@pytest.mark.parametrize("S", [16, 40])
+def test_no_tokens(S):
     import torch
     import paper_2609_32114_amd as P
-    D, S = 70, 16
+    D = 70
     A, s0 = -torch.rand(D, S, device="cuda"), torch.randn(2, D, S, device="cuda")
     x, B, cu = torch.empty(0, D, device="cuda"), torch.empty(0, S, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
     y, final, saved = P.ssm_prefill(x, x, A, B, B, initial_state=s0, cu_seqlens=cu, output_checkpoints=True)
@@ -274,14 +275,15 @@ def test_no_tokens():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("bad", [[0, 5, 3, 200], [1, 5, 9, 200], [0, 5, 9, 199], [0, 300, 9, 200], [-4, 5, 9, 200]])
-def test_malformed_offsets(bad):
+@pytest.mark.parametrize("S", [16, 40])
+def test_malformed_offsets(bad, S):
     """No token is processed, states pass through, the status says so."""
     import torch
     import paper_2609_32114_amd as P
-    d = make((5, 4, 191), 68, 16, seed=2)
+    d = make((5, 4, 191), 68, S, seed=2)
     t = {k: None if v is None else v.cuda() for k, v in d.items()}
     cu = torch.tensor(bad, dtype=torch.int32, device="cuda")
-    ws = torch.zeros(P.ssm_workspace_size(200, 68, 16, 1, True), dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(P.ssm_workspace_size(200, 68, S, 1, True), dtype=torch.uint8, device="cuda")
     out = torch.full((200, 68), 7.0, dtype=torch.bfloat16, device="cuda")
     args = (t["x"], t["dt"], t["A"], t["B"], t["C"])
     how = dict(skip=t["skip"], z=t["z"], dt_bias=t["bias"], initial_state=t["s0"], cu_seqlens=cu, workspace=ws,
@@ -296,12 +298,13 @@ def test_malformed_offsets(bad):
 
 
 @pytest.mark.gpu
-def test_no_value_of_another_sequence():
+@pytest.mark.parametrize("S", [16, 40])
+def test_no_value_of_another_sequence(S):
     """A sequence's results are the same beside neighbours of NaN and infinities, in its wave and
     in the chunks around it."""
     import torch
     lens = (45, 60, 70)
-    d = make(lens, 66, 16, 1, "f32", "f32", seed=4)
+    d = make(lens, 66, S, 1, "f32", "f32", seed=4)
     clean = run(d, lens, True)
     mid = slice(45, 105)
     for v in (float("nan"), float("inf")):
@@ -374,9 +377,10 @@ def test_decode_continues_prefill():
 
 
 @pytest.mark.gpu
-def test_repeats_bit_for_bit():
+@pytest.mark.parametrize("S", [16, 40])
+def test_repeats_bit_for_bit(S):
     import torch
     lens = (700, 3, 900)
-    d = make(lens, 520, 16, seed=6)
+    d = make(lens, 520, S, seed=6)
     a, b = run(d, lens, True), run(d, lens, True)
     assert all(torch.equal(a[k], b[k]) for k in a)
