@@ -238,7 +238,7 @@ __global__ __launch_bounds__(1024) void pool_fork_plan_kernel(PoolPlanArgs a) {
     const int i = base + t, s = i < a.M ? source(i) : -1;
     const bool moved = s >= 0 && a.mark[s] != i;
     const int k = moves + prefix(moved, sWaves, total);
-    if (moved) a.moves[2 + 2 * k] = s;
+    if (moved && k < a.num_slots) a.moves[2 + 2 * k] = s;  // more than the slots are counted, not carried out
     moves += total;
   }
   int free_slots = 0;

@@ -4,6 +4,8 @@ row at a time on the host."""
 import numpy as np
 import pytest
 
+from gpu_harness import say
+
 # rows of every alignment: (type, shape of a row)
 ROWS = [("float32", (16, 33)), ("bfloat16", (3, 70)), ("float32", (7,)), ("bfloat16", (1,)), ("uint8", (5,)),
         ("float32", (2, 64, 64)), ("int64", (3,)), ("uint8", (4099,))]
@@ -254,6 +256,38 @@ def test_beam_search_over_states():
     table_after = P.pool_compact([windows, states], new)
     assert sorted(table_after.tolist()) == [0, 1, 2, 3]
     assert torch.equal(states[table_after.long()], apart[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,M,S", [(40, 4096, 4096), (3, 4097, 4096), (3000, 4096, 4097), (3000, 4500, 6000), (1, 5000, 100),
+                                   (100, 5000, 100), (200, 4097, 1), (2000, 9000, 5000)])
+def test_fork_of_thousands(N, M, S):
+    """Plans in LDS and in memory, with enough free slots and with far fewer than children; nothing
+    around the workspace and the new table is written."""
+    import torch
+    import paper_2609_32114_amd as P
+    r = np.random.default_rng(M + S)
+    rows = [("float32", (2,)), ("uint8", (5,))]
+    size = P.pool_workspace_size(S)
+    for i in range(3):
+        pools = make(S, rows, seed=i)
+        before = [raw(p) for p in pools]
+        slots = r.permutation(max(S, N))[:N].tolist()
+        parents = r.integers(0, N, M).tolist() if i else [0] * M
+        if i == 2:
+            parents = [p if r.random() > 0.2 else int(r.choice([-1, N])) for p in parents]
+            slots = [s if r.random() > 0.2 else -1 for s in slots]
+        new, moves, missing = forked(slots, parents, S)
+        around = torch.full((size + 131072,), 9, dtype=torch.uint8, device="cuda")
+        tables = torch.full((M + 4096,), 9, dtype=torch.int32, device="cuda")
+        ws, out = around[65536:65536 + size], tables[2048:2048 + M]
+        say(f"fork of {N} sequences into {M} children, {S} slots, form {i}")
+        got = P.pool_fork(pools, table(slots), table(parents), workspace=ws, out=out)
+        assert got.tolist() == new
+        assert P.device_status(ws) == (P.DEV_POOL_FULL if missing else P.DEV_OK)
+        same(pools, copied(before, [d for d, _ in moves], [s for _, s in moves]))
+        for guard in (around[:65536], around[65536 + size:], tables[:2048], tables[2048 + M:]):
+            assert bool((guard == 9).all())
 
 
 def test_rules_on_the_host():
