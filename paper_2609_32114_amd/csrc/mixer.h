@@ -59,7 +59,7 @@ hipError_t launch_check_offsets(const int32_t *cu, int N, int T, int *status, hi
 inline int conv_run(int T, int D, int cus) {
   const long cols = ((long)D + 255) / 256, waves = 16l * (cus > 0 ? cus : 256);
   const long run = ((long)T * cols + waves - 1) / waves;
-  return (int)(run < 16 ? 16 : run);
+  return (int)(run < 16 ? 16 : run < T || T < 16 ? run : T);  // (a run of all tokens may pass 31 bits)
 }
 // The forward pass's: two waves a SIMD, but runs long enough beside the rows that they
 // read a second time.

@@ -4,6 +4,8 @@ never-dereferenced device pointers)."""
 
 import ctypes
 import os
+import subprocess
+import sys
 
 import pytest
 
@@ -121,6 +123,26 @@ def test_workspace_sizes():
                 lambda: P.pool_workspace_size((1 << 20) + 1)):
         with pytest.raises(P.HagdnError):
             bad()
+
+
+def test_conv_workspace_sizes_of_the_largest_calls():
+    """Every size in the documented ranges gives a workspace's bytes or none, and the process goes on
+    (in one of its own: a quotient by zero would end it)."""
+    code = """
+import paper_2609_32114_amd as P
+lib = P.load_library()
+MOST = 0x7fff0000
+for T in (1 << 24, 1 << 30, 1 << 30 | 12345, MOST):
+    for D in (1, 4096, 1 << 20, 1 << 28):
+        for W in (2, 8):
+            n = lib.hagdn_conv_workspace_size(T, D, W, 1)
+            # a run's sums at least; at most one for every 16 tokens
+            assert 256 + (W + 1) * D * 4 <= n <= 256 + ((T + 15) // 16) * (W + 1) * D * 4, (T, D, W, n)
+print("sizes passed")
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120,
+                       cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert r.returncode == 0 and "sizes passed" in r.stdout, (r.returncode, r.stdout + r.stderr)
 
 
 # ------------------------------------------------------------------------- pools
