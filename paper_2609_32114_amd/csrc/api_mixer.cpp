@@ -140,6 +140,7 @@ int check_ssm(int T, int D, int S, int G, int dtype, int dt_dtype, int pre) {
 struct SsmPlan {
   int chunk, chunks;
   size_t maps, sums, resets, dbc, dweights, bytes;
+  bool fits;  // below 2^62 bytes: what stands above is not wrapped
 };
 SsmPlan ssm_plan(int T, int D, int S, int G, bool backward) {
   SsmPlan p = {};
@@ -148,20 +149,27 @@ SsmPlan ssm_plan(int T, int D, int S, int G, bool backward) {
   p.chunks = T > 0 ? (T - 1) / p.chunk + 1 : 1;
   const size_t between = p.chunks > 1 ? p.chunks : 0;  // one chunk leaves nothing to another
   size_t at = hagdn::kMixerHeader;
-  const auto take = [&](size_t n) {
+  p.fits = true;
+  const auto take = [&](size_t rows, size_t cols) {  // fp32 values
+    size_t n;
     const size_t here = at;
-    at += pad256(n);
+    p.fits = p.fits && !__builtin_mul_overflow(rows, cols * 4, &n) && n < (size_t)1 << 62;
+    if (p.fits) at += pad256(n);
+    p.fits = p.fits && at < (size_t)1 << 62;
     return here;
   };
-  p.maps = take(between * np * D * 4);
-  p.sums = take(between * D * 4);
-  p.resets = take(between * 4);
+  p.maps = take(between, np * D);
+  p.sums = take(between, D);
+  p.resets = take(between, 1);
   if (backward) {
-    p.dbc = take((size_t)hagdn::ssm_teams(D, G) * T * G * 2 * np * 4);
-    p.dweights = take((size_t)p.chunks * (np + 2) * D * 4);
+    p.dbc = take((size_t)hagdn::ssm_teams(D, G) * T, 2 * np * G);
+    p.dweights = take(p.chunks, (np + 2) * D);
   }
   p.bytes = at;
   return p;
+}
+int check_fits(const SsmPlan &p, int T, int D, int S, int G) {
+  return p.fits ? HAGDN_OK : fail(HAGDN_EINVAL, "sizes too large for a workspace (%d x %d x %d, %d groups)", T, D, S, G);
 }
 
 int check_ssm_call(const int32_t *cu, int N, int T, int D, int S, int G, int dtype, int dt_dtype, int pre,
@@ -171,6 +179,7 @@ int check_ssm_call(const int32_t *cu, int N, int T, int D, int S, int G, int dty
   if ((size_t)N * (size_t)D * (size_t)S >= 0x7fffffffu) return fail(HAGDN_EINVAL, "N x D x S too large (%d x %d x %d)", N, D, S);
   if (dt_bias && !pre) return fail(HAGDN_EINVAL, "dt_bias needs HAGDN_PRE_GATE_SOFTPLUS");
   *plan = ssm_plan(T, D, S, G, backward);
+  if (int rc = check_fits(*plan, T, D, S, G)) return rc;
   return check_workspace(ws, ws_bytes, plan->bytes);
 }
 
@@ -375,7 +384,8 @@ int hagdn_conv_decode(const void *x, int64_t x_stride, const float *weight, cons
 
 size_t ssm_workspace_size(int T_total, int D, int S, int G, int backward) {
   if (check_ssm(T_total, D, S, G, HAGDN_F32, HAGDN_F32, 0) != HAGDN_OK) return 0;
-  return ssm_plan(T_total, D, S, G, backward != 0).bytes;
+  const SsmPlan p = ssm_plan(T_total, D, S, G, backward != 0);
+  return check_fits(p, T_total, D, S, G) == HAGDN_OK ? p.bytes : 0;
 }
 
 size_t ssm_checkpoints_size(int T_total, int D, int S) {

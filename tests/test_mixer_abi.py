@@ -145,6 +145,20 @@ print("sizes passed")
     assert r.returncode == 0 and "sizes passed" in r.stdout, (r.returncode, r.stdout + r.stderr)
 
 
+def test_ssm_workspace_sizes_of_the_largest_calls():
+    """A size that does not fit is none, with its message, and a call of it is turned down, not taken
+    for a smaller one."""
+    lib = P.load_library()
+    for T in (1, 1 << 24, 1 << 30, 0x7fff0000):
+        for D in (1, 4096, 1 << 20, 1 << 28):
+            for S, G in ((1, 1), (16, 1), (64, 1), (1, D), (64, D)):
+                n = lib.ssm_workspace_size(T, D, S, G, 1)
+                least = T * G * 2 * S * 4  # the sums of dB and dC alone
+                assert n >= least if least < 1 << 58 else n == 0 if least >= 1 << 62 else True, (T, D, S, G, n)
+                assert n or "too large" in lib.hagdn_last_error().decode(), (T, D, S, G)
+    assert call("ssm_backward", SSM_BACK, wsb=BIG, N=1, T=1 << 30, D=1 << 24, S=64, G=1 << 24)[0] == EINVAL
+
+
 # ------------------------------------------------------------------------- pools
 def arrays(pools, sizes):
     n = len(pools)
