@@ -248,6 +248,10 @@ int check_ranges(void *const *pools, const void *const *sources, const size_t *r
   Range r[2 * hagdn::kMaxPools];
   int n = 0;
   for (int p = 0; p < num_pools; ++p) {
+    size_t bytes;
+    const int most = sources && src_rows > dst_rows ? src_rows : dst_rows;
+    if (__builtin_mul_overflow(row_bytes[p], (size_t)most, &bytes) || bytes >> 62)
+      return fail(HAGDN_EINVAL, "pools[%d] too large (%d rows of %zu bytes)", p, most, row_bytes[p]);
     r[n++] = {(uintptr_t)pools[p], row_bytes[p] * (size_t)dst_rows, p, false};
     if (sources) r[n++] = {(uintptr_t)sources[p], row_bytes[p] * (size_t)src_rows, p, true};
   }

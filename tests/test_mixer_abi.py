@@ -207,3 +207,13 @@ def test_pool_plan_refusals():
     for over in (dict(parents=None), dict(M=-1), dict(out=F[1]), dict(out=F[2])):
         assert fork(**over) == EINVAL, over
     assert fork(M=(1 << 20) + 1) == EUNSUP and compact(N=(1 << 20) + 1) == EUNSUP
+
+
+def test_pools_of_more_bytes_than_there_are_addresses():
+    """Rows whose bytes do not fit are turned down, and not taken for few."""
+    lib = P.load_library()
+    assert copy([F[0]], [1 << 39], rows=1 << 25, n=0) == EINVAL and "too large" in lib.hagdn_last_error().decode()
+    assert copy([F[0], F[0] + 64], [1 << 39, 64], rows=1 << 25, n=0) == EINVAL
+    assert copy([F[0]], [1 << 39], sources=[F[1]], rows=1, src_rows=1 << 25, n=0) == EINVAL
+    p, s = arrays([F[0]], [(1 << 40) - 256])
+    assert lib.hagdn_pool_compact(p, s, 1, F[1], 3, 1 << 20, F[3], F[4], 100, None) == EWS  # 2^60 bytes do
