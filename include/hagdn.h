@@ -336,8 +336,9 @@ int hagdn_gate_norm_backward(const void *dy, int64_t dy_stride, const void *o,
  *   2^31 - 2^16;
  *   windows [N, W - 1, D] dtype, oldest input first; w0 NULL: zeros;
  *   activation HAGDN_ACT_SILU or HAGDN_ACT_NONE.
- * Sums are fp32.  Outputs must not overlap inputs (w_final not even w0 exactly: other
- * workgroups read that window while one writes it).  Results repeat bit for bit. */
+ * Sums are fp32.  Outputs and workspace must not overlap inputs or each other (w_final not even
+ * w0 exactly: other workgroups read that window while one writes it).  Results repeat bit for
+ * bit. */
 
 /* Bytes of workspace (0 on invalid sizes); backward 1: of hagdn_conv_backward. */
 size_t hagdn_conv_workspace_size(int T_total, int D, int W, int backward);
@@ -380,9 +381,10 @@ int hagdn_conv_decode(const void *x, int64_t x_stride, const float *weight, cons
  *   A [D, S], skip [D] (or NULL) fp32;  S = 1 .. 64;  D % G == 0;
  *   states [N, D, S] fp32; s0 NULL: zero.
  * dt A <= 0 is expected: where some 500 tokens together let a state grow by e^88
- * results are unspecified.  N x D x S below 2^31, T_total up to 2^31 - 2^16.  Sums and states are fp32.  Outputs must
- * not overlap inputs (s_final not even s0 exactly, nor ds0 dfinal).  Results repeat bit
- * for bit on one device.  No value of one sequence reaches another. */
+ * results are unspecified.  N x D x S below 2^31, T_total up to 2^31 - 2^16.  Sums and states
+ * are fp32.  Outputs and workspace must not overlap inputs or each other (s_final not even s0
+ * exactly, nor ds0 dfinal).  Results repeat bit for bit on one device.  No value of one sequence
+ * reaches another. */
 
 /* Bytes of workspace (0 on invalid sizes); backward 1: of ssm_backward. */
 size_t ssm_workspace_size(int T_total, int D, int S, int G, int backward);
@@ -446,7 +448,7 @@ int hagdn_pool_copy(void *const *pools, const void *const *sources, const size_t
  * name: the children must be all that the pools hold.  new_slots [M] receives the
  * children's slots, -1 for a parent outside [0, N) or in no slot of the pools, and for
  * children beyond the free slots (hagdn_device_status: HAGDN_DEV_POOL_FULL).  new_slots
- * must not overlap slots or parents.
+ * must not overlap slots or parents; tables and workspace overlap neither pools nor each other.
  * Rows that are free afterwards keep what they held. */
 size_t hagdn_pool_workspace_size(int num_slots);
 int hagdn_pool_fork(void *const *pools, const size_t *row_bytes, int num_pools,
@@ -456,7 +458,8 @@ int hagdn_pool_fork(void *const *pools, const size_t *row_bytes, int num_pools,
 /* The states that the table slots [N] names move to the front of the pools: with L live
  * slots, those from L on move, in order, to the free ones below L.  new_slots [N] (it may be
  * slots itself) receives the table after it; entries outside the pools (padding, ended
- * sequences) stay as they are.  Entries that name one slot still name one. */
+ * sequences) stay as they are.  Entries that name one slot still name one.  Tables and workspace
+ * overlap no pool. */
 int hagdn_pool_compact(void *const *pools, const size_t *row_bytes, int num_pools,
                        const int32_t *slots, int N, int num_slots, int32_t *new_slots,
                        void *workspace, size_t workspace_bytes, void *stream);

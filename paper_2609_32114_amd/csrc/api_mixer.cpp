@@ -44,7 +44,7 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
   const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
   return p && q && na && nb && (p >= q ? p - q < nb : q - p < na);
 }
-// Outputs against inputs and each other.
+// Outputs (the workspace among them) against inputs and each other.
 template <size_t NO, size_t NI> int check_overlaps(const Buf (&outs)[NO], const Buf (&ins)[NI]) {
   for (size_t i = 0; i < NO; ++i) {
     for (const Buf &b : ins)
@@ -288,6 +288,23 @@ int check_plan(void *const *pools, const size_t *row_bytes, int num_pools, int n
   return check_workspace(ws, ws_bytes, plan_bytes(num_slots));
 }
 
+// A plan's tables (in entries of 4 bytes) and workspace against the pools, and the workspace against
+// the tables.
+template <size_t N>
+int check_plan_overlaps(void *const *pools, const size_t *row_bytes, int num_pools, int num_slots, const Buf (&tables)[N],
+                        const void *ws) {
+  const size_t need = plan_bytes(num_slots);
+  for (int p = 0; p < num_pools; ++p) {
+    const size_t bytes = row_bytes[p] * (size_t)num_slots;
+    for (const Buf &t : tables)
+      if (overlap(t.p, t.bytes, pools[p], bytes)) return fail(HAGDN_EINVAL, "%s overlaps pools[%d]", t.name, p);
+    if (overlap(ws, need, pools[p], bytes)) return fail(HAGDN_EINVAL, "workspace overlaps pools[%d]", p);
+  }
+  for (const Buf &t : tables)
+    if (overlap(ws, need, t.p, t.bytes)) return fail(HAGDN_EINVAL, "workspace overlaps %s", t.name);
+  return HAGDN_OK;
+}
+
 hagdn::PoolPlanArgs plan_args(const int32_t *slots, int N, int num_slots, int32_t *out, void *ws) {
   hagdn::PoolPlanArgs a = {};
   a.slots = slots; a.N = N; a.num_slots = num_slots; a.out = out;
@@ -320,7 +337,8 @@ int hagdn_conv_prefill(const void *x, int64_t x_stride, const float *weight, con
   const Buf ins[] = {{x, "x", tok, e, extent(T_total, x_stride, D, dtype)}, {w0, "w0", false, e, windows},
                      {weight, "weight", true, 4, (size_t)D * W * 4}, {bias, "bias", false, 4, (size_t)D * 4},
                      {cu_seqlens, "cu_seqlens", false, 4, ((size_t)N + 1) * 4}};
-  const Buf outs[] = {{y, "y", tok, e, extent(T_total, D, D, dtype)}, {w_final, "w_final", false, e, windows}};
+  const Buf outs[] = {{y, "y", tok, e, extent(T_total, D, D, dtype)}, {w_final, "w_final", false, e, windows},
+                      {workspace, "workspace", false, 16, conv_bytes(T_total, D, W, false)}};
   if (int rc = check_buffers(ins)) return rc;
   if (int rc = check_buffers(outs)) return rc;
   if (int rc = check_overlaps(outs, ins)) return rc;
@@ -347,7 +365,8 @@ int hagdn_conv_backward(const void *dy, int64_t dy_stride, const void *x, int64_
                      {weight, "weight", true, 4, (size_t)D * W * 4}, {bias, "bias", false, 4, (size_t)D * 4},
                      {cu_seqlens, "cu_seqlens", false, 4, ((size_t)N + 1) * 4}};
   const Buf outs[] = {{dx, "dx", tok, e, extent(T_total, D, D, dtype)}, {dweight, "dweight", true, 4, (size_t)D * W * 4},
-                      {dbias, "dbias", bias != nullptr, 4, (size_t)D * 4}, {dw0, "dw0", false, e, windows}};
+                      {dbias, "dbias", bias != nullptr, 4, (size_t)D * 4}, {dw0, "dw0", false, e, windows},
+                      {workspace, "workspace", true, 16, conv_bytes(T_total, D, W, true)}};
   if (int rc = check_buffers(ins)) return rc;
   if (int rc = check_buffers(outs)) return rc;
   if (int rc = check_overlaps(outs, ins)) return rc;
@@ -423,7 +442,8 @@ int ssm_prefill(const void *x, int64_t x_stride, const void *dt, int64_t dt_stri
                      {cu_seqlens, "cu_seqlens", false, 4, ((size_t)N + 1) * 4}};
   const Buf outs[] = {{y, "y", tok, e, extent(T_total, D, D, dtype)},
                       {s_final, "s_final", false, 4, states},
-                      {checkpoints, "checkpoints", false, 4, ssm_checkpoints_size(T_total, D, S) * 4}};
+                      {checkpoints, "checkpoints", false, 4, ssm_checkpoints_size(T_total, D, S) * 4},
+                      {workspace, "workspace", true, 16, plan.bytes}};
   if (int rc = check_buffers(ins)) return rc;
   if (int rc = check_buffers(outs)) return rc;
   if (int rc = check_overlaps(outs, ins)) return rc;
@@ -473,7 +493,8 @@ int ssm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_str
                       {dskip, "dskip", skip != nullptr, 4, (size_t)D * 4},
                       {dz, "dz", tok && z != nullptr, e, rows},
                       {d_dt_bias, "d_dt_bias", dt_bias != nullptr, 4, (size_t)D * 4},
-                      {ds0, "ds0", false, 4, states}};
+                      {ds0, "ds0", false, 4, states},
+                      {workspace, "workspace", true, 16, plan.bytes}};
   if (int rc = check_buffers(ins)) return rc;
   if (int rc = check_buffers(outs)) return rc;
   if (int rc = check_overlaps(outs, ins)) return rc;
@@ -565,6 +586,8 @@ int hagdn_pool_fork(void *const *pools, const size_t *row_bytes, int num_pools, 
   if (int rc = check_buffers(ins)) return rc;
   if (int rc = check_buffers(outs)) return rc;
   if (int rc = check_overlaps(outs, ins)) return rc;
+  const Buf tables[] = {ins[0], ins[1], outs[0]};
+  if (int rc = check_plan_overlaps(pools, row_bytes, num_pools, num_slots, tables, workspace)) return rc;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   hagdn::PoolPlanArgs plan = plan_args(slots, N, num_slots, new_slots, workspace);
   plan.parents = parents;
@@ -582,10 +605,11 @@ int hagdn_pool_compact(void *const *pools, const size_t *row_bytes, int num_pool
   if (int rc = check_plan(pools, row_bytes, num_pools, num_slots, workspace, workspace_bytes)) return rc;
   if (N < 0) return fail(HAGDN_EINVAL, "N must be >= 0 (got %d)", N);
   if (N > hagdn::kMaxPoolSlots) return fail(HAGDN_EUNSUPPORTED, "N > %d unsupported (got %d)", hagdn::kMaxPoolSlots, N);
-  const Buf tables[] = {{slots, "slots", N > 0, 4, 0}, {new_slots, "new_slots", N > 0, 4, 0}};
+  const Buf tables[] = {{slots, "slots", N > 0, 4, (size_t)N * 4}, {new_slots, "new_slots", N > 0, 4, (size_t)N * 4}};
   if (int rc = check_buffers(tables)) return rc;
   if (new_slots != slots && overlap(new_slots, (size_t)N * 4, slots, (size_t)N * 4))
     return fail(HAGDN_EINVAL, "new_slots overlaps slots partly");
+  if (int rc = check_plan_overlaps(pools, row_bytes, num_pools, num_slots, tables, workspace)) return rc;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const hagdn::PoolPlanArgs plan = plan_args(slots, N, num_slots, new_slots, workspace);
   if (hipError_t e = hagdn::launch_pool_compact_plan(plan, s)) return done(e);

@@ -217,3 +217,37 @@ def test_pools_of_more_bytes_than_there_are_addresses():
     assert copy([F[0]], [1 << 39], sources=[F[1]], rows=1, src_rows=1 << 25, n=0) == EINVAL
     p, s = arrays([F[0]], [(1 << 40) - 256])
     assert lib.hagdn_pool_compact(p, s, 1, F[1], 3, 1 << 20, F[3], F[4], 100, None) == EWS  # 2^60 bytes do
+
+
+def test_plans_overlaps():
+    """A plan's tables and workspace lie apart from the pools that it moves rows of and from each other:
+    the copies would write over them while they are read."""
+    lib = P.load_library()
+    p, s = arrays([F[5], F[0]], [64, 64])
+    size = lib.hagdn_pool_workspace_size(8)
+    fork = lambda **o: lib.hagdn_pool_fork(*{**dict(p=p, s=s, n=2, slots=F[1], N=3, parents=F[2], M=4, S=8, out=F[3], ws=F[4],
+                                                     wsb=BIG, stream=None), **o}.values())
+    compact = lambda **o: lib.hagdn_pool_compact(*{**dict(p=p, s=s, n=2, slots=F[1], N=3, S=8, out=F[3], ws=F[4], wsb=BIG,
+                                                           stream=None), **o}.values())
+    inside = F[0] + 64 * 7 + 48  # the last pool's last row
+    for f in (fork, compact):
+        for over in (dict(slots=inside), dict(out=inside), dict(ws=inside), dict(ws=F[0] - 16), dict(slots=F[5] - 4),
+                     dict(ws=F[1]), dict(ws=F[3]), dict(slots=F[4] + 16), dict(out=F[4] + size - 4), dict(slots=F[4] - 4)):
+            assert f(**over) == EINVAL and "overlaps" in lib.hagdn_last_error().decode(), over
+    for over in (dict(parents=inside), dict(ws=F[2]), dict(parents=F[4] + 64)):
+        assert fork(**over) == EINVAL and "overlaps" in lib.hagdn_last_error().decode(), over
+    # neighbours do not overlap: these stop at the workspace that is too small
+    for f in (fork, compact):
+        assert f(wsb=size - 4, slots=F[0] + 512, ws=F[0] - 16 * (size // 16 + 1), out=F[5] - 16) == EWS
+
+
+@pytest.mark.parametrize("fn,d", [("hagdn_conv_prefill", CONV), ("hagdn_conv_backward", CONV_BACK), ("ssm_prefill", SSM),
+                                  ("ssm_backward", SSM_BACK)], ids=["conv", "conv backward", "scan", "scan backward"])
+def test_workspace_overlaps(fn, d):
+    """A workspace lies apart from everything else that the call reads or writes."""
+    for name, place in d.items():
+        if isinstance(place, int) and place >= F[0] and name != "ws":
+            rc, msg = call(fn, d, wsb=BIG, ws=place)
+            assert rc == EINVAL and "overlaps" in msg, (name, rc, msg)
+            rc, msg = call(fn, d, wsb=BIG, ws=place - 16)
+            assert rc == EINVAL and "overlaps" in msg, (name, rc, msg)
