@@ -380,11 +380,10 @@ int hagdn_conv_decode(const void *x, int64_t x_stride, const float *weight, cons
  *   between tokens);
  *   A [D, S], skip [D] (or NULL) fp32;  S = 1 .. 64;  D % G == 0;
  *   states [N, D, S] fp32; s0 NULL: zero.
- * dt A <= 0 is expected: where some 500 tokens together let a state grow by e^88
- * results are unspecified.  N x D x S below 2^31, T_total up to 2^31 - 2^16.  Sums and states
- * are fp32.  Outputs and workspace must not overlap inputs or each other (s_final not even s0
- * exactly, nor ds0 dfinal).  Results repeat bit for bit on one device.  No value of one sequence
- * reaches another. */
+ * dt A <= 0 is expected; where it is not, states grow, and their errors with them.
+ * N x D x S below 2^31, T_total up to 2^31 - 2^16.  Sums and states are fp32.  Outputs and
+ * workspace must not overlap inputs or each other (s_final not even s0 exactly, nor ds0 dfinal).
+ * Results repeat bit for bit on one device.  No value of one sequence reaches another. */
 
 /* Bytes of workspace (0 on invalid sizes); backward 1: of ssm_backward. */
 size_t ssm_workspace_size(int T_total, int D, int S, int G, int backward);

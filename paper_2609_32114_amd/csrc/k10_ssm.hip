@@ -147,8 +147,11 @@ template <bool BACKWARD, bool HELD> __global__ __launch_bounds__(1024) void ssm_
     const int k = BACKWARD ? a.chunks - 1 - i : i;
     return i < min(hi, a.chunks - 1) ? Passed{*place(i), a.sums[(size_t)k * a.D + c], uniform(a.resets[k]) != 0} : Passed{0.f, 0.f, false};
   };
+  // The factor is applied as two of half its exponent, and not to a state of zero: over a run of
+  // chunks a positive rate may pass fp32's range where the state itself, small or not fed yet, does not.
   const auto fold = [&](const Passed &p, float s) {
-    return p.reset ? p.left : __builtin_fmaf(__builtin_amdgcn_exp2f(rate * p.sum), s, p.left);
+    const float half = __builtin_amdgcn_exp2f(0.5f * rate * p.sum);
+    return p.reset || s == 0.f ? p.left : __builtin_fmaf(half, half * s, p.left);
   };
   Passed held[kHeld];
   float state = 0.f, sum = 0.f;

@@ -384,3 +384,26 @@ def test_repeats_bit_for_bit(S):
     d = make(lens, 520, S, seed=6)
     a, b = run(d, lens, True), run(d, lens, True)
     assert all(torch.equal(a[k], b[k]) for k in a)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("S", [2, 20])
+def test_slow_growth_over_many_chunks(S):
+    """Rates above zero, with less than e^60 in any 500 tokens but more than fp32 holds over a run of
+    the carry's chunks: a state that is still zero, or small enough, stays what it is."""
+    import torch
+    D, T = 8, 16384
+    for form in ("zero", "small"):
+        d = make((T,), D, S, 1, "f32", "f32", False, False, False, form == "small", seed=S)
+        d["A"][:, 0] = 0.6
+        d["dt"] = torch.full((T, D), 0.2)
+        if form == "zero":  # fed in the last 400 tokens only, read (in the backward pass) in the first 300
+            d["A"][:, 1:] = -0.6
+            d["x"][:T - 400] = 0.0
+            d["dy"][300:] = 0.0
+        else:  # e^120 in 1000 tokens, from 1e-20 on, and nothing after them
+            d["dt"][:1024] = d["dt"][2024:] = 0.0
+            d["s0"] *= 1e-20
+            d["dfinal"] *= 1e-20
+            d["x"][:] = d["dy"][:] = 0.0
+        check(run(d, (T,), False), expected(d, (T,), False), "f32", "f32", f"growth from {form} S={S}")
