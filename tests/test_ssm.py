@@ -407,3 +407,39 @@ def test_slow_growth_over_many_chunks(S):
             d["dfinal"] *= 1e-20
             d["x"][:] = d["dy"][:] = 0.0
         check(run(d, (T,), False), expected(d, (T,), False), "f32", "f32", f"growth from {form} S={S}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("S", [16, 17, 20, 32, 33, 40, 64])
+@pytest.mark.parametrize("D,G,pick", [(8192, 1, (0, 63, 64, 4097, 8191)), (4096, 64, (0, 63, 4032, 4095)),
+                                      (4104, 2, (0, 2051, 2052, 4103))])
+def test_chunks_of_many_groups(D, G, pick, S):
+    """Backward chunks of several groups of 16 tokens for every padded number of states, in workgroups
+    of one wave and of four, the last of whose lanes lie beyond a group of channels: a few channels
+    against the plain form in 64 bits (in the others, x and dy are zero)."""
+    import torch
+    import paper_2609_32114_amd as P
+    lens = (1500, 700, 1, 400)
+    T, where = sum(lens), torch.tensor(pick)
+    groups = sorted({c // (D // G) for c in pick})
+    dtype = "f32" if S in (20, 40) else "bf16"
+    d = make(lens, len(pick), S, len(groups), dtype, "f32", seed=D + S, slow=True)
+    wide = {}
+    for k, v in d.items():
+        axis = 0 if k in ("A", "skip", "bias") else 1
+        shape = list(v.shape)
+        shape[axis] = G if k in ("B", "C") else D
+        wide[k] = torch.zeros(shape, dtype=v.dtype)
+        wide[k].index_copy_(axis, torch.tensor(groups) if k in ("B", "C") else where, v)
+    wide["A"][wide["A"] == 0] = -1.0
+    # tokens of a chunk, from the parts of the workspace that grow with the number of chunks
+    padded = 16 if S <= 16 else 32 if S <= 32 else 64
+    teams = -(-(D // G) // 64) if D // G < 193 else -(-(D // G) // 256)
+    rest = P.ssm_workspace_size(T, D, S, G, True) - teams * T * G * 2 * padded * 4
+    assert T / (rest / ((2 * padded + 3) * D * 4)) > 40
+    got = run(wide, lens, True)
+    narrow = {}
+    for k, v in got.items():
+        axis = 0 if k in ("dA", "dskip", "dbias") else 1
+        narrow[k] = v.index_select(axis, torch.tensor(groups if k in ("dB", "dC") else pick, device="cuda"))
+    check(narrow, expected(d, lens, True), dtype, "f32", f"{T} x {D} x {S}, {G} groups")
