@@ -380,7 +380,9 @@ int hagdn_conv_decode(const void *x, int64_t x_stride, const float *weight, cons
  *   between tokens);
  *   A [D, S], skip [D] (or NULL) fp32;  S = 1 .. 64;  D % G == 0;
  *   states [N, D, S] fp32; s0 NULL: zero.
- * dt A <= 0 is expected; where it is not, states grow, and their errors with them.
+ * dt A <= 0 is expected; where it is not, states grow, and their errors with them.  An infinite
+ * operand or state may give NaN where the formula gives an infinity, in its sequence (and in the
+ * sums over sequences: dA, dskip, d_dt_bias).
  * N x D x S below 2^31, T_total up to 2^31 - 2^16.  Sums and states are fp32.  Outputs and
  * workspace must not overlap inputs or each other (s_final not even s0 exactly, nor ds0 dfinal).
  * Results repeat bit for bit on one device.  No value of one sequence reaches another. */
@@ -447,7 +449,7 @@ int hagdn_pool_copy(void *const *pools, const void *const *sources, const size_t
  * name: the children must be all that the pools hold.  new_slots [M] receives the
  * children's slots, -1 for a parent outside [0, N) or in no slot of the pools, and for
  * children beyond the free slots (hagdn_device_status: HAGDN_DEV_POOL_FULL).  new_slots
- * must not overlap slots or parents; tables and workspace overlap neither pools nor each other.
+ * must not overlap slots or parents, tables and workspace no pool, the workspace no table.
  * Rows that are free afterwards keep what they held. */
 size_t hagdn_pool_workspace_size(int num_slots);
 int hagdn_pool_fork(void *const *pools, const size_t *row_bytes, int num_pools,
@@ -458,7 +460,7 @@ int hagdn_pool_fork(void *const *pools, const size_t *row_bytes, int num_pools,
  * slots, those from L on move, in order, to the free ones below L.  new_slots [N] (it may be
  * slots itself) receives the table after it; entries outside the pools (padding, ended
  * sequences) stay as they are.  Entries that name one slot still name one.  Tables and workspace
- * overlap no pool. */
+ * must not overlap the pools, nor the workspace the tables. */
 int hagdn_pool_compact(void *const *pools, const size_t *row_bytes, int num_pools,
                        const int32_t *slots, int N, int num_slots, int32_t *new_slots,
                        void *workspace, size_t workspace_bytes, void *stream);

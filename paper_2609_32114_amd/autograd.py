@@ -173,5 +173,6 @@ def conv(x, weight, bias=None, initial_window=None, cu_seqlens=None, activation=
 def ssm(x, dt, A, B, C, skip=None, z=None, dt_bias=None, initial_state=None, cu_seqlens=None, preprocess=0,
         workspace=None):
     """Differentiable ssm_prefill: (y, final state).  A ``workspace`` must suffice for
-    ssm_backward."""
+    ssm_backward.  States are saved in every call: where nothing is differentiated,
+    ssm_prefill saves writing them."""
     return _Ssm.apply(x, dt, A, B, C, skip, z, dt_bias, initial_state, cu_seqlens, preprocess, workspace)

@@ -212,7 +212,6 @@ int check_pools(void *const *pools, const size_t *row_bytes, int num_pools) {
 struct Range {
   uintptr_t at;
   size_t bytes;
-  int index;
   bool source;
 };
 bool ranges_disjoint(Range *r, int n) {
@@ -252,8 +251,8 @@ int check_ranges(void *const *pools, const void *const *sources, const size_t *r
     const int most = sources && src_rows > dst_rows ? src_rows : dst_rows;
     if (__builtin_mul_overflow(row_bytes[p], (size_t)most, &bytes) || bytes >> 62)
       return fail(HAGDN_EINVAL, "pools[%d] too large (%d rows of %zu bytes)", p, most, row_bytes[p]);
-    r[n++] = {(uintptr_t)pools[p], row_bytes[p] * (size_t)dst_rows, p, false};
-    if (sources) r[n++] = {(uintptr_t)sources[p], row_bytes[p] * (size_t)src_rows, p, true};
+    r[n++] = {(uintptr_t)pools[p], row_bytes[p] * (size_t)dst_rows, false};
+    if (sources) r[n++] = {(uintptr_t)sources[p], row_bytes[p] * (size_t)src_rows, true};
   }
   return ranges_disjoint(r, n) ? HAGDN_OK : fail(HAGDN_EINVAL, "pools overlap each other or a source");
 }

@@ -54,8 +54,8 @@ hipError_t launch_conv_step(const ConvStepArgs &, bool bf16, hipStream_t);
 // Writes whether cu[0 .. N] are the offsets of N sequences over T tokens to *status.
 hipError_t launch_check_offsets(const int32_t *cu, int N, int T, int *status, hipStream_t);
 
-// The backward pass's runs of tokens: a wave goes over one run of 256 channels (64 in calls
-// of odd widths below four).
+// The backward pass's runs of tokens: a wave goes over one run of 256 channels (of 64 in calls
+// below 256 channels).
 inline int conv_run(int T, int D, int cus) {
   const long cols = ((long)D + 255) / 256, waves = 16l * (cus > 0 ? cus : 256);
   const long run = ((long)T * cols + waves - 1) / waves;
@@ -124,8 +124,8 @@ inline long ssm_teams(int D, int G) { return (ssm_columns(D, G) + ssm_waves(D, G
 // Tokens of a chunk, which a workgroup goes over.  The scan is bound by its arithmetic, so that
 // every CU should get as many workgroups as the others: one round of what can be resident (by
 // registers and LDS), or in calls where a chunk would pass 512 tokens as few rounds as keep it
-// below.  (17401 x 2048 tokens in 68 chunks of 256, 2.1 workgroups a CU: outputs 230 us, backward
-// 1022; in chunks of 136 and 288 160 and 760.)  Calls of up to 64 tokens of 16 states are one
+// below.  (17401 x 2048 tokens in 68 chunks of 256, 2.1 workgroups a CU: outputs 203 us, backward
+// 913; in chunks of 136 and 272 149 and 632 to 666.)  Calls of up to 64 tokens of 16 states are one
 // chunk, which needs one launch instead of three.
 inline int ssm_chunk(int T, int D, int S, int G, int cus, bool backward) {
   const auto over = [](long a, long b) { return (a + b - 1) / b; };

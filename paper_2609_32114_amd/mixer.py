@@ -24,6 +24,7 @@ from .layer import (_F32, _check, _fp32, _like, _matrix, _output, _rows, _same_t
                     _workspace)
 
 _ACTIVATIONS = {"silu": 0, None: 2}
+_CHECKED_IN_PLACE = 512  # sequences up to which hagdn_conv_prefill takes calls without a workspace
 
 
 def _activation(name):
@@ -94,7 +95,7 @@ def conv_prefill(x, weight, bias=None, initial_window=None, cu_seqlens=None, act
     if initial_window is not None:
         _check_buffer("initial_window", initial_window, x.device, x.dtype, windows)
     ws, ws_bytes = None, 0  # only a caller's own tells of malformed offsets
-    if workspace is not None or N > 512:
+    if workspace is not None or N > _CHECKED_IN_PLACE:
         ws, ws_bytes = _workspace(workspace, lambda: conv_workspace_size(T, D, W), x)
     y = _like("out", out, x)
     final = _output("final_out", final_out, windows, x.dtype, x) if output_final_window else None

@@ -2,7 +2,7 @@
 token by token, with bounds on what the fp32 kernels may differ by, in the manner of
 layer_ref.py.
 
-The reckoning, made before the kernels ran.  One fp32 rounding costs half of EPS = 2^-23
+The reckoning, from the kernels' arithmetic.  One fp32 rounding costs half of EPS = 2^-23
 relative.  A logistic function is off by (|v| + 5) EPS relative (the exponent's product,
 an ulp each of exponential and reciprocal), its product or slope by 3 EPS more.  A step
 size log(1 + e^v) is off by (2 |v| + 8) EPS relative: v's own sum, the exponential, the
