@@ -63,7 +63,7 @@ def test_scan(T, D, G, S):
                      stream=torch.cuda.current_stream().cuda_stream)
         pointers = lambda d: {k: v.data_ptr() for k, v in d.items()}
         ws = g.place("workspace", (size,), torch.uint8)
-        assert call("ssm_prefill", SSM, **pointers({**shared, **outs, "ws": ws}), **sizes, wsb=size) == (0, "")
+        assert call("ssm_prefill", SSM, **pointers({**shared, **outs, "ws": ws}), **sizes, wsb=size)[0] == 0
         g.check()
         back = {"dx": g.place("dx", (T, D), dtype), "ddt": g.place("ddt", (T, D), torch.float32),
                 "dA": g.place("dA", (D, S), torch.float32), "dB": g.place("dB", (T, G, S), dtype),
